@@ -343,6 +343,108 @@ MOE_API int moe_layer_bwd_inputs_in(const moe_cfg* cfg, const moe_layer_bufs* b,
 MOE_API int moe_layer_expert_dw(const moe_cfg* cfg, const moe_layer_bufs* const* calls, int32_t n, int32_t accumulate, void* stream);
 
 /*
+ * Scored routing: the gate of layers with many experts.
+ *   s = softmax(logits) or sigmoid(logits); c = s + balance (balance: fp32 [E] or NULL; it takes part in the choice only, has no
+ *   gradient, and is what a trainer moves to even out the load);
+ *   groups > 1: the experts form `groups` equal runs; a group's score is its best c (group_rank 1) or the sum of its two best
+ *   (group_rank 2), and only the top_groups best groups stay (equal scores: lower group);
+ *   the k best c among them are chosen, best first, equal values by ascending expert id;
+ *   topk_w[t][j] = scale * s_j / (renorm ? sum of the chosen s : 1).
+ * An expert whose logit (or balance) is minus infinity or NaN is never chosen; a logit of plus infinity counts as the largest
+ * finite number.  A slot for which no expert is left has topk_idx = -1 and topk_w = 0, which every later call treats as a dropped
+ * assignment.  (A group with fewer than group_rank experts that can be chosen scores minus infinity.)
+ * The order is that of double precision scores: where single precision cannot tell two keys apart they are compared in double.
+ * The product with Wr is moe_route's; bias is added to the logits as there.  If logits_in is given the product is skipped, x and Wr
+ * may be NULL and logits_out is not written.  1 <= groups <= 16 and divides E; group_rank <= E / groups; top_groups <= groups and
+ * top_groups * (E / groups) >= k, else MOE_ERR_BAD_SHAPE.  scale must be finite.
+ */
+#define MOE_MAX_GROUPS 16
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct moe_score {
+  int32_t score;       /* MOE_SCORE_* */
+  int32_t groups;
+  int32_t top_groups;
+  int32_t group_rank;  /* 1 or 2 */
+  int32_t renorm;
+  float scale;
+} moe_score;
+MOE_API int moe_route_scored(const moe_cfg* cfg, const moe_score* score, const void* x, const float* Wr, const float* bias,
+                     const float* balance, const float* logits_in, float* logits_out, int32_t* topk_idx, float* topk_w,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward: d_logits[T][E] from d_topk_w, then as in moe_route_bwd dWr = x^T d_logits (NULL: skipped; `accumulate`) and
+ * dx += d_logits Wr^T (NULL: skipped).  `logits` are those the choice was made on.  ws is needed for dWr and dx only.
+ * With p_j = topk_w[j] / scale and D = sum_j p_j d_topk_w[j], d_logits of the chosen experts is, renorm: scale p_j (dw_j - D),
+ * for sigmoid times 1 - s_j; else sigmoid: scale s_j (1 - s_j) dw_j; zero for the others.  Softmax without renorm has a gradient for
+ * every expert: scale s_e ([e chosen] dw_e - D).  Experts that cannot be chosen get zero.
+ */
+MOE_API int moe_route_scored_bwd(const moe_cfg* cfg, const moe_score* score, const void* x, const float* Wr, const float* logits,
+                     const int32_t* topk_idx, const float* d_topk_w, float* d_logits, float* dWr, void* dx, int32_t accumulate,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Activations in 8 bits.  A row is cut into blocks of 32 values (the last one filled up with zeros) that share a power of two:
+ * codes [rows][blocks * 32] bytes and scales [rows][blocks] bytes, value = element(code) * 2^(scale - 127), element an e4m3 number
+ * (MOE_PACK_E4M3) or a two's complement number of 64ths (MOE_PACK_I8); the MXFP8 and MXINT8 formats of the OCP microscaling
+ * specification.  The scale is the smallest from 2^-127 to 2^127 with which the block's largest magnitude does not exceed the largest
+ * element (numbers of 64ths next to 2^128 saturate); codes are
+ * rounded to nearest, ties to even.  A block with an infinity or NaN gets scale 255 and unpacks to NaN.  Unpacked values are clamped
+ * to the largest finite number of their type.
+ * moe_pack8 / moe_unpack8: any dense matrix of `rows` rows and `width` columns of storage type `dtype`, `pitch` (>= width)
+ * elements from row to row; rows that start at multiples of 16 bytes are moved 16 bytes at a time.  rows * pitch < 2^40.
+ */
+enum { MOE_PACK_NONE = 0, MOE_PACK_E4M3 = 1, MOE_PACK_I8 = 2 };
+MOE_API int moe_pack8_bytes(int64_t rows, int32_t width, size_t* codes, size_t* scales);
+MOE_API int moe_pack8(int32_t dtype, int32_t fmt, int64_t rows, int32_t width, int64_t pitch, const void* src, void* codes, void* scales, void* stream);
+MOE_API int moe_unpack8(int32_t dtype, int32_t fmt, int64_t rows, int32_t width, int64_t pitch, const void* codes, const void* scales, void* dst, void* stream);
+
+/*
+ * Checkpoints of the expert FFN in 8 bits, instead of its GEMM again (moe_expert_ffn_recompute).  moe_saved_pack8 packs the
+ * pre-activation plane(s) of `saved` (GELU: A; SwiGLU: G, U), [planes][T*k] rows of d_ff; moe_saved_restore8 fills every plane of
+ * a `saved` buffer from them, the hidden plane computed anew from the unpacked values, ready for moe_expert_ffn_bwd.  Rows outside
+ * the shares are neither read nor written.
+ */
+MOE_API int moe_saved_pack8_bytes(const moe_cfg* cfg, size_t* codes, size_t* scales);
+MOE_API int moe_saved_pack8(const moe_cfg* cfg, int32_t fmt, const void* saved, const int32_t* offsets, const int32_t* kept,
+                    const int32_t* slice_lo, const int32_t* slice_hi, void* codes, void* scales, void* stream);
+MOE_API int moe_saved_restore8(const moe_cfg* cfg, int32_t fmt, const void* codes, const void* scales, const int32_t* offsets,
+                       const int32_t* kept, const int32_t* slice_lo, const int32_t* slice_hi, void* saved, void* stream);
+
+/*
+ * A dense product with its epilogue, the shared expert's: y = act(x W + bias) + residual.
+ *   x [T][d_in], W, Wb [d_in][d_out], bias, bias_b [d_out], residual, y, pre, pre_b [T][d_out], all in the storage type `dtype`.
+ *   act MOE_ACT_NONE: z + r; MOE_ACT_GELU: gelu_erf(z) + r; MOE_ACT_SWIGLU: silu(x W + bias) * (x Wb + bias_b) + r.
+ * Wb, bias_b, pre_b for SwiGLU only.  bias, bias_b, residual may be NULL; residual may be y itself.  pre, pre_b: the
+ * pre-activations as the backward wants them, NULL: not kept (always for MOE_ACT_NONE).
+ * Sums are fp32, the epilogue works on them in fp32 and rounds once.
+ *
+ * Backward: dz = dy act'(pre) (the residual's gradient is dy itself), dbias = sum over the tokens of dz,
+ * dW = x^T dz, dx = dz W^T (SwiGLU: + dz_b Wb^T) + dx_add (NULL: nothing; may be dx itself).  dx, dW, dbias may be NULL: skipped.
+ * dz is rounded to the storage type for the products; dbias sums it before that.
+ * moe_linear.pre_pack: how pre, pre_b come: MOE_PACK_NONE in the storage type, else as moe_pack8's codes with pre_scales,
+ * pre_b_scales.  moe_linear.grad: type of dW, dWb, dbias, dbias_b: MOE_DTYPE_F32 (accumulate != 0 adds to them) or the storage
+ * type (accumulate must be 0).
+ * Shapes: T >= 0 (0: fp32 gradients are left as they are or zeroed); d_in, d_out multiples of 64 (16-bit) or 4 (fp32), and
+ * d_in * d_out * 4 < 2^32; T <= 2^24.
+ * `ws` holds moe_linear_workspace_bytes and is free again when the call is done.
+ */
+enum { MOE_ACT_NONE = 2 };   /* moe_linear only */
+typedef struct moe_linear {
+  int32_t T, d_in, d_out;
+  int32_t dtype;      /* MOE_DTYPE_* */
+  int32_t act;        /* MOE_ACT_* */
+  int32_t pre_pack;   /* MOE_PACK_* */
+  int32_t grad;       /* MOE_DTYPE_F32 or dtype */
+} moe_linear;
+MOE_API int moe_linear_workspace_bytes(const moe_linear* lin, size_t* bytes);
+MOE_API int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,
+                   const void* residual, void* pre, void* pre_b, void* y, void* ws, size_t ws_bytes, void* stream);
+MOE_API int moe_linear_bwd(const moe_linear* lin, const void* dy, const void* x, const void* W, const void* Wb, const void* pre,
+                   const void* pre_b, const void* pre_scales, const void* pre_b_scales, const void* dx_add, void* dx,
+                   void* dW, void* dWb, void* dbias, void* dbias_b, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Planner of the asymmetric expert assignment (Section 4.2 of the paper, Algorithm 1 and the paragraph
  * on memory limits).  HOST-ONLY: runs on the CPU, enqueues nothing, and `o` is a HOST pointer.
  *

@@ -14,14 +14,17 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
 
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
-ACT_GELU, ACT_SWIGLU = 0, 1
-MAX_E, MAX_K = 256, 8
+ACT_GELU, ACT_SWIGLU, ACT_NONE = 0, 1, 2   # ACT_NONE: moe_linear only
+MAX_E, MAX_K, MAX_GROUPS = 256, 8, 16
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+PACK_NONE, PACK_E4M3, PACK_I8 = 0, 1, 2
 
 SYMBOLS = ("moe_error_string", "moe_last_hip_error", "moe_workspace_bytes", "moe_saved_bytes", "moe_route",
            "moe_dispatch", "moe_dispatch_static", "moe_expert_ffn_fwd", "moe_expert_ffn_fwd_light", "moe_expert_ffn_recompute", "moe_combine", "moe_combine_bwd", "moe_expert_ffn_bwd", "moe_expert_ffn_bwd_inputs",
            "moe_route_bwd", "moe_layer_fwd", "moe_layer_bwd", "moe_layer_bwd_inputs_ws_bytes", "moe_layer_bwd_inputs",
            "moe_layer_bwd_inputs_room_bytes", "moe_layer_bwd_inputs_in",
-           "moe_layer_expert_dw", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
+           "moe_layer_expert_dw", "moe_route_scored", "moe_route_scored_bwd", "moe_pack8_bytes", "moe_pack8", "moe_unpack8",
+           "moe_saved_pack8_bytes", "moe_saved_pack8", "moe_saved_restore8", "moe_linear_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
 
 PROF = {"gemm1_fwd": 0, "gemm2_fwd": 1, "dh_bwd": 2, "dw2_bwd": 3, "dw1_bwd": 4, "dx_bwd": 5, "gather": 6,
         "combine": 7, "combine_bwd": 8, "route": 9}
@@ -47,6 +50,14 @@ class MoeCfg(ctypes.Structure):
                [("prof", ctypes.POINTER(MoeProf))]
 
 
+class MoeScore(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "top_groups", "group_rank", "renorm")] + [("scale", ctypes.c_float)]
+
+
+class MoeLinear(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d_in", "d_out", "dtype", "act", "pre_pack", "grad")]
+
+
 class MoeError(RuntimeError):
     def __init__(self, fn, code, text, hip):
         super().__init__(f"{fn} failed: {code} ({text})" + (f", hipError {hip}" if code == -6 else ""))
@@ -66,7 +77,7 @@ def lib():
         l.moe_error_string.restype = ctypes.c_char_p
         l.moe_error_string.argtypes = [ctypes.c_int]
         l.moe_last_hip_error.restype = ctypes.c_int
-        p, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+        p, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         cfgp = ctypes.POINTER(MoeCfg)
         sig = {
             "moe_workspace_bytes": [cfgp, ctypes.POINTER(ctypes.c_size_t)],
@@ -89,6 +100,17 @@ def lib():
             "moe_layer_bwd_inputs_room_bytes": [cfgp, ctypes.POINTER(ctypes.c_size_t)],
             "moe_layer_bwd_inputs_in": [cfgp, p, p, sz, i32, p],
             "moe_layer_expert_dw": [cfgp, p, i32, i32, p],
+            "moe_route_scored": [cfgp, ctypes.POINTER(MoeScore)] + [p] * 9 + [sz, p],
+            "moe_route_scored_bwd": [cfgp, ctypes.POINTER(MoeScore)] + [p] * 8 + [i32, p, sz, p],
+            "moe_pack8_bytes": [i64, i32] + [ctypes.POINTER(sz)] * 2,
+            "moe_pack8": [i32, i32, i64, i32, i64] + [p] * 4,
+            "moe_unpack8": [i32, i32, i64, i32, i64] + [p] * 4,
+            "moe_saved_pack8_bytes": [cfgp] + [ctypes.POINTER(sz)] * 2,
+            "moe_saved_pack8": [cfgp, i32] + [p] * 8,
+            "moe_saved_restore8": [cfgp, i32] + [p] * 8,
+            "moe_linear_workspace_bytes": [ctypes.POINTER(MoeLinear), ctypes.POINTER(sz)],
+            "moe_linear_fwd": [ctypes.POINTER(MoeLinear)] + [p] * 10 + [sz, p],
+            "moe_linear_bwd": [ctypes.POINTER(MoeLinear)] + [p] * 14 + [i32, p, sz, p],
             "moe_asymea_plan": [i32] * 4 + [ctypes.c_double] * 3 + [i32, i32, ctypes.POINTER(i32)],
             "moe_asymea_shares": [i32] * 6 + [ctypes.POINTER(i32), ctypes.POINTER(i32)],
             "moe_bench_stream": [p, p, sz, i32, p],
@@ -295,6 +317,96 @@ def moe_layer_expert_dw(cfg, calls, accumulate=0, stream=None):
     ptrs = (ctypes.c_size_t * max(len(bufs), 1))(*[ctypes.addressof(b) for b in bufs])
     _check("moe_layer_expert_dw", lib().moe_layer_expert_dw(ctypes.byref(cfg), ptrs, len(bufs), int(accumulate),
                                                             _stream() if stream is None else stream))
+
+
+def make_score(score=SCORE_SOFTMAX, groups=1, top_groups=1, group_rank=1, renorm=1, scale=1.0) -> MoeScore:
+    return MoeScore(int(score), int(groups), int(top_groups), int(group_rank), int(renorm), float(scale))
+
+
+def moe_route_scored(cfg, score, x, Wr, bias, balance, logits_in, logits_out, topk_idx, topk_w, ws=None, stream=None, ws_bytes=None):
+    """Gate with softmax or sigmoid scores, a balance bias, groups of experts and renormalised weights."""
+    _check("moe_route_scored", lib().moe_route_scored(
+        ctypes.byref(cfg), ctypes.byref(score), _ptr(x), _ptr(Wr), _ptr(bias), _ptr(balance), _ptr(logits_in), _ptr(logits_out),
+        _ptr(topk_idx), _ptr(topk_w), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream() if stream is None else stream))
+
+
+def moe_route_scored_bwd(cfg, score, x, Wr, logits, topk_idx, d_topk_w, d_logits, dWr, dx, ws=None, accumulate=0, stream=None,
+                         ws_bytes=None):
+    _check("moe_route_scored_bwd", lib().moe_route_scored_bwd(
+        ctypes.byref(cfg), ctypes.byref(score), _ptr(x), _ptr(Wr), _ptr(logits), _ptr(topk_idx), _ptr(d_topk_w), _ptr(d_logits), _ptr(dWr),
+        _ptr(dx), int(accumulate), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream() if stream is None else stream))
+
+
+def _two_sizes(name, call):
+    a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(name, call(ctypes.byref(a), ctypes.byref(b)))
+    return a.value, b.value
+
+
+def moe_pack8_bytes(rows, width):
+    """Bytes of the codes and of the scales."""
+    return _two_sizes("moe_pack8_bytes", lambda a, b: lib().moe_pack8_bytes(int(rows), int(width), a, b))
+
+
+def _rows_ptr(t, width, pitch):
+    """A matrix whose rows are dense and `pitch` elements apart: a view of such a tensor, not only a contiguous one."""
+    if t is None or isinstance(t, int) or t.is_contiguous():
+        return _ptr(t)
+    if t.dim() != 2 or t.shape[1] != width or t.stride() != (pitch, 1):
+        raise ValueError("tensor must be contiguous, or rows of `width` elements `pitch` apart")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def moe_pack8(dtype, fmt, rows, width, pitch, src, codes, scales, stream=None):
+    """A matrix to 8 bits in blocks of 32 with a shared power of two."""
+    _check("moe_pack8", lib().moe_pack8(int(dtype), int(fmt), int(rows), int(width), int(pitch), _rows_ptr(src, width, pitch), _ptr(codes),
+                                        _ptr(scales), _stream() if stream is None else stream))
+
+
+def moe_unpack8(dtype, fmt, rows, width, pitch, codes, scales, dst, stream=None):
+    _check("moe_unpack8", lib().moe_unpack8(int(dtype), int(fmt), int(rows), int(width), int(pitch), _ptr(codes), _ptr(scales),
+                                            _rows_ptr(dst, width, pitch), _stream() if stream is None else stream))
+
+
+def moe_saved_pack8_bytes(cfg):
+    return _two_sizes("moe_saved_pack8_bytes", lambda a, b: lib().moe_saved_pack8_bytes(ctypes.byref(cfg), a, b))
+
+
+def moe_saved_pack8(cfg, fmt, saved, offsets, kept, slice_lo, slice_hi, codes, scales, stream=None):
+    """The pre-activation plane(s) of the expert FFN to 8 bits."""
+    _check("moe_saved_pack8", lib().moe_saved_pack8(ctypes.byref(cfg), int(fmt), _ptr(saved), _ptr(offsets), _ptr(kept), _ptr(slice_lo),
+                                                    _ptr(slice_hi), _ptr(codes), _ptr(scales), _stream() if stream is None else stream))
+
+
+def moe_saved_restore8(cfg, fmt, codes, scales, offsets, kept, slice_lo, slice_hi, saved, stream=None):
+    """Every saved plane from the packed pre-activations."""
+    _check("moe_saved_restore8", lib().moe_saved_restore8(ctypes.byref(cfg), int(fmt), _ptr(codes), _ptr(scales), _ptr(offsets), _ptr(kept),
+                                                          _ptr(slice_lo), _ptr(slice_hi), _ptr(saved), _stream() if stream is None else stream))
+
+
+def make_linear(T, d_in, d_out, dtype=DTYPE_BF16, act=ACT_NONE, pre=PACK_NONE, grad=DTYPE_F32) -> MoeLinear:
+    return MoeLinear(int(T), int(d_in), int(d_out), int(dtype), int(act), int(pre), int(grad))
+
+
+def moe_linear_workspace_bytes(lin) -> int:
+    n = ctypes.c_size_t(0)
+    _check("moe_linear_workspace_bytes", lib().moe_linear_workspace_bytes(ctypes.byref(lin), ctypes.byref(n)))
+    return n.value
+
+
+def moe_linear_fwd(lin, x, W, Wb, bias, bias_b, residual, pre, pre_b, y, ws, stream=None, ws_bytes=None):
+    """y = act(x W + bias) + residual."""
+    _check("moe_linear_fwd", lib().moe_linear_fwd(
+        ctypes.byref(lin), _ptr(x), _ptr(W), _ptr(Wb), _ptr(bias), _ptr(bias_b), _ptr(residual), _ptr(pre), _ptr(pre_b), _ptr(y), _ptr(ws),
+        _nbytes(ws) if ws_bytes is None else ws_bytes, _stream() if stream is None else stream))
+
+
+def moe_linear_bwd(lin, dy, x, W, Wb, pre, pre_b, pre_scales, pre_b_scales, dx_add, dx, dW, dWb, dbias, dbias_b, accumulate, ws, stream=None,
+                   ws_bytes=None):
+    _check("moe_linear_bwd", lib().moe_linear_bwd(
+        ctypes.byref(lin), _ptr(dy), _ptr(x), _ptr(W), _ptr(Wb), _ptr(pre), _ptr(pre_b), _ptr(pre_scales), _ptr(pre_b_scales), _ptr(dx_add),
+        _ptr(dx), _ptr(dW), _ptr(dWb), _ptr(dbias), _ptr(dbias_b), int(accumulate), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+        _stream() if stream is None else stream))
 
 
 def moe_asymea_plan(n, L, M, N, T_A_attn, T_E_attn, T_E_exp, n_min=0, n_max=-1):

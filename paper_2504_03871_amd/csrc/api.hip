@@ -1,6 +1,8 @@
 // C ABI of the MoE library: argument validation, workspace layout, kernel sequencing.
 #include "common.h"
 #include "gemm.h"
+#include "linear.h"
+#include "pack8.h"
 #include "prof.h"
 #include "tile_map.h"
 #include <algorithm>
@@ -92,6 +94,10 @@ int launch_combine(const moe_cfg*, const void*, const float*, const int32_t*, co
                    const int32_t*, const int32_t*, const int32_t*, void*, int, hipStream_t);
 int launch_combine_bwd(const moe_cfg*, const void*, const void*, const float*, const int32_t*, const int32_t*,
                        const int32_t*, const int32_t*, const int32_t*, const int32_t*, void*, float*, const SideWork*, hipStream_t);
+int launch_wr_transpose(const moe_cfg*, const float*, float*, hipStream_t);
+int launch_score(const moe_cfg*, const moe_score*, const float*, const float*, int32_t*, float*, hipStream_t);
+int launch_score_bwd(const moe_cfg*, const moe_score*, const float*, const int32_t*, const float*, float*, hipStream_t);
+int launch_score_dx(const moe_cfg*, const float*, const float*, void*, hipStream_t);
 bool input_grad_has_dwr(const moe_cfg*);
 int launch_input_grad(const moe_cfg*, const moe_layer_bufs*, const float*, float*, bool, hipStream_t);
 int launch_gate_dwr(const moe_cfg*, const void*, const float*, float*, int, float*, bool, hipStream_t);
@@ -338,6 +344,190 @@ int moe_route(const moe_cfg* cfg, const void* x, const float* Wr, const float* b
   void* wfrag = ws != nullptr ? static_cast<char*>(ws) + ws_layout(cfg).route_wrt : nullptr;
   ProfScope ps(cfg, MOE_PROF_ROUTE, (hipStream_t)stream);
   return launch_route(cfg, x, Wr, bias, logits_in, logits_out, topk_idx, topk_w, wfrag, (hipStream_t)stream);
+}
+
+static int check_score(const moe_cfg* c, const moe_score* s) {
+  if (s == nullptr) return MOE_ERR_NULL;
+  if (s->score != MOE_SCORE_SOFTMAX && s->score != MOE_SCORE_SIGMOID) return MOE_ERR_BAD_DTYPE;
+  if (s->groups < 1 || s->groups > MOE_MAX_GROUPS || c->E % s->groups != 0) return MOE_ERR_BAD_SHAPE;
+  const int size = c->E / s->groups;
+  if (s->group_rank < 1 || s->group_rank > 2 || s->group_rank > size) return MOE_ERR_BAD_SHAPE;
+  if (s->top_groups < 1 || s->top_groups > s->groups || s->top_groups * size < c->k) return MOE_ERR_BAD_SHAPE;
+  if (!(s->scale >= -3.4028234663852886e38f && s->scale <= 3.4028234663852886e38f)) return MOE_ERR_BAD_SHAPE;
+  return MOE_OK;
+}
+
+int moe_route_scored(const moe_cfg* cfg, const moe_score* score, const void* x, const float* Wr, const float* bias, const float* balance,
+                     const float* logits_in, float* logits_out, int32_t* topk_idx, float* topk_w, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_cfg(cfg));
+  CHECK(check_score(cfg, score));
+  if (logits_in == nullptr) { REQUIRE(x); REQUIRE(Wr); REQUIRE(logits_out); }
+  if (logits_in == nullptr && cfg->dtype != MOE_DTYPE_F32) REQUIRE(ws);   // the matrix-core gate (16-bit storage)
+  REQUIRE(topk_idx);
+  REQUIRE(topk_w);
+  ALIGNED(x); ALIGNED(Wr); ALIGNED(bias); ALIGNED(balance); ALIGNED(logits_in); ALIGNED(logits_out); ALIGNED(topk_idx); ALIGNED(topk_w);
+  ALIGNED(ws);
+  CHECK(check_ws(cfg, ws, ws_bytes));
+  if (cfg->T == 0) return MOE_OK;
+  const hipStream_t s = (hipStream_t)stream;
+  if (logits_in == nullptr) {   // the gate's product; what its own selection writes is overwritten
+    void* wfrag = ws != nullptr ? static_cast<char*>(ws) + ws_layout(cfg).route_wrt : nullptr;
+    ProfScope ps(cfg, MOE_PROF_ROUTE, s);
+    CHECK(launch_route(cfg, x, Wr, bias, nullptr, logits_out, topk_idx, topk_w, wfrag, s));
+    logits_in = logits_out;
+  }
+  return launch_score(cfg, score, logits_in, balance, topk_idx, topk_w, s);
+}
+
+int moe_route_scored_bwd(const moe_cfg* cfg, const moe_score* score, const void* x, const float* Wr, const float* logits,
+                         const int32_t* topk_idx, const float* d_topk_w, float* d_logits, float* dWr, void* dx, int32_t accumulate,
+                         void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_cfg(cfg));
+  CHECK(check_score(cfg, score));
+  REQUIRE(logits); REQUIRE(topk_idx); REQUIRE(d_topk_w); REQUIRE(d_logits);
+  if (dWr != nullptr) { REQUIRE(x); REQUIRE(ws); }
+  if (dx != nullptr) { REQUIRE(Wr); REQUIRE(ws); }
+  ALIGNED(x); ALIGNED(Wr); ALIGNED(logits); ALIGNED(topk_idx); ALIGNED(d_topk_w); ALIGNED(d_logits); ALIGNED(dWr); ALIGNED(dx); ALIGNED(ws);
+  CHECK(check_ws(cfg, ws, ws_bytes));
+  const hipStream_t s = (hipStream_t)stream;
+  if (cfg->T == 0) {
+    if (dWr == nullptr || accumulate) return MOE_OK;
+    const int n = cfg->d_model * cfg->E;
+    fill_zero_kernel<<<(n + 255) / 256, 256, 0, s>>>(dWr, n);
+    return launch_status();
+  }
+  const WsLayout w = ws_layout(cfg);
+  CHECK(launch_score_bwd(cfg, score, logits, topk_idx, d_topk_w, d_logits, s));
+  if (dx != nullptr) {
+    float* WrT = reinterpret_cast<float*>(static_cast<char*>(ws) + w.route_wrt);
+    CHECK(launch_wr_transpose(cfg, Wr, WrT, s));
+    CHECK(launch_score_dx(cfg, d_logits, WrT, dx, s));
+  }
+  if (dWr == nullptr) return MOE_OK;
+  return launch_gate_dwr(cfg, x, d_logits, dWr, accumulate, reinterpret_cast<float*>(static_cast<char*>(ws) + w.route_partials), false, s);
+}
+
+static int check_pack(int32_t dtype, int32_t fmt, int64_t rows, int32_t width, int64_t pitch) {
+  if (dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_F16) return MOE_ERR_BAD_DTYPE;
+  if (fmt != MOE_PACK_E4M3 && fmt != MOE_PACK_I8) return MOE_ERR_BAD_DTYPE;
+  if (rows < 0 || width < 1 || width > (1 << 24) || pitch < width || pitch > (1ll << 40)) return MOE_ERR_BAD_SHAPE;
+  if (rows > (1ll << 40) / pitch) return MOE_ERR_BAD_SHAPE;
+  return MOE_OK;
+}
+
+int moe_pack8_bytes(int64_t rows, int32_t width, size_t* codes, size_t* scales) {
+  CHECK(check_pack(MOE_DTYPE_F32, MOE_PACK_I8, rows, width, width));
+  REQUIRE(codes); REQUIRE(scales);
+  *scales = (size_t)rows * blocks8(width);
+  *codes = *scales * BLOCK8;
+  return MOE_OK;
+}
+
+int moe_pack8(int32_t dtype, int32_t fmt, int64_t rows, int32_t width, int64_t pitch, const void* src, void* codes, void* scales, void* stream) {
+  CHECK(check_pack(dtype, fmt, rows, width, pitch));
+  if (rows == 0) return MOE_OK;
+  REQUIRE(src); REQUIRE(codes); REQUIRE(scales);
+  ALIGNED(src); ALIGNED(codes); ALIGNED(scales);
+  return launch_pack8(dtype, fmt, rows, width, pitch, src, codes, scales, (hipStream_t)stream);
+}
+
+int moe_unpack8(int32_t dtype, int32_t fmt, int64_t rows, int32_t width, int64_t pitch, const void* codes, const void* scales, void* dst, void* stream) {
+  CHECK(check_pack(dtype, fmt, rows, width, pitch));
+  if (rows == 0) return MOE_OK;
+  REQUIRE(codes); REQUIRE(scales); REQUIRE(dst);
+  ALIGNED(codes); ALIGNED(scales); ALIGNED(dst);
+  return launch_unpack8(dtype, fmt, rows, width, pitch, codes, scales, dst, (hipStream_t)stream);
+}
+
+int moe_saved_pack8_bytes(const moe_cfg* cfg, size_t* codes, size_t* scales) {
+  CHECK(check_cfg(cfg));
+  REQUIRE(codes); REQUIRE(scales);
+  *scales = (size_t)(cfg->act == MOE_ACT_SWIGLU ? 2 : 1) * cfg->T * cfg->k * blocks8(cfg->d_ff);
+  *codes = *scales * BLOCK8;
+  return MOE_OK;
+}
+
+static int saved8_checks(const moe_cfg* cfg, int32_t fmt, const void* saved, const void* codes, const void* scales, const int32_t* offsets,
+                         const int32_t* kept, const int32_t* lo, const int32_t* hi) {
+  CHECK(check_cfg(cfg));
+  if (fmt != MOE_PACK_E4M3 && fmt != MOE_PACK_I8) return MOE_ERR_BAD_DTYPE;
+  CHECK(check_slices(lo, hi));
+  REQUIRE(saved); REQUIRE(codes); REQUIRE(scales); REQUIRE(offsets); REQUIRE(kept);
+  ALIGNED(saved); ALIGNED(codes); ALIGNED(scales); ALIGNED(offsets); ALIGNED(kept); ALIGNED(lo); ALIGNED(hi);
+  return MOE_OK;
+}
+
+int moe_saved_pack8(const moe_cfg* cfg, int32_t fmt, const void* saved, const int32_t* offsets, const int32_t* kept, const int32_t* slice_lo,
+                    const int32_t* slice_hi, void* codes, void* scales, void* stream) {
+  CHECK(saved8_checks(cfg, fmt, saved, codes, scales, offsets, kept, slice_lo, slice_hi));
+  if (cfg->T == 0) return MOE_OK;
+  return launch_saved_pack8(cfg, fmt, saved, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, codes, scales, (hipStream_t)stream);
+}
+
+int moe_saved_restore8(const moe_cfg* cfg, int32_t fmt, const void* codes, const void* scales, const int32_t* offsets, const int32_t* kept,
+                       const int32_t* slice_lo, const int32_t* slice_hi, void* saved, void* stream) {
+  CHECK(saved8_checks(cfg, fmt, saved, codes, scales, offsets, kept, slice_lo, slice_hi));
+  if (cfg->T == 0) return MOE_OK;
+  return launch_saved_restore8(cfg, fmt, codes, scales, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, saved, (hipStream_t)stream);
+}
+
+static int check_linear(const moe_linear* c) {
+  if (c == nullptr) return MOE_ERR_NULL;
+  if (c->dtype != MOE_DTYPE_F32 && c->dtype != MOE_DTYPE_BF16 && c->dtype != MOE_DTYPE_F16) return MOE_ERR_BAD_DTYPE;
+  if (c->act != MOE_ACT_NONE && c->act != MOE_ACT_GELU && c->act != MOE_ACT_SWIGLU) return MOE_ERR_BAD_DTYPE;
+  if (c->pre_pack != MOE_PACK_NONE && c->pre_pack != MOE_PACK_E4M3 && c->pre_pack != MOE_PACK_I8) return MOE_ERR_BAD_DTYPE;
+  if (c->grad != MOE_DTYPE_F32 && c->grad != c->dtype) return MOE_ERR_BAD_DTYPE;
+  const int mult = c->dtype == MOE_DTYPE_F32 ? 4 : 64;
+  if (c->T < 0 || c->T > (1 << 24) || c->d_in < 1 || c->d_out < 1 || c->d_in % mult != 0 || c->d_out % mult != 0) return MOE_ERR_BAD_SHAPE;
+  if ((long long)c->d_in * c->d_out * 4 >= (1ll << 32)) return MOE_ERR_BAD_SHAPE;
+  return MOE_OK;
+}
+
+int moe_linear_workspace_bytes(const moe_linear* lin, size_t* bytes) {
+  CHECK(check_linear(lin));
+  REQUIRE(bytes);
+  *bytes = linear_plan(lin).total;
+  return MOE_OK;
+}
+
+int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,
+                   const void* residual, void* pre, void* pre_b, void* y, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_linear(lin));
+  if (lin->T == 0) return MOE_OK;
+  REQUIRE(x); REQUIRE(W); REQUIRE(y);
+  const bool two = lin->act == MOE_ACT_SWIGLU;
+  if (two) REQUIRE(Wb);
+  if (!two && (Wb != nullptr || bias_b != nullptr || pre_b != nullptr)) return MOE_ERR_BAD_DTYPE;
+  if (lin->act == MOE_ACT_NONE && pre != nullptr) return MOE_ERR_BAD_DTYPE;
+  if (two && (pre == nullptr) != (pre_b == nullptr)) return MOE_ERR_NULL;
+  ALIGNED(x); ALIGNED(W); ALIGNED(Wb); ALIGNED(bias); ALIGNED(bias_b); ALIGNED(residual); ALIGNED(pre); ALIGNED(pre_b); ALIGNED(y); ALIGNED(ws);
+  const size_t need = linear_plan(lin).total;
+  if (need > 0) REQUIRE(ws);
+  if (ws_bytes < need) return MOE_ERR_WORKSPACE;
+  return launch_linear_fwd(lin, x, W, Wb, bias, bias_b, residual, pre, pre_b, y, ws, (hipStream_t)stream);
+}
+
+int moe_linear_bwd(const moe_linear* lin, const void* dy, const void* x, const void* W, const void* Wb, const void* pre, const void* pre_b,
+                   const void* pre_scales, const void* pre_b_scales, const void* dx_add, void* dx, void* dW, void* dWb, void* dbias,
+                   void* dbias_b, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_linear(lin));
+  const bool two = lin->act == MOE_ACT_SWIGLU, packed = lin->pre_pack != MOE_PACK_NONE;
+  if (!two && (Wb != nullptr || pre_b != nullptr || dWb != nullptr || dbias_b != nullptr)) return MOE_ERR_BAD_DTYPE;
+  if (accumulate && lin->grad != MOE_DTYPE_F32) return MOE_ERR_BAD_DTYPE;
+  if (two && ((dW == nullptr) != (dWb == nullptr) || (dbias == nullptr) != (dbias_b == nullptr))) return MOE_ERR_NULL;
+  ALIGNED(dy); ALIGNED(x); ALIGNED(W); ALIGNED(Wb); ALIGNED(pre); ALIGNED(pre_b); ALIGNED(pre_scales); ALIGNED(pre_b_scales); ALIGNED(dx_add);
+  ALIGNED(dx); ALIGNED(dW); ALIGNED(dWb); ALIGNED(dbias); ALIGNED(dbias_b); ALIGNED(ws);
+  if (lin->T > 0) {
+    REQUIRE(dy);
+    if (dW != nullptr) REQUIRE(x);
+    if (dx != nullptr) { REQUIRE(W); if (two) REQUIRE(Wb); }
+    if (lin->act != MOE_ACT_NONE) { REQUIRE(pre); if (two) REQUIRE(pre_b); }
+    if (lin->act != MOE_ACT_NONE && packed) { REQUIRE(pre_scales); if (two) REQUIRE(pre_b_scales); }
+    const size_t need = linear_plan(lin).total;
+    if (need > 0) REQUIRE(ws);
+    if (ws_bytes < need) return MOE_ERR_WORKSPACE;
+  }
+  return launch_linear_bwd(lin, dy, x, W, Wb, pre, pre_b, pre_scales, pre_b_scales, dx_add, dx, dW, dWb, dbias, dbias_b, accumulate, ws, (hipStream_t)stream);
 }
 
 int moe_dispatch(const moe_cfg* cfg, const void* x, const int32_t* topk_idx, const int32_t* slice_lo,

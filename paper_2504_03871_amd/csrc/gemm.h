@@ -267,7 +267,11 @@ enum Epilogue {
   EPI_SWIGLU_FWD = 2,  // dual accumulators g,u: C = g, C2 = u (both skipped when C is NULL), C3 = silu(g)*u
   EPI_GELU_BWD = 3,    // C = acc * gelu'(S1)
   EPI_SWIGLU_BWD = 4,  // C = dG = acc * S2 * silu'(S1), C2 = dU = acc * silu(S1)   (S1 = G, S2 = U)
-  EPI_DW = 5           // fp32 C_e = acc (+ C_e)
+  EPI_DW = 5,          // fp32 C_e = acc (+ C_e)
+  // dense products (DENSE below): z = acc + bias, C = z (skipped when C is NULL), C3 = act(z) + S1 (S1: residual, may be NULL)
+  EPI_LIN_NONE = 6,
+  EPI_LIN_GELU = 7,
+  EPI_LIN_SWIGLU = 8   // dual accumulators: C = z, C2 = z2, C3 = silu(z) z2 + S1
 };
 
 struct GemmArgs {
@@ -298,6 +302,11 @@ struct GemmArgs {
   int chunked;   // row-tile GEMMs: order of the full tiles (block_to_tile)
   int stream;    // row-tile GEMMs: row tiles from which on weights that one of them takes are requested as streaming data, 0: never (streamed_from)
   int tile_rows; // row-tile GEMMs: rows per entry of the tile map
+  // Dense products, one matrix and no experts, know their tiles without a map.  Row-tile GEMMs: M rows; tiles from split_first on
+  // are cut along K into split_parts (1: none).  Weight gradients: K rows in E segments of `seg`, each with a gradient of its own.
+  int split_first, split_parts, seg;
+  const void* bias;    // storage type, may be NULL
+  const void* bias2;
 };
 
 // blocks of a weight-gradient launch of bm x bn tiles (dw_block), of two gradients where the second is asked for

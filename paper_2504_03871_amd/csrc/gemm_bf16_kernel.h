@@ -327,7 +327,8 @@ __device__ __forceinline__ void epilogue_fwd(const OutPlanes& o, const unsigned 
 // products in a sum of their own that is added to the total: the sums, and their rounding, of call after call.
 // STREAM (row tiles): the weights of an expert with a single row tile are requested as streaming data (streamed_from).  A
 // template parameter because the choice, once per load, costs a main loop that never takes it 1 to 3 %.
-template <typename ST, int MODE, int EPI, bool DUAL, bool CHAIN, int BM, int BN, int WGM, int WGN, bool SEGS = false, bool STREAM = false>
+// DENSE: one matrix instead of one per expert, tiles from the sizes alone (GemmArgs).
+template <typename ST, int MODE, int EPI, bool DUAL, bool CHAIN, int BM, int BN, int WGM, int WGN, bool SEGS = false, bool STREAM = false, bool DENSE = false>
 __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, char* smem, const DwSegs* segs = nullptr) {
   constexpr int NT = WGM * WGN * 64;
   constexpr int WTM = (BM / 32 + WGM - 1) / WGM, WTN = BN / WGN / 32;   // (an odd number of bands: the last wave row has one less)
@@ -366,11 +367,14 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
       int slot, mt;
       if (!dw_block(vb, ntm, ntn, slot, mt, nt)) return;
       if (g.C2 != nullptr) { slot = __builtin_amdgcn_readfirstlane(slot); second = slot & 1; slot >>= 1; }   // the two gradients of an expert follow each other
-      e = g.order[slot];
+      e = DENSE ? __builtin_amdgcn_readfirstlane(slot) : g.order[slot];
       m0 = mt * BM;
       rt = 0;
       int l, h;
-      if constexpr (SEGS) {
+      if constexpr (DENSE) {   // segment e of the rows
+        row0 = e * g.seg;
+        klen = min(g.seg, g.K - row0);
+      } else if constexpr (SEGS) {
         static_assert(MODE == MODE_TN, "weight gradients");
         int all = 0;
 #pragma unroll
@@ -397,28 +401,29 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
       mvalid = min(BM, g.M - m0);
       if (klen == 0 && g.accumulate) return;
     } else {
-      constexpr bool CAN_SPLIT = EPI == EPI_STORE;
+      constexpr bool CAN_SPLIT = EPI == EPI_STORE || DENSE;
       const int kall = CHAIN ? 2 * g.K : g.K;
-      const int n_rt = g.ntiles[0];
+      const int n_rt = DENSE ? (g.M + BM - 1) / BM : g.ntiles[0], n_full_rt = DENSE ? g.M / BM : g.ntiles[1];
       RowBlock rb;
       klen = g.K;
       TailSplit ts = {0, 1};
-      if (CAN_SPLIT && g.split_tail) ts = tail_split(n_rt * ntn, kall);
+      if constexpr (DENSE) ts = TailSplit{g.split_first, g.split_parts};
+      else if (CAN_SPLIT && g.split_tail) ts = tail_split(n_rt * ntn, kall);
       if (CAN_SPLIT && ts.parts > 1) {          // the tiles of the last round are split along K
-        if (!tail_split_block(vb, n_rt, g.ntiles[1], ntn, g.chunked != 0, ts, rb)) return;
+        if (!tail_split_block(vb, n_rt, n_full_rt, ntn, g.chunked != 0, ts, rb)) return;
         if (rb.split_tile >= 0) {
           const int stages = kall / BKT, k0 = rb.ksplit * stages / ts.parts, k1 = (rb.ksplit + 1) * stages / ts.parts;
           if constexpr (CHAIN) { skip = k0; part_stages = k1 - k0; }
           else { kbase = k0 * BKT; klen = (k1 - k0) * BKT; }
-          part_sums = g.split_ws + (size_t)(rb.split_tile * ts.parts + rb.ksplit) * (BM * BN);
+          part_sums = g.split_ws + (size_t)(rb.split_tile * ts.parts + rb.ksplit) * (BM * BN * (DUAL ? 2 : 1));
           part_pitch = BN;
         }
       } else {
         // or the smallest row tiles: the last n_sp row tiles are not part of the regular numbering; their blocks
         // follow it, SPLIT_K per (row tile, column tile), each with a K range of its own
-        const int n_sp = (CAN_SPLIT && !CHAIN && g.split_small) ? g.ntiles[2] : 0;
-        if (!row_tile_block(vb, n_rt, g.ntiles[1], n_sp, ntn, g.chunked != 0, rb)) return;
-        if (CAN_SPLIT && !CHAIN && rb.split_tile >= 0) {
+        const int n_sp = (!DENSE && CAN_SPLIT && !CHAIN && g.split_small) ? g.ntiles[2] : 0;
+        if (!row_tile_block(vb, n_rt, n_full_rt, n_sp, ntn, g.chunked != 0, rb)) return;
+        if (!DENSE && CAN_SPLIT && !CHAIN && rb.split_tile >= 0) {
           klen = g.K / SPLIT_K;
           kbase = rb.ksplit * klen;
           part_sums = g.split_ws + (size_t)(rb.split_tile * SPLIT_K + rb.ksplit) * SPLIT_ROWS * g.N + rb.nt * BN;
@@ -432,7 +437,9 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
       klen = __builtin_amdgcn_readfirstlane(klen);
       skip = __builtin_amdgcn_readfirstlane(skip);
       part_stages = __builtin_amdgcn_readfirstlane(part_stages);
-      const RowTile t = g.tiles[rt];
+      RowTile t;
+      if constexpr (DENSE) t = RowTile{0, rt * BM, min(BM, g.M - rt * BM), 0};
+      else t = g.tiles[rt];
       e = t.e;
       row0 = t.row0;
       mvalid = t.nrows;
@@ -757,20 +764,24 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
   const int grp = lane >> 4, r8 = lane & 7, right = (lane >> 3) & 1;   // after swap8: row of eight, left or right half of a line
   auto band_row = [&](int i) { return ((i >> 1) * WGM + wm) * 32 + (i & 1) * 16; };   // first row of row tile i
   auto empty = [&](int i) { return band_row(i) >= mvalid; };
-  if (MODE != MODE_TN && EPI == EPI_STORE && part_sums != nullptr) {   // fp32 partial sums of this block's K part
+  if (MODE != MODE_TN && (EPI == EPI_STORE || DENSE) && part_sums != nullptr) {   // fp32 partial sums of this block's K part
+    auto put_sums = [&](f32x4 (&s)[TM][TNN], float* to) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-      if (!empty(i)) {
+      for (int i = 0; i < TM; ++i)
+        if (!empty(i)) {
 #pragma unroll
-        for (int j = 0; j < TNN; j += 2) {
-          swap8(acc[i][j], acc[i][j + 1]);
+          for (int j = 0; j < TNN; j += 2) {
+            swap8(s[i][j], s[i][j + 1]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int m = band_row(i) + h * 8 + r8;
-            if (m < mvalid) *reinterpret_cast<f32x4*>(part_sums + (size_t)m * part_pitch + wn * C + j * 16 + right * 16 + grp * 4) = acc[i][j + h];
+            for (int h = 0; h < 2; ++h) {
+              const int m = band_row(i) + h * 8 + r8;
+              if (m < mvalid) *reinterpret_cast<f32x4*>(to + (size_t)m * part_pitch + wn * C + j * 16 + right * 16 + grp * 4) = s[i][j + h];
+            }
           }
         }
-      }
+    };
+    put_sums(acc, part_sums);
+    if constexpr (DUAL && DENSE) put_sums(acc2, part_sums + BM * BN);   // the second matrix's behind the first's
     return;
   }
   if constexpr (MODE == MODE_TN) {   // fp32 weight gradient of expert e; M is a multiple of 64: whole bands
@@ -813,6 +824,71 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
 #pragma unroll
           for (int j = 0; j < TNN; ++j) buf_store16<AUX_NT>(rc, at(i, j), __builtin_bit_cast(u32x4, acc[i][j]));
         }
+    }
+  } else if constexpr (EPI >= EPI_LIN_NONE) {
+    // Bias, activation and residual on the fp32 sums: eight columns per lane, the residual requested AHEAD row tiles ahead.
+    constexpr int NH = TNN / 2, AHEAD = TNN == 4 ? 3 : 4;   // stores per row tile: of 8 rows x 128 bytes, or one of 16 x 64
+    typedef Half16<ST> H;
+    const size_t first = (size_t)row0 * g.N + n0, bytes = ((size_t)mvalid * g.N - n0) * 2;
+    auto plane = [&](const void* p) { return out_rsrc(reinterpret_cast<const ST*>(p) + (p != nullptr ? first : 0), p != nullptr ? bytes : 0); };
+    const __amdgpu_buffer_rsrc_t oy = plane(g.C3), oz = plane(g.C), oz2 = plane(DUAL ? g.C2 : g.C), res = plane(g.S1);
+    const unsigned pitch = (unsigned)g.N * 2u, lane_col = (unsigned)(wn * C + (TNN == 4 ? right * 32 : 0) + lane_col8(grp));
+    auto at = [&](int i, int h) {
+      const int m = band_row(i) + (TNN == 4 ? h * 8 + r8 : (lane & 15));
+      return m < mvalid ? (unsigned)m * pitch + lane_col * 2u : OUT_OF_RANGE;
+    };
+    auto up8 = [](const u32x4& r, float (&f)[8]) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) { f[2 * q] = H::lo(r[q]); f[2 * q + 1] = H::hi(r[q]); }
+    };
+    auto pk8 = [](const float (&f)[8]) { return u32x4{H::pack2(f[0], f[1]), H::pack2(f[2], f[3]), H::pack2(f[4], f[5]), H::pack2(f[6], f[7])}; };
+    u32x4 bias = {0u, 0u, 0u, 0u}, bias2 = {0u, 0u, 0u, 0u};
+    if (g.bias != nullptr) bias = *reinterpret_cast<const u32x4*>(reinterpret_cast<const ST*>(g.bias) + n0 + lane_col);
+    if (DUAL && g.bias2 != nullptr) bias2 = *reinterpret_cast<const u32x4*>(reinterpret_cast<const ST*>(g.bias2) + n0 + lane_col);
+    u32x4 rv[AHEAD][NH];
+    auto load_res = [&](int i) {   // no residual: a descriptor of no bytes, which returns zeros
+#pragma unroll
+      for (int h = 0; h < NH; ++h) rv[i % AHEAD][h] = buf_load16_nt(res, at(i, h));
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD - 1 && i < TM; ++i) load_res(i);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      if (i + AHEAD - 1 < TM) load_res(i + AHEAD - 1);
+      if (!empty(i)) {
+        auto to_rows = [&](f32x4 (&s)[TNN]) {   // rows 0-7: columns 0-3 in [0], 4-7 in [1]; rows 8-15: [2], [3]
+          join_tiles(s[0], s[1]);
+          if constexpr (TNN == 4) {
+            join_tiles(s[2], s[3]);
+            swap8(s[0], s[2]);
+            swap8(s[1], s[3]);
+          }
+        };
+        to_rows(acc[i]);
+        if constexpr (DUAL) to_rows(acc2[i]);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          float z[8], y[8], b[8], r[8];
+          up8(bias, b);
+          up8(rv[i % AHEAD][h], r);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) z[q] = acc[i][2 * h + q / 4][q % 4] + b[q];
+          if (EPI != EPI_LIN_NONE && g.C != nullptr) buf_store16<AUX_NT>(oz, at(i, h), pk8(z));
+          if constexpr (EPI == EPI_LIN_SWIGLU) {
+            float z2[8], b2[8];
+            up8(bias2, b2);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) z2[q] = acc2[i][2 * h + q / 4][q % 4] + b2[q];
+            if (g.C != nullptr) buf_store16<AUX_NT>(oz2, at(i, h), pk8(z2));
+#pragma unroll
+            for (int q = 0; q < 8; ++q) y[q] = fmaf(z[q] * sigmoid_fast(z[q]), z2[q], r[q]);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) y[q] = EPI == EPI_LIN_GELU ? fmaf(z[q], phi_fast(z[q]), r[q]) : z[q] + r[q];
+          }
+          buf_store16<AUX_NT>(oy, at(i, h), pk8(y));
+        }
+      }
     }
   } else {
     const size_t first = (size_t)row0 * g.N + n0, bytes = ((size_t)mvalid * g.N - n0) * 2;

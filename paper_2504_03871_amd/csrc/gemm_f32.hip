@@ -65,7 +65,7 @@ __device__ __forceinline__ void f32_chunk(int id, unsigned pitch, unsigned& off,
 
 template <int EPI>
 __device__ __forceinline__ void epilogue_f32x4(const GemmArgs& g, size_t idx, const f32x4& a, const f32x4& a2, const f32x4& s1,
-                                               const f32x4& s2, bool second_grad) {
+                                               const f32x4& s2, bool second_grad, const f32x4& b = f32x4{}, const f32x4& b2 = f32x4{}) {
   auto at = [&](void* base) { return reinterpret_cast<f32x4*>(reinterpret_cast<float*>(base) + idx); };
   f32x4 r, q;
   if constexpr (EPI == EPI_STORE) {
@@ -93,6 +93,19 @@ __device__ __forceinline__ void epilogue_f32x4(const GemmArgs& g, size_t idx, co
     }
     *at(g.C) = r;
     *at(g.C2) = q;
+  } else if constexpr (EPI >= EPI_LIN_NONE) {   // b, b2: bias; s1: residual
+    const f32x4 z = a + b;
+    if (EPI != EPI_LIN_NONE && g.C != nullptr) *at(g.C) = z;
+    if constexpr (EPI == EPI_LIN_SWIGLU) {
+      const f32x4 z2 = a2 + b2;
+      if (g.C != nullptr) *at(g.C2) = z2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = z[i] * sigmoid_f(z[i]) * z2[i] + s1[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = (EPI == EPI_LIN_GELU ? gelu_f(z[i]) : z[i]) + s1[i];
+    }
+    *at(g.C3) = r;
   } else {
     *at(second_grad ? g.C2 : g.C) = g.accumulate ? s1 + a : a;
   }
@@ -101,8 +114,8 @@ __device__ __forceinline__ void epilogue_f32x4(const GemmArgs& g, size_t idx, co
 template <bool DUAL, int BM>
 constexpr int f32_lds_bytes() { return (f32_tile_bytes(BM) + f32_tile_bytes(SB) * (DUAL ? 2 : 1)) * (DUAL ? 2 : 3); }
 
-// One output tile; vb = its number in dispatch order.
-template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
+// One output tile; vb = its number in dispatch order.  DENSE: one matrix instead of one per expert (GemmArgs).
+template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM, bool DENSE = false>
 __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, char* smem) {
   constexpr bool A_KC = MODE != MODE_TN, B_KC = MODE == MODE_NT;
   constexpr int BANDS = BM / 16, KH = 4 / BANDS;                        // KH waves share a band, each with every KH-th run of 16 K values
@@ -120,18 +133,29 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
     int slot, mt;
     if (!dw_block(vb, (g.M + BM - 1) / BM, ntn, slot, mt, nt)) return;
     if (g.C2 != nullptr) { second_grad = slot & 1; slot >>= 1; }   // the two gradients of an expert follow each other
-    e = g.order[slot];
+    e = DENSE ? slot : g.order[slot];
     m0 = mt * BM;
-    int l, h;
-    share_of(g.lo, g.hi, g.kept[e], e, l, h);
-    row0 = g.offsets[e] + l;
-    klen = h - l;
+    if constexpr (DENSE) {   // segment e of the rows
+      row0 = e * g.seg;
+      klen = min(g.seg, g.K - row0);
+    } else {
+      int l, h;
+      share_of(g.lo, g.hi, g.kept[e], e, l, h);
+      row0 = g.offsets[e] + l;
+      klen = h - l;
+    }
     mvalid = min(BM, g.M - m0);
     if (klen == 0 && g.accumulate) return;
   } else {
     RowBlock rb;
-    if (!row_tile_block(vb, g.ntiles[0], g.ntiles[1], 0, ntn, false, rb)) return;
-    const RowTile t = g.tiles[rb.rt];
+    RowTile t;
+    if constexpr (DENSE) {
+      if (!row_tile_block(vb, (g.M + BM - 1) / BM, g.M / BM, 0, ntn, false, rb)) return;
+      t = RowTile{0, rb.rt * BM, min(BM, g.M - rb.rt * BM), 0};
+    } else {
+      if (!row_tile_block(vb, g.ntiles[0], g.ntiles[1], 0, ntn, false, rb)) return;
+      t = g.tiles[rb.rt];
+    }
     e = t.e;
     row0 = t.row0;
     mvalid = t.nrows;
@@ -257,7 +281,11 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   if (!active || n0 + c * 4 >= g.N) return;
   // accumulator register v of a lane: row 4 grp + v of the wave's 16, one column of each of the four column tiles
   size_t idx[4];
-  f32x4 s1[4], s2[4];
+  f32x4 s1[4], s2[4], bias = {0.f, 0.f, 0.f, 0.f}, bias2 = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (EPI >= EPI_LIN_NONE) {
+    if (g.bias != nullptr) bias = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(g.bias) + n0 + c * 4);
+    if (DUAL && g.bias2 != nullptr) bias2 = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(g.bias2) + n0 + c * 4);
+  }
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const int m = band * 16 + grp * 4 + v, mc = min(m, mvalid - 1);
@@ -265,6 +293,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
     else idx[v] = (size_t)(row0 + mc) * g.N + n0 + c * 4;
     if constexpr (EPI == EPI_GELU_BWD || EPI == EPI_SWIGLU_BWD) s1[v] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(g.S1) + idx[v]);
     if constexpr (EPI == EPI_SWIGLU_BWD) s2[v] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(g.S2) + idx[v]);
+    if constexpr (EPI >= EPI_LIN_NONE) s1[v] = g.S1 != nullptr ? *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(g.S1) + idx[v]) : f32x4{0.f, 0.f, 0.f, 0.f};
     if constexpr (EPI == EPI_DW)
       if (g.accumulate) s1[v] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(second_grad ? g.C2 : g.C) + idx[v]);
   }
@@ -272,7 +301,8 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   for (int v = 0; v < 4; ++v)
     if (band * 16 + grp * 4 + v < mvalid)
       epilogue_f32x4<EPI>(g, idx[v], f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]},
-                          DUAL ? f32x4{acc2[0][v], acc2[DUAL ? 1 : 0][v], acc2[DUAL ? 2 : 0][v], acc2[DUAL ? 3 : 0][v]} : f32x4{}, s1[v], s2[v], second_grad);
+                          DUAL ? f32x4{acc2[0][v], acc2[DUAL ? 1 : 0][v], acc2[DUAL ? 2 : 0][v], acc2[DUAL ? 3 : 0][v]} : f32x4{}, s1[v], s2[v], second_grad,
+                          bias, bias2);
 }
 
 template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
@@ -317,6 +347,34 @@ int launch_gemm_f32(int mode, int epi, bool dual, bool chain, const GemmArgs& g,
   if (mode == MODE_NT && epi == EPI_STORE && !chain) return launch_one<MODE_NT, EPI_STORE, false, false>(g, tile_rows, max_tiles, s);
   if (mode == MODE_NT && epi == EPI_STORE && chain) return launch_one<MODE_NT, EPI_STORE, false, true>(g, tile_rows, max_tiles, s);
   if (mode == MODE_TN && epi == EPI_DW) return launch_one<MODE_TN, EPI_DW, false, false>(g, tile_rows, max_tiles, s);
+  return MOE_ERR_BAD_DTYPE;
+}
+
+// Dense products (linear.hip): g.M rows, or weight gradients over g.E segments of g.seg rows.
+template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
+__global__ __launch_bounds__(256, BM == SB ? 3 : 4) void linear_f32_kernel(GemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char smem[f32_lds_bytes<DUAL, BM>()];
+  gemm_f32_tile<MODE, EPI, DUAL, CHAIN, BM, true>(g, blockIdx.x, smem);
+}
+template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
+static int launch_linear_bm(const GemmArgs& g, hipStream_t s) {
+  const long long ntn = (g.N + SB - 1) / SB, blocks = MODE == MODE_TN ? dw_blocks(g, BM, SB) : ntn * ((g.M + BM - 1) / BM);
+  if (blocks > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
+  linear_f32_kernel<MODE, EPI, DUAL, CHAIN, BM><<<dim3((unsigned)blocks), 256, 0, s>>>(g);
+  return launch_status();
+}
+template <int MODE, int EPI, bool DUAL, bool CHAIN>
+static int launch_linear_rows(const GemmArgs& g, hipStream_t s) {
+  const int rows = MODE == MODE_TN ? dw_tile_rows(g) : f32_tile_rows(g.M, 0, g.N);
+  return rows == SB ? launch_linear_bm<MODE, EPI, DUAL, CHAIN, SB>(g, s) : launch_linear_bm<MODE, EPI, DUAL, CHAIN, SB / 2>(g, s);
+}
+int launch_linear_f32(int mode, int epi, bool chain, const GemmArgs& g, hipStream_t s) {
+  if (mode == MODE_NN && epi == EPI_LIN_NONE) return launch_linear_rows<MODE_NN, EPI_LIN_NONE, false, false>(g, s);
+  if (mode == MODE_NN && epi == EPI_LIN_GELU) return launch_linear_rows<MODE_NN, EPI_LIN_GELU, false, false>(g, s);
+  if (mode == MODE_NN && epi == EPI_LIN_SWIGLU) return launch_linear_rows<MODE_NN, EPI_LIN_SWIGLU, true, false>(g, s);
+  if (mode == MODE_NT && chain) return launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, true>(g, s);
+  if (mode == MODE_NT) return launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, false>(g, s);
+  if (mode == MODE_TN) return launch_linear_rows<MODE_TN, EPI_DW, false, false>(g, s);
   return MOE_ERR_BAD_DTYPE;
 }
 

@@ -916,6 +916,12 @@ int launch_gate_dwr(const moe_cfg* c, const void* x, const float* d_logits, floa
   return launch_dwr<float>(c, x, d_logits, dWr, accumulate, partials, s);
 }
 
+// WrT [E][d] = the transpose of Wr [d][E]
+int launch_wr_transpose(const moe_cfg* c, const float* Wr, float* WrT, hipStream_t s) {
+  wr_transpose_kernel<<<(c->d_model * c->E + 255) / 256, 256, 0, s>>>(Wr, WrT, c->d_model, c->E);
+  return launch_status();
+}
+
 int launch_route_bwd(const moe_cfg* c, const void* x, const float* Wr, const int32_t* idx, const float* w,
                      const float* dw, float* d_logits, float* dWr, void* dx, int accumulate, float* partials,
                      float* WrT, hipStream_t s) {

@@ -1,0 +1,609 @@
+"""Scored routing, activations in 8 bits and dense products with an epilogue on the GPU, against the 64-bit oracle."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import operators_oracle as O
+from paper_2504_03871_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+DEV = "cuda:0"
+TD = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+DT = {"f32": B.DTYPE_F32, "bf16": B.DTYPE_BF16, "f16": B.DTYPE_F16}
+FMT = {"e4m3": B.PACK_E4M3, "i8": B.PACK_I8}
+U = 2.0 ** -24           # rounding to fp32, half a step
+F32_MAX = float(np.finfo(np.float32).max)
+
+
+def half_step(dtype):
+    return torch.finfo(TD[dtype]).eps / 2
+
+
+def dev(a, dtype=torch.float32):
+    return torch.as_tensor(np.asarray(a)).to(dtype).to(DEV)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ---- scored routing ------------------------------------------------------------------------------------------------
+
+def route_inputs(T, E, seed, kind):
+    """Logits as they come, and at the places where a choice can go wrong."""
+    r = np.random.default_rng(seed)
+    l = r.normal(0, 1.5, (T, E))
+    if kind == "masked":
+        l[r.random((T, E)) < 0.4] = -np.inf
+        l[::3] = -np.inf                                    # rows with nothing left
+    elif kind == "odd":
+        l[r.random((T, E)) < 0.1] = np.nan
+        l[r.random((T, E)) < 0.1] = np.inf
+        l[r.random((T, E)) < 0.1] = -F32_MAX                # the type's lowest value takes part
+        l[1::4] = np.nan
+    elif kind == "ties":
+        l = r.integers(-2, 3, (T, E)).astype(np.float64)
+        l[::2] = 0.25
+    elif kind == "tiny":
+        l = l - 100.0                                       # sigmoids of 1e-44: only their ratios are left
+    elif kind == "wide":
+        l = l * 20.0
+    return l.astype(np.float32)
+
+
+SHAPES = [  # T, E, k, groups, top_groups, rank
+    (1, 1, 1, 1, 1, 1), (1, 256, 8, 8, 4, 2), (17, 8, 2, 1, 1, 1), (5, 12, 3, 4, 2, 2), (33, 16, 8, 16, 8, 1), (100, 33, 5, 1, 1, 1),
+    (64, 64, 6, 8, 3, 1), (31, 72, 8, 3, 1, 2), (48, 160, 8, 8, 3, 2), (16, 255, 4, 5, 2, 2), (70, 256, 8, 8, 4, 2), (15, 128, 1, 16, 1, 2),
+]
+
+
+def run_route(l, kind, k, balance, groups, top, rank, renorm, scale):
+    T, E = l.shape
+    cfg = B.make_cfg(T, 64, 64, E, k)
+    sc = B.make_score(B.SCORE_SOFTMAX if kind == "softmax" else B.SCORE_SIGMOID, groups, top, rank, renorm, scale)
+    lg = dev(l)
+    idx = torch.full((T, k), -7, dtype=torch.int32, device=DEV)
+    w = torch.full((T, k), 7.0, device=DEV)
+    B.moe_route_scored(cfg, sc, None, None, None, None if balance is None else dev(balance), lg, None, idx, w)
+    dw = dev(np.random.default_rng(9).normal(0, 1, (T, k)))
+    dl = torch.full((T, E), 7.0, device=DEV)
+    B.moe_route_scored_bwd(cfg, sc, None, None, lg, idx, dw, dl, None, None)
+    return idx.cpu().numpy(), f64(w), f64(dw), f64(dl)
+
+
+def check_route(l, kind, k, balance, groups, top, rank, renorm, scale):
+    idx, w, dw, dl = run_route(l, kind, k, balance, groups, top, rank, renorm, scale)
+    ridx, rw = O.route(l, kind, k, balance, groups, top, rank, renorm, scale)
+    assert np.array_equal(idx, ridx)
+    # A weight is a quotient of exponentials of l - top: each is good to 2^-24 of its argument (rounded once) and three units
+    # in the last place (half-steps: six), the sum of up to 256 of them to eight rounding errors of its pairwise order and one per
+    # term of a lane, the quotient and the scale to one each
+    lf = np.where(np.isfinite(l), l.astype(np.float64), 0.0)
+    reach = np.abs(np.where(np.abs(lf) < 1e30, lf, 0.0)).max(axis=1, keepdims=True) * 2
+    rel = (reach + 6 + 24 + 2) * U
+    tiny = 2.0 ** -120
+    assert np.all(np.abs(w - rw) <= rel * np.abs(rw) + tiny)
+    rdl = O.route_bwd(l, kind, ridx, dw, renorm, scale)
+    s, _ = O.scores(l, kind)
+    p = np.zeros_like(s)
+    for t in range(len(l)):
+        for j, e in enumerate(ridx[t]):
+            if e >= 0:
+                p[t, e] = abs(rw[t, j])
+    most = np.abs(dw).max(axis=1, keepdims=True)
+    size = 2 * most * (p + (abs(scale) * s if kind == "softmax" and not renorm else 0))
+    assert np.all(np.abs(dl - rdl) <= (2 * rel + 16 * U) * size + tiny), np.abs(dl - rdl).max()
+
+
+@pytest.mark.parametrize("inputs", ["plain", "masked", "odd", "ties", "tiny", "wide"])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_scored_routing(shape, kind, inputs):
+    T, E, k, groups, top, rank = shape
+    l = route_inputs(T, E, sum(shape), inputs)
+    r = np.random.default_rng(E)
+    bal = (np.round(r.normal(0, 30, E)) * 0.001).astype(np.float32)
+    for renorm, scale, balance in ((1, 1.0, None), (0, 2.5, bal), (1, 2.5, bal), (0, 1.0, None)):
+        check_route(l, kind, k, balance, groups, top, rank, renorm, scale)
+
+
+def test_keys_closer_than_single_precision_resolves():
+    """Scores plus bias that differ by less than an fp32 step, in both orders of the expert ids, and in the scores of groups."""
+    E = 32
+    base = 0.3
+    l = np.full((64, E), -4.0, np.float32)
+    bal = np.zeros(E, np.float32)
+    bal[:16] = np.float32(0.25)
+    for t in range(64):
+        a, b = t % 16, 16 + (t * 7) % 16
+        l[t, a] = base + t * 1e-3
+        # the logit whose sigmoid lies a quarter above: the nearest fp32 numbers around it give keys 1e-8 apart
+        v = 1 / (1 + math.exp(-float(l[t, a]))) + 0.25
+        x = np.float32(math.log(v / (1 - v)))
+        l[t, b] = np.nextafter(x, np.float32(9)) if t % 2 else np.nextafter(x, np.float32(-9))
+    for groups, rank in ((1, 1), (2, 1), (2, 2), (4, 2)):
+        check_route(l, "sigmoid", 1, bal, groups, 1, rank, 0, 1.0)
+        check_route(l, "sigmoid", 4, bal, groups, groups, rank, 1, 1.0)
+
+
+def test_balance_of_minus_infinity_closes_an_expert():
+    l = route_inputs(20, 24, 3, "plain")
+    bal = np.zeros(24, np.float32)
+    bal[::2] = -np.inf
+    check_route(l, "sigmoid", 8, bal, 3, 2, 2, 1, 1.0)
+    bal[:] = -np.inf
+    idx, w, _, dl = run_route(l, "softmax", 3, bal, 1, 1, 1, 1, 1.0)
+    assert (idx == -1).all() and (w == 0).all() and (dl == 0).all()
+
+
+def test_routing_gradient_against_differences():
+    """d sum(w dw) / d l by central differences of the oracle's weights at a fixed choice, in 64 bits."""
+    for kind, renorm, scale in (("softmax", 1, 2.0), ("softmax", 0, 1.0), ("sigmoid", 1, 1.5), ("sigmoid", 0, 1.0)):
+        l = route_inputs(6, 20, 5, "plain")
+        idx, _, dw, dl = run_route(l, kind, 4, None, 1, 1, 1, renorm, scale)
+        h = 1e-4
+        for t in range(6):
+            for e in range(20):
+                two = []
+                for sign in (1, -1):
+                    m = l.astype(np.float64)[t:t + 1].copy()
+                    m[0, e] += sign * h
+                    s, ll = O.scores(m, kind)
+                    two.append((O.weights(ll[0], s[0], idx[t], kind, renorm) * scale * dw[t]).sum())
+                # differences: h^2 / 6 of a third derivative that is at most about 4 scale sum |dw|; kernel: fp32
+                size = abs(scale) * np.abs(dw[t]).sum()
+                assert abs((two[0] - two[1]) / (2 * h) - dl[t, e]) <= size * (h * h + 40 * U)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,d,E,k", [(1, 64, 8, 2), (77, 192, 40, 4), (300, 1024, 256, 8)])
+def test_scored_routing_from_the_gate_product(dtype, T, d, E, k):
+    """The whole gate: product, choice, and the gradients of x and Wr for sparse and dense logit gradients."""
+    r = np.random.default_rng(T)
+    x, Wr = dev(r.normal(0, 1, (T, d)), TD[dtype]), dev(r.normal(0, d ** -0.5, (d, E)))
+    bias = dev(r.normal(0, 0.3, E))
+    cfg = B.make_cfg(T, d, 64, E, k, DT[dtype])
+    ws = torch.empty(B.moe_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    for kind, renorm in ((B.SCORE_SIGMOID, 1), (B.SCORE_SOFTMAX, 0)):
+        sc = B.make_score(kind, 1, 1, 1, renorm, 1.0)
+        logits, idx, w = torch.empty(T, E, device=DEV), torch.empty(T, k, dtype=torch.int32, device=DEV), torch.empty(T, k, device=DEV)
+        B.moe_route_scored(cfg, sc, x, Wr, bias, None, None, logits, idx, w, ws)
+        ref = f64(x) @ f64(Wr) + f64(bias)
+        size = np.abs(f64(x)) @ np.abs(f64(Wr)) + 1
+        term = 2.0 ** -17 if dtype != "f32" else 0.0          # the weight as two bf16 terms
+        assert np.all(np.abs(f64(logits) - ref) <= (8 * math.sqrt(d) * U + term) * size)
+        name = "sigmoid" if kind == B.SCORE_SIGMOID else "softmax"
+        ridx, rw = O.route(logits.cpu().numpy(), name, k, renorm=renorm)
+        assert np.array_equal(idx.cpu().numpy(), ridx)
+        assert np.allclose(f64(w), rw, rtol=60 * U, atol=0)
+        dw = dev(r.normal(0, 1, (T, k)))
+        dl, dWr, dx = torch.empty(T, E, device=DEV), dev(np.ones((d, E))), dev(r.normal(0, 1, (T, d)), TD[dtype])
+        before = f64(dx)
+        B.moe_route_scored_bwd(cfg, sc, x, Wr, logits, idx, dw, dl, dWr, dx, ws, accumulate=1)
+        g = f64(dl)
+        rdl = O.route_bwd(logits.cpu().numpy(), name, ridx, f64(dw), renorm)
+        assert np.abs(g - rdl).max() <= 100 * U * max(1.0, np.abs(rdl).max())
+        want, size = f64(x).T @ g + 1, np.abs(f64(x)).T @ np.abs(g) + 1
+        assert np.all(np.abs(f64(dWr) - want) <= (8 * math.sqrt(T) * U + term) * size)
+        want, size = before + g @ f64(Wr).T, np.abs(before) + np.abs(g) @ np.abs(f64(Wr)).T
+        # 2^-25: half the step of fp16's subnormal numbers
+        assert np.all(np.abs(f64(dx) - want) <= half_step(dtype) * np.abs(want) + 8 * math.sqrt(E) * U * size + 2.0 ** -25)
+
+
+def test_empty_slots_travel_through_the_layer():
+    """Tokens without an expert: dropped by dispatch, nothing in the output, no gradient."""
+    from paper_2504_03871_amd.layer import MoELayer
+    T, d, f, E, k = 40, 64, 128, 8, 4
+    L = MoELayer(T, d, f, E, k)
+    r = np.random.default_rng(0)
+    for t, std in ((L.x, 1), (L.Wr, 0.1), (L.W1, 0.05), (L.W2, 0.05), (L.d_out, 1)):
+        t.copy_(dev(r.normal(0, std, tuple(t.shape))))
+    lg = route_inputs(T, E, 1, "masked")
+    L.logits.copy_(dev(lg))
+    sc = B.make_score(B.SCORE_SIGMOID, 1, 1, 1, 1, 1.0)
+    B.moe_route_scored(L.cfg, sc, None, None, None, None, L.logits, None, L.topk_idx, L.topk_w)
+    L.dispatch(); L.ffn_fwd(); L.combine(); L.combine_bwd()
+    B.moe_route_scored_bwd(L.cfg, sc, None, None, L.logits, L.topk_idx, L.d_topk_w, L.d_logits, None, None)
+    idx = L.topk_idx.cpu().numpy()
+    assert (idx[::3] == -1).all() and (idx == -1).sum() > 40
+    assert int(L.counts.sum()) == (idx >= 0).sum()
+    assert (f64(L.out)[::3] == 0).all() and (f64(L.d_logits)[::3] == 0).all() and (f64(L.d_topk_w)[idx == -1] == 0).all()
+
+
+# ---- 8 bits ----------------------------------------------------------------------------------------------------------
+
+def pack_inputs(rows, width, dtype, seed):
+    r = np.random.default_rng(seed)
+    v = r.normal(0, 1, (rows, width)) * np.exp(r.normal(0, 3, (rows, 1)))
+    t = torch.as_tensor(v).to(TD[dtype])
+    if rows >= 8:
+        big = torch.finfo(TD[dtype]).max
+        small = torch.finfo(TD[dtype]).tiny * torch.finfo(TD[dtype]).eps
+        t[1] = 0
+        t[2, ::3] = big
+        t[3, 0] = -big
+        t[4] = small * torch.arange(width, dtype=torch.float64).to(TD[dtype])       # subnormal numbers
+        t[5, width // 2] = math.inf
+        t[6, width - 1] = math.nan
+        t[7] = torch.linspace(-2, 2, width)                                         # many ties of both grids
+    return t
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,width,pitch", [(1, 1, 1), (9, 4, 4), (8, 31, 40), (12, 33, 33), (10, 64, 64), (16, 516, 516), (20, 200, 264), (40, 1024, 1024)])
+def test_pack_and_unpack(rows, width, pitch, dtype, fmt):
+    v = pack_inputs(rows, width, dtype, rows + width)
+    src = torch.full((rows, pitch), 77.0, dtype=TD[dtype])
+    src[:, :width] = v
+    src = src.to(DEV)
+    n = B.moe_pack8_bytes(rows, width)
+    codes, scales = (torch.full((m + 64,), 0xAB, dtype=torch.uint8, device=DEV) for m in n)
+    B.moe_pack8(DT[dtype], FMT[fmt], rows, width, pitch, src, codes, scales)
+    rc, rs, rv = O.pack(v.double().numpy(), fmt)
+    assert np.array_equal(scales[:n[1]].cpu().numpy().reshape(rs.shape), rs)
+    got = codes[:n[0]].cpu().numpy().reshape(rc.shape)
+    known = np.repeat(rs != 255, 32, axis=1)
+    assert np.array_equal(got[known], rc[known])
+    assert (codes[n[0]:] == 0xAB).all() and (scales[n[1]:] == 0xAB).all()
+    out = torch.full((rows, pitch), 77.0, dtype=TD[dtype], device=DEV)
+    B.moe_unpack8(DT[dtype], FMT[fmt], rows, width, pitch, codes, scales, out)
+    most = torch.finfo(TD[dtype]).max
+    want = torch.as_tensor(np.clip(rv, -most, most)).to(TD[dtype])
+    back = out.cpu()
+    assert torch.equal(back[:, :width].isnan(), want.isnan())
+    assert torch.equal(torch.nan_to_num(back[:, :width].float()), torch.nan_to_num(want.float()))
+    assert (back[:, width:] == 77.0).all()
+
+
+def test_pack_of_every_bf16_number():
+    """Each bf16 number in a block of its own with a second value that fixes the scale, and alone."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    v = torch.zeros(65536, 32, dtype=torch.bfloat16)
+    v[:, 0] = bits
+    v[:, 5] = bits * 0.37
+    v[:, 9] = -bits * 0.011
+    for fmt in FMT:
+        codes, scales = (torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(65536, 32))
+        B.moe_pack8(B.DTYPE_BF16, FMT[fmt], 65536, 32, 32, v.to(DEV), codes, scales)
+        rc, rs, _ = O.pack(v.double().numpy(), fmt)
+        assert np.array_equal(scales.cpu().numpy().reshape(rs.shape), rs)
+        ok = np.repeat(rs != 255, 32, axis=1)
+        assert np.array_equal(codes.cpu().numpy().reshape(rc.shape)[ok], rc[ok])
+
+
+def test_pack_beyond_32_bit_offsets():
+    rows, width = 66000, 65536
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("memory")
+    src = torch.zeros(rows, width, dtype=torch.bfloat16, device=DEV)
+    tail = pack_inputs(8, width, "bf16", 5)
+    src[-8:] = tail.to(DEV)
+    codes, scales = (torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(rows, width))
+    B.moe_pack8(B.DTYPE_BF16, B.PACK_I8, rows, width, width, src, codes, scales)
+    src.fill_(5.0)
+    B.moe_unpack8(B.DTYPE_BF16, B.PACK_I8, rows, width, width, codes, scales, src)
+    _, _, rv = O.pack(tail.double().numpy(), "i8")
+    most = torch.finfo(torch.bfloat16).max
+    want = torch.as_tensor(np.clip(rv, -most, most)).to(torch.bfloat16)
+    assert torch.equal(torch.nan_to_num(src[-8:].cpu().float()), torch.nan_to_num(want.float()))
+    assert int((src[:-8] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("sliced", [False, True])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("dtype,f", [("f32", 100), ("bf16", 192), ("f16", 64)])
+def test_saved_planes(dtype, f, act, sliced):
+    T, E, k = 37, 6, 2
+    A, mats = T * k, 2 if act == "swiglu" else 1
+    cfg = B.make_cfg(T, 64, f, E, k, DT[dtype], B.ACT_SWIGLU if act == "swiglu" else B.ACT_GELU)
+    kept = np.array([20, 0, 7, 30, 0, 11])                    # 68 of 74 rows in use
+    offsets = np.concatenate([[0], np.cumsum(kept)])
+    lo, hi = ([3, 0, 5, 0, 0, 9], [15, 4, 2, 99, 1, 11]) if sliced else (None, None)
+    live = np.zeros(A, bool)
+    for e in range(E):
+        a, b = (min(max(lo[e], 0), kept[e]), min(max(hi[e], 0), kept[e])) if sliced else (0, kept[e])
+        live[offsets[e] + a:offsets[e] + max(a, b)] = True
+    r = np.random.default_rng(f)
+    pre = dev(r.normal(0, 2, (mats, A, f)), TD[dtype])
+    pre[:, torch.as_tensor(~live).to(DEV)] = math.nan         # rows that may not be read
+    i32 = lambda a: None if a is None else dev(a, torch.int32)  # noqa: E731
+    for fmt in FMT:
+        codes, scales = (torch.full((m,), 0xAB, dtype=torch.uint8, device=DEV) for m in B.moe_saved_pack8_bytes(cfg))
+        args = (i32(offsets), i32(kept), i32(lo), i32(hi))
+        B.moe_saved_pack8(cfg, FMT[fmt], pre, *args, codes, scales)
+        out = torch.full((mats + 1, A, f), 77.0, dtype=TD[dtype], device=DEV)
+        B.moe_saved_restore8(cfg, FMT[fmt], codes, scales, *args, out)
+        dead = torch.as_tensor(~live).to(DEV)
+        nb = -(-f // 32)
+        assert (codes.view(mats, A, nb * 32)[:, dead] == 0xAB).all() and (scales.view(mats, A, nb)[:, dead] == 0xAB).all()
+        assert (out[:, dead] == 77.0).all()
+        z = [O.pack(f64(pre[m])[live], fmt)[2] for m in range(mats)]
+        for m in range(mats):
+            assert np.array_equal(f64(out[m])[live], z[m])
+        h = O.act(z, act)
+        slack = 4e-7 * np.abs(z[0]) * (np.abs(z[1]) if mats == 2 else 1)   # Phi to 3e-7; sigmoid to a few units in the last place
+        assert np.all(np.abs(f64(out[-1])[live] - h) <= half_step(dtype) * np.abs(h) + slack + 2.0 ** -25)
+
+
+# ---- dense products --------------------------------------------------------------------------------------------------
+
+def linear_case(T, d, n, dtype, act, bias=True, residual=True, seed=0):
+    r = np.random.default_rng(seed + T + d + n)
+    mats = 2 if act == "swiglu" else 1
+    new = lambda *s, std=1.0: dev(r.normal(0, std, s), TD[dtype])  # noqa: E731
+    return dict(T=T, d=d, n=n, dtype=dtype, act=act, mats=mats, x=new(T, d), W=[new(d, n, std=d ** -0.5) for _ in range(mats)],
+                b=[new(n, std=0.3) for _ in range(mats)] if bias else [None, None][:mats], r=new(T, n) if residual else None, dy=new(T, n),
+                pre=[new(T, n, std=1.2) for _ in range(mats)], add=new(T, d))
+
+
+def two(v):
+    return (list(v) + [None, None])[:2]
+
+
+ACTS = {"none": B.ACT_NONE, "gelu": B.ACT_GELU, "swiglu": B.ACT_SWIGLU}
+
+
+def run_fwd(c, keep=True, y=None, stream=None):
+    lin = B.make_linear(c["T"], c["d"], c["n"], DT[c["dtype"]], ACTS[c["act"]])
+    ws = torch.empty(max(16, B.moe_linear_workspace_bytes(lin)), dtype=torch.uint8, device=DEV)
+    y = torch.full((c["T"], c["n"]), 77.0, dtype=TD[c["dtype"]], device=DEV) if y is None else y
+    pre = [torch.full_like(y, 77.0) for _ in range(c["mats"])] if keep and c["act"] != "none" else []
+    B.moe_linear_fwd(lin, c["x"], *two(c["W"]), *two(c["b"]), c["r"], *two(pre), y, ws, stream=stream)
+    return y, pre
+
+
+def check_fwd(c):
+    y, pre = run_fwd(c)
+    x, W = f64(c["x"]), [f64(w) for w in c["W"]]
+    z = [x @ w + (0 if b is None else f64(b)) for w, b in zip(W, c["b"])]
+    # fp32 sums of K exact products in an order of the kernel's choosing: a random walk of at most K roundings of the running
+    # sum, 6 sigma; the running sum is at most the sum of magnitudes
+    err = [6 * math.sqrt(c["d"]) * U * (np.abs(x) @ np.abs(w) + 1) for w in W]
+    hs = half_step(c["dtype"])
+    for p, zz, e in zip(pre, z, err):
+        assert np.all(np.abs(f64(p) - zz) <= hs * np.abs(zz) + e + 2.0 ** -25)
+    want = O.act(z, c["act"])
+    slopes = O.act_slopes(z, c["act"])
+    slack = sum((np.abs(s) + e) * e for s, e in zip(slopes, err)) + 8e-7 * np.abs(z[0]) * (np.abs(z[-1]) if c["mats"] == 2 else 1)
+    want = want + (0 if c["r"] is None else f64(c["r"]))
+    assert np.all(np.abs(f64(y) - want) <= hs * np.abs(want) + slack + 2.0 ** -25), np.abs(f64(y) - want).max()
+    return y
+
+
+def run_bwd(c, grad="f32", fmt=None, accumulate=0, add=True, skip=(), fill=77.0):
+    lin = B.make_linear(c["T"], c["d"], c["n"], DT[c["dtype"]], ACTS[c["act"]], pre=FMT[fmt] if fmt else B.PACK_NONE, grad=DT[grad])
+    ws = torch.empty(max(16, B.moe_linear_workspace_bytes(lin)), dtype=torch.uint8, device=DEV)
+    new = lambda *s, t=TD[grad]: torch.full(s, fill, dtype=t, device=DEV)  # noqa: E731
+    dx = None if "dx" in skip else new(c["T"], c["d"], t=TD[c["dtype"]])
+    dW = [] if "dW" in skip else [new(c["d"], c["n"]) for _ in range(c["mats"])]
+    db = [] if "db" in skip else [new(c["n"]) for _ in range(c["mats"])]
+    pre, sc = (c["pre"], []) if c["act"] != "none" else ([], [])
+    if fmt:
+        packed = []
+        for p in pre:
+            q = [torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(c["T"], c["n"])]
+            B.moe_pack8(DT[c["dtype"]], FMT[fmt], c["T"], c["n"], c["n"], p, *q)
+            packed.append(q)
+        pre, sc = [q[0] for q in packed], [q[1] for q in packed]
+    B.moe_linear_bwd(lin, c["dy"], c["x"], *two(c["W"]), *two(pre), *two(sc), c["add"] if add else None, dx, *two(dW), *two(db), accumulate, ws)
+    return dx, dW, db
+
+
+def check_bwd(c, grad="f32", fmt=None, accumulate=0, add=True):
+    dx, dW, db = run_bwd(c, grad, fmt, accumulate, add, fill=0.5 if accumulate else 77.0)
+    old = 0.5 if accumulate else 0.0
+    pre = [f64(p) for p in c["pre"]]
+    if fmt:
+        pre = [O.pack(p, fmt)[2] for p in pre]
+    dy, x = f64(c["dy"]), f64(c["x"])
+    dz = [dy * s for s in O.act_slopes(pre, c["act"])] if c["act"] != "none" else [dy]
+    hs, hg = half_step(c["dtype"]), half_step(grad)
+    # dz: the slope to 1e-6 (rational approximation, fast reciprocal), then one rounding to the storage type; the products' sums
+    # carry the independent roundings of dz (6 sigma) and of fp32 accumulation as in the forward
+    fuzz = 1e-6 if c["act"] != "none" else 0.0
+    round_dz = hs if c["act"] != "none" else 0.0
+    mag = np.abs(dy) * (1 + sum(np.abs(p) for p in pre)) if c["act"] != "none" else np.abs(dy)
+    want = sum(g @ f64(w).T for g, w in zip(dz, c["W"])) + (f64(c["add"]) if add else 0)
+    walk = sum(np.sqrt((g ** 2) @ (f64(w).T ** 2)) for g, w in zip(dz, c["W"]))
+    sums = sum(np.abs(g) @ np.abs(f64(w)).T + fuzz / U * 0 for g, w in zip(dz, c["W"]))
+    slope = sum(mag @ np.abs(f64(w)).T for w in c["W"]) * fuzz
+    tol = hs * np.abs(want) + 6 * round_dz * walk + 6 * math.sqrt(2 * c["n"]) * U * (sums + 1) + slope + 2.0 ** -25
+    assert np.all(np.abs(f64(dx) - want) <= tol), ("dx", np.abs(f64(dx) - want).max())
+    for m, g in enumerate(dz):
+        want = x.T @ g + old
+        tol = hg * np.abs(want) + 6 * round_dz * np.sqrt((x.T ** 2) @ (g ** 2)) + 6 * math.sqrt(c["T"] + 16) * U * (np.abs(x).T @ np.abs(g) + 1) + \
+            np.abs(x).T @ mag * fuzz
+        assert np.all(np.abs(f64(dW[m]) - want) <= tol), ("dW", np.abs(f64(dW[m]) - want).max())
+        want = g.sum(axis=0) + old
+        tol = hg * np.abs(want) + 6 * math.sqrt(c["T"] + 16) * U * (np.abs(g).sum(axis=0) + 1) + fuzz * mag.sum(axis=0)
+        assert np.all(np.abs(f64(db[m]) - want) <= tol), ("db", np.abs(f64(db[m]) - want).max())
+
+
+SIZES = [("bf16", 1, 64, 64), ("bf16", 1, 1024, 192), ("f16", 7, 2048, 320), ("bf16", 33, 512, 1088), ("f16", 64, 256, 64), ("bf16", 65, 192, 448),
+         ("bf16", 161, 1024, 512), ("f16", 300, 2880, 320), ("bf16", 513, 256, 2048), ("bf16", 700, 2048, 256), ("f16", 1025, 64, 832),
+         ("f32", 1, 4, 4), ("f32", 3, 100, 36), ("f32", 70, 516, 132), ("f32", 257, 68, 1540), ("f32", 1000, 256, 512)]
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("dtype,T,d,n", SIZES)
+def test_linear_forward(dtype, T, d, n, act):
+    check_fwd(linear_case(T, d, n, dtype, act))
+    check_fwd(linear_case(T, d, n, dtype, act, bias=False, residual=False))
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("dtype,T,d,n", SIZES)
+def test_linear_backward(dtype, T, d, n, act):
+    c = linear_case(T, d, n, dtype, act)
+    check_bwd(c)
+    check_bwd(c, grad=dtype, add=False)
+    check_bwd(c, accumulate=1)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("dtype,T,d,n", [("bf16", 5, 64, 64), ("f16", 300, 128, 448), ("f32", 70, 64, 100)])
+def test_linear_backward_from_packed_pre_activations(dtype, T, d, n, act, fmt):
+    check_bwd(linear_case(T, d, n, dtype, act), fmt=fmt)
+
+
+def test_linear_long_token_axis():
+    """Weight gradients over many tokens, in segments: few tiles, a token count that no segment divides."""
+    for dtype, T, d, n in (("bf16", 9001, 64, 128), ("f32", 4099, 64, 68)):
+        c = linear_case(T, d, n, dtype, "gelu")
+        check_bwd(c)
+        check_bwd(c, accumulate=1)
+
+
+def test_linear_outputs_may_be_skipped():
+    c = linear_case(130, 128, 192, "bf16", "swiglu")
+    full = run_bwd(c)
+    for skip in (("dx",), ("dW",), ("db",), ("dx", "db"), ("dW", "db"), ("dx", "dW")):
+        part = run_bwd(c, skip=skip)
+        for name, a, b in zip(("dx", "dW", "db"), part, full):
+            if name in skip:
+                continue
+            for u, v in zip(a if isinstance(a, list) else [a], b if isinstance(b, list) else [b]):
+                assert torch.equal(u, v), (skip, name)
+
+
+def test_linear_residual_in_place():
+    """The residual may be the output itself, and dx_add dx itself."""
+    for dtype, T, d, n in (("bf16", 20, 1024, 256), ("bf16", 300, 2048, 256), ("bf16", 600, 64, 256), ("f32", 70, 64, 100)):
+        c = linear_case(T, d, n, dtype, "none")
+        apart, _ = run_fwd(c)
+        y = c["r"].clone()
+        run_fwd({**c, "r": y}, y=y)
+        assert torch.equal(apart, y)
+
+
+def test_linear_non_finite_values_stay_in_their_rows():
+    c = linear_case(200, 128, 128, "bf16", "gelu")
+    clean, _ = run_fwd(c)
+    c["x"][17] = math.nan
+    c["x"][150, 3] = math.inf
+    y, _ = run_fwd(c)
+    rest = [i for i in range(200) if i not in (17, 150)]
+    assert torch.equal(y[rest], clean[rest])
+    assert y[17].isnan().all() and not torch.isfinite(y[150]).all()
+
+
+def test_linear_without_tokens():
+    for accumulate, want in ((0, 0.0), (1, 7.0)):
+        c = dict(T=0, d=64, n=128, dtype="bf16", act="gelu", mats=1, x=torch.empty(0, 64, dtype=torch.bfloat16, device=DEV))
+        c.update(W=[dev(np.ones((64, 128)), torch.bfloat16)], b=[None], r=None, dy=torch.empty(0, 128, dtype=torch.bfloat16, device=DEV),
+                 pre=[torch.empty(0, 128, dtype=torch.bfloat16, device=DEV)], add=None)
+        run_fwd(c)
+        _, dW, db = run_bwd(c, accumulate=accumulate, fill=7.0)
+        assert (dW[0] == want).all() and (db[0] == want).all()
+
+
+def test_linear_gradient_against_differences():
+    """Directional derivatives of sum(dy y) by central differences of the fp32 forward."""
+    for act in ("gelu", "swiglu"):
+        c = linear_case(40, 32, 48, "f32", act, residual=False)
+        y, pre = run_fwd(c)
+        dx, dW, db = run_bwd({**c, "pre": pre}, add=False)
+        r = np.random.default_rng(2)
+        h = 2.0 ** -6
+
+        def loss(**change):
+            yy, _ = run_fwd({**c, **change})
+            return float((f64(yy) * f64(c["dy"])).sum())
+        # truncation: h^2 / 6 of a third derivative of order one per unit direction; rounding: |y| 2^-24 sqrt(outputs) / h
+        for name, grads in (("x", [dx]), ("W", dW), ("b", db)):
+            for i, g in enumerate(grads):
+                v = torch.as_tensor(r.normal(0, 1, tuple(g.shape))).to(torch.float32).to(DEV)
+                v = v / v.norm()
+                moved = []
+                for s in (h, -h):
+                    t = (c["x"] if name == "x" else c[name][i]) + s * v
+                    moved.append(loss(**({"x": t} if name == "x" else {name: [t if j == i else o for j, o in enumerate(c[name])]})))
+                want = (moved[0] - moved[1]) / (2 * h)
+                noise = 16 * U * float(np.linalg.norm(f64(y) * f64(c["dy"]))) * math.sqrt(32) / h
+                assert abs(want - float((f64(g) * f64(v)).sum())) <= h * h * float(np.linalg.norm(f64(c["dy"]))) + noise, (act, name)
+
+
+def test_linear_beyond_32_bit_offsets():
+    T, d, n = (1 << 19) + 3, 64, 8256        # 4.3e9 outputs
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("memory")
+    x = torch.zeros(T, d, dtype=torch.bfloat16, device=DEV)
+    r = np.random.default_rng(0)
+    tail = dev(r.normal(0, 1, (5, d)), torch.bfloat16)
+    x[-5:] = tail
+    W = dev(r.normal(0, 0.1, (d, n)), torch.bfloat16)
+    lin = B.make_linear(T, d, n)
+    ws = torch.empty(max(16, B.moe_linear_workspace_bytes(lin)), dtype=torch.uint8, device=DEV)
+    y = torch.full((T, n), 7.0, dtype=torch.bfloat16, device=DEV)
+    B.moe_linear_fwd(lin, x, W, None, None, None, None, None, None, y, ws)
+    want = f64(tail) @ f64(W)
+    assert np.all(np.abs(f64(y[-5:]) - want) <= 2.0 ** -8 * np.abs(want) + 1e-5)
+    assert int((y[:-5] != 0).sum()) == 0
+    dW = torch.empty(d, n, device=DEV)
+    y[:-5] = 1.0
+    B.moe_linear_bwd(lin, y, x, W, None, None, None, None, None, None, None, dW, None, None, None, 0, ws)
+    want = f64(tail).T @ f64(y[-5:])
+    assert np.abs(f64(dW) - want).max() <= 1e-5 * np.abs(want).max()
+
+
+def test_operators_on_a_stream_and_in_a_graph():
+    """On a side stream, and captured: every replay gives the eager bits, with eager calls between the replays."""
+    c = linear_case(300, 2048, 256, "bf16", "gelu")
+    lin = B.make_linear(300, 2048, 256, B.DTYPE_BF16, B.ACT_GELU)
+    ws = torch.empty(B.moe_linear_workspace_bytes(lin), dtype=torch.uint8, device=DEV)
+    y, z, dx = torch.empty_like(c["dy"]), torch.empty_like(c["dy"]), torch.empty_like(c["x"])
+    dW, db = torch.empty(2048, 256, device=DEV), torch.empty(256, device=DEV)
+    lg = dev(route_inputs(300, 256, 1, "plain"))
+    cfg, sc = B.make_cfg(300, 64, 64, 256, 8), B.make_score(B.SCORE_SIGMOID, 8, 4, 2, 1, 2.5)
+    idx, w, dl = torch.empty(300, 8, dtype=torch.int32, device=DEV), torch.empty(300, 8, device=DEV), torch.empty(300, 256, device=DEV)
+    bal = dev(np.linspace(-0.05, 0.05, 256))
+    codes, scales = (torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(300, 256))
+
+    def step():
+        B.moe_route_scored(cfg, sc, None, None, None, bal, lg, None, idx, w)
+        B.moe_route_scored_bwd(cfg, sc, None, None, lg, idx, w, dl, None, None)
+        B.moe_linear_fwd(lin, c["x"], c["W"][0], None, c["b"][0], None, c["r"], z, None, y, ws)
+        B.moe_pack8(B.DTYPE_BF16, B.PACK_E4M3, 300, 256, 256, z, codes, scales)
+        B.moe_unpack8(B.DTYPE_BF16, B.PACK_E4M3, 300, 256, 256, codes, scales, z)
+        B.moe_linear_bwd(lin, c["dy"], c["x"], c["W"][0], None, z, None, None, None, None, dx, dW, None, db, None, 0, ws)
+
+    outs = (idx, w, dl, y, z, dx, dW, db, codes, scales)
+    step()
+    torch.cuda.synchronize()
+    eager = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for o in outs:
+            o.zero_()
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+def test_tensors_must_be_contiguous():
+    c = linear_case(64, 64, 128, "bf16", "none")
+    with pytest.raises(ValueError):
+        run_fwd({**c, "x": torch.empty(64, 64, dtype=torch.bfloat16, device=DEV).t()})
+    big = torch.zeros(8, 64, dtype=torch.bfloat16, device=DEV)
+    codes, scales = (torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(8, 40))
+    B.moe_pack8(B.DTYPE_BF16, B.PACK_I8, 8, 40, 64, big[:, :40], codes, scales)          # a view of rows that are 64 apart
+    with pytest.raises(ValueError):
+        B.moe_pack8(B.DTYPE_BF16, B.PACK_I8, 8, 40, 40, big[:, :40], codes, scales)      # the pitch says something else
