@@ -10,6 +10,7 @@
 // Sixteen lanes own a token (four tokens per wave): lane i holds the V = 2^n experts from i V on, so that the lowest lane and
 // the lowest slot of equal keys is the lowest expert, and a maximum over the token is four steps within a row of 16 lanes.
 #include "common.h"
+#include <type_traits>
 
 namespace moe {
 
@@ -22,12 +23,13 @@ struct ScoreArgs {
   float* topk_w;
   int T, E, k;
   int softmax, groups, top_groups, rank, renorm;
+  int group_lanes;         // lanes that hold a group, where that is a power of two and no lane holds two groups; else 0
   float scale;
 };
 
 // ---- reductions over the 16 lanes of a token; every lane gets the result ----
 template <int N> __device__ __forceinline__ float row_ror(float v) {
-  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, false));
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, row_ror<1>(v));
@@ -40,16 +42,6 @@ __device__ __forceinline__ float row_sum(float v) {
   v += row_ror<2>(v);
   v += row_ror<4>(v);
   return v + row_ror<8>(v);
-}
-__device__ __forceinline__ double row_max(double v) {
-#pragma unroll
-  for (int s = 1; s < SC_LANES; s <<= 1) v = fmax(v, __shfl_xor(v, s, SC_LANES));
-  return v;
-}
-__device__ __forceinline__ double row_sum(double v) {
-#pragma unroll
-  for (int s = 1; s < SC_LANES; s <<= 1) v += __shfl_xor(v, s, SC_LANES);
-  return v;
 }
 // the token's 16 bits of a wave-wide vote
 __device__ __forceinline__ unsigned row_vote(bool b) {
@@ -65,115 +57,336 @@ __device__ __forceinline__ void wave_lds_sync() {
 // A logit that takes part: minus infinity and NaN do not, plus infinity counts as the largest number.
 __device__ __forceinline__ float usable(float l) { return l > -INFINITY ? fminf(l, 3.4028234663852886e38f) : -INFINITY; }
 
-__device__ __forceinline__ float score_exp(float v) { return __expf(v); }
-__device__ __forceinline__ double score_exp(double v) { return exp(v); }
-__device__ __forceinline__ float score_sigmoid(float l) { return __builtin_amdgcn_rcpf(1.f + __expf(-l)); }
-__device__ __forceinline__ double score_sigmoid(double l) { return 1.0 / (1.0 + exp(-l)); }
-
-// The token's choice in arithmetic F: chosen experts and their logits to pick_e, pick_l [k] in LDS (-1: none left).  BY_LOGIT:
-// the scores grow with the logits and nothing is added to them, so the logits themselves are the keys.
-// Returns whether two keys (or the scores of two groups) that decide lie closer together than F resolves.
-template <typename F, int V, bool BY_LOGIT>
-__device__ __forceinline__ bool choose(const ScoreArgs& a, const float (&l)[V], float row_top, int lane, F* keys_lds, int* pick_e, float* pick_l) {
-  F key[V], top_s = 0, top_b = 0;
+// lane i's V values of a row of E, `rest` past its end
+template <int V>
+__device__ __forceinline__ void load_row(const float* __restrict__ row, int E, int lane, float rest, float (&l)[V]) {
   const int e0 = lane * V;
+  if (V >= 4 && (E & 3) == 0) {
+    float4 q[V < 4 ? 1 : V / 4];
+#pragma unroll
+    for (int v = 0; v < V; v += 4) q[v / 4] = *reinterpret_cast<const float4*>(row + min(e0 + v, E - 4));
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float4 p = q[v / 4];
+      l[v] = e0 + v < E ? (v % 4 == 0 ? p.x : v % 4 == 1 ? p.y : v % 4 == 2 ? p.z : p.w) : rest;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) l[v] = row[min(e0 + v, E - 1)];
+#pragma unroll
+    for (int v = 0; v < V; ++v) l[v] = e0 + v < E ? l[v] : rest;
+  }
+}
+
+// ---- the choice, in single precision ----
+// Keys c (-inf: cannot be chosen) and what they are made of: the largest score plus the largest finite bias.  BY_LOGIT: the scores
+// grow with the logits and nothing is added to them, so the logits themselves are the keys.
+template <int V, bool BY_LOGIT>
+__device__ __forceinline__ float make_keys(const ScoreArgs& a, const float (&l)[V], float row_top, int lane, float (&key)[V]) {
+  float top_s = 0.f, top_b = 0.f;
   if constexpr (BY_LOGIT) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = (F)l[v];
+    for (int v = 0; v < V; ++v) {
+      key[v] = l[v];
+      top_s = fmaxf(top_s, l[v] > -INFINITY ? fabsf(l[v]) : 0.f);
+    }
+    return row_max(top_s);
   } else {
-    F inv = 1;
+    float b[V];
+    if (a.balance != nullptr) load_row<V>(a.balance, a.E, lane, 0.f, b);
     if (a.softmax) {
-      F z = 0;
+      float z = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        key[v] = l[v] > -INFINITY ? score_exp((F)l[v] - (F)row_top) : (F)0;
+        key[v] = l[v] > -INFINITY ? __expf(l[v] - row_top) : 0.f;
         z += key[v];
       }
       z = row_sum(z);
-      inv = z > 0 ? 1 / z : (F)0;
+      const float inv = z > 0.f ? __builtin_amdgcn_rcpf(z) : 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] *= inv;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = __builtin_amdgcn_rcpf(1.f + __expf(-l[v]));   // 0 for minus infinity
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const F s = a.softmax ? key[v] * inv : l[v] > -INFINITY ? score_sigmoid((F)l[v]) : (F)0;
-      const F b = a.balance != nullptr && e0 + v < a.E ? (F)a.balance[e0 + v] : (F)0;
-      const F c = s + b;
-      top_s = s > top_s ? s : top_s;
-      const F mag = b < 0 ? -b : b;
-      if (mag < (F)INFINITY && mag > top_b) top_b = mag;
-      key[v] = (l[v] > -INFINITY && c > (F)-INFINITY) ? c : (F)-INFINITY;
+    for (int v = 0; v < V; ++v) top_s = fmaxf(top_s, key[v]);
+    if (a.balance != nullptr) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float mag = fabsf(b[v]);
+        top_b = fmaxf(top_b, mag < INFINITY ? mag : 0.f);
+        key[v] += b[v] > -INFINITY ? b[v] : -INFINITY;   // (not a NaN)
+      }
     }
-    top_s = row_max(top_s);
-    top_b = row_max(top_b);
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? key[v] : -INFINITY;
+    return row_max(top_s) + row_max(top_b);
   }
-  // What two keys must differ by for their order to be certain.  Single precision: the exponential's argument is good to
-  // 2^-24 of itself, which x e^-x <= 0.37 turns into less than 2^-24 of the largest score, exponential, reciprocal and sum add a
-  // few units in the last place, the bias one: 2^-21 of the largest magnitudes together, for either key, with room.
-  const F unit = sizeof(F) == 4 ? (F)1.9073486328125e-6 * (top_s + top_b) : (F)0;   // 2^-19
-  bool close = false;
+}
 
-  if (a.groups > 1) {
-    const int size = a.E / a.groups;
+// the best two of (b >= n) and (ob >= on)
+template <typename F>
+__device__ __forceinline__ void merge_two(F& b, F& n, F ob, F on) {
+  const F lo = b < ob ? b : ob, hi = b < ob ? ob : b, m = n < on ? on : n;
+  n = lo < m ? m : lo;
+  b = hi;
+}
+template <int CTRL> __device__ __forceinline__ float dpp_of(float v) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// merges over runs of 2^steps adjacent lanes; each step pairs runs whose lanes already agree, so that mirrors serve as well
+__device__ __forceinline__ void merge_lanes(float& b, float& n, int lanes) {
+  if (lanes > 1) merge_two(b, n, dpp_of<0xB1>(b), dpp_of<0xB1>(n));      // lane ^ 1
+  if (lanes > 2) merge_two(b, n, dpp_of<0x4E>(b), dpp_of<0x4E>(n));      // lane ^ 2
+  if (lanes > 4) merge_two(b, n, dpp_of<0x141>(b), dpp_of<0x141>(n));    // halves of eight mirrored
+  if (lanes > 8) merge_two(b, n, dpp_of<0x140>(b), dpp_of<0x140>(n));    // the row mirrored
+}
+
+// the larger of two numbers that are none of them NaN, in one instruction (fmaxf first makes sure of that)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
+// how many of the 15 other lanes hold a larger value
+template <int R> __device__ __forceinline__ int lanes_above(float g) {
+  if constexpr (R < SC_LANES) return (row_ror<R>(g) > g ? 1 : 0) + lanes_above<R + 1>(g);
+  else return 0;
+}
+
+// Groups: closes the keys outside the top_groups best.  Returns whether it is not certain which these are: the scores of the last
+// group that is in and the first that is out lie within `unit` of each other.
+// Where a group is a run of 2^n whole lanes (a.group_lanes), its lanes find its best two together; else lane g reads group g's keys
+// from LDS.
+template <int V>
+__device__ __forceinline__ bool restrict_groups(const ScoreArgs& a, float (&key)[V], int lane, float* keys_lds, float unit) {
+  const int size = a.E / a.groups, e0 = lane * V;
+  const int lanes = a.group_lanes > 0 ? a.group_lanes : 1;
+  float g = -INFINITY, best = -INFINITY, next = -INFINITY;
+  if (a.group_lanes > 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      next = __builtin_amdgcn_fmed3f(best, next, key[v]);   // best >= next: the middle one is the new second
+      best = larger(best, key[v]);
+    }
+    merge_lanes(best, next, a.group_lanes);
+  } else {
 #pragma unroll
     for (int v = 0; v < V; ++v)
       if (e0 + v < a.E) keys_lds[e0 + v] = key[v];
     wave_lds_sync();
-    F best = (F)-INFINITY, next = (F)-INFINITY;
     if (lane < a.groups)
       for (int i = 0; i < size; ++i) {
-        const F c = keys_lds[lane * size + i];
-        if (c > best) { next = best; best = c; } else if (c > next) next = c;
+        const float c = keys_lds[lane * size + i];
+        next = __builtin_amdgcn_fmed3f(best, next, c);
+        best = larger(best, c);
       }
     wave_lds_sync();
-    const F g = lane >= a.groups ? (F)-INFINITY : a.rank == 2 ? best + next : best;
-    int ahead = 0;
+  }
+  const bool holds = lane < a.groups * lanes;   // the lane holds a group's score, with the other lanes of the group
+  if (holds) g = a.rank == 2 ? best + next : best;
+  const bool in = holds && lanes_above<1>(g) < a.top_groups * lanes;
+  const unsigned who = row_vote(in);
+  const float worst_in = -row_max(in ? -g : -INFINITY), best_out = row_max(in || !holds ? -INFINITY : g);
+  if (a.group_lanes > 0) {
 #pragma unroll
-    for (int j = 0; j < SC_LANES; ++j) {
-      const F o = __shfl(g, j, SC_LANES);
-      ahead += (o > g || (o == g && j < lane)) ? 1 : 0;
-    }
-    const bool in = lane < a.groups && ahead < a.top_groups;
-    const unsigned allowed = row_vote(in);
-    if constexpr (!BY_LOGIT) {
-      const F worst_in = -row_max(in ? -g : (F)-INFINITY), best_out = row_max(in ? (F)-INFINITY : g);
-      if (best_out > (F)-INFINITY && !(worst_in - best_out > 2 * unit)) close = true;
-    }
+    for (int v = 0; v < V; ++v) key[v] = in ? key[v] : -INFINITY;
+  } else {
     int grp = e0 / size, left = size - e0 % size;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      if (!((allowed >> (grp & 31)) & 1u)) key[v] = (F)-INFINITY;
+      if (!((who >> (grp & 31)) & 1u)) key[v] = -INFINITY;
       if (--left == 0) { ++grp; left = size; }
     }
   }
+  // equal scores at the border let too many in
+  return __builtin_popcount(who) != a.top_groups * lanes || (best_out > -INFINITY && !(worst_in - best_out > unit));
+}
 
-  F last = (F)INFINITY;
-  for (int j = 0; j <= a.k; ++j) {   // one more than is chosen: the first that is not
-    F mine = key[0];
+// The k + 1 largest keys, best first, to pick_e in LDS (-1: none left), and what is not certain about them: ORDER, keys within `unit`
+// of each other among them; ALL, more than them.
+// Every lane keeps the best DEPTH of its keys in order, with the slot in place of the lowest bits, so that taking the
+// token's best is a step within its 16 lanes and a shift in one of them.  (Going through all V keys per choice: 32768
+// tokens, 8 of 256 experts in 8 groups, 77 us, with every uncertain token in double precision 43; as it is 24.)  A lane whose list runs out while
+// it had more keys than the list holds also leaves ALL open.
+enum { CERTAIN = 0, ORDER = 1, ALL = 2 };
+// numbers in order as integers, and back
+__device__ __forceinline__ int ordered(float f) { const int i = (int)__float_as_uint(f); return i ^ ((i >> 31) & 0x7fffffff); }
+__device__ __forceinline__ float from_ordered(int i) { return __uint_as_float((unsigned)(i ^ ((i >> 31) & 0x7fffffff))); }
+__device__ __forceinline__ int middle(int a, int b, int c) {
+  int m;
+  asm("v_med3_i32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+  return m;
+}
+template <int N> __device__ __forceinline__ int row_ror(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true); }
+__device__ __forceinline__ int row_max(int v) {
+  v = max(v, row_ror<1>(v));
+  v = max(v, row_ror<2>(v));
+  v = max(v, row_ror<4>(v));
+  return max(v, row_ror<8>(v));
+}
+template <int V>
+__device__ __forceinline__ int pick_fast(const ScoreArgs& a, const float (&key)[V], int lane, float unit, int* pick_e) {
+  constexpr int DEPTH = V < 8 ? V : 8;   // (six: 34.9 us with the gradient instead of 33.1; four: 51.6)
+  constexpr int SLOT = V - 1, CLOSED = (int)0x80000000u;   // below any key
+  int best[DEPTH];
 #pragma unroll
-    for (int v = 1; v < V; ++v) mine = key[v] > mine ? key[v] : mine;
-    const F top = row_max(mine);
-    if constexpr (!BY_LOGIT) { if (j > 0 && top > (F)-INFINITY && !(last - top > unit)) close = true; }
-    last = top;
-    if (j == a.k) break;
-    const unsigned have = row_vote(mine == top);
-    if (top > (F)-INFINITY) {
-      if (lane == __builtin_ctz(have)) {
-        bool done = false;
+  for (int q = 0; q < DEPTH; ++q) best[q] = CLOSED;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (!done && key[v] == top) {
-            done = true;
-            key[v] = (F)-INFINITY;
-            pick_e[j] = e0 + v;
-            pick_l[j] = l[v];
-          }
+  for (int v = 0; v < V; ++v) {
+    const int i = (ordered(__builtin_amdgcn_fmed3f(key[v], -3.0e38f, 3.0e38f)) & ~SLOT) | v;
+    const int x = key[v] > -INFINITY ? i : CLOSED;
+#pragma unroll
+    for (int q = DEPTH - 1; q > 0; --q) best[q] = middle(x, best[q - 1], best[q]);   // best[q - 1] >= best[q]
+    best[0] = max(best[0], x);
+  }
+  bool order = false, edge = false;   // edge: of the last key that is chosen and the first that is not
+  float last = INFINITY;
+  int taken = 0;
+  for (int j = 0; j <= a.k; ++j) {
+    const int top = row_max(best[0]);
+    const float f = from_ordered(top);
+    edge = top != CLOSED && !(last - f > unit);
+    order |= edge;
+    last = f;
+    if (lane == __builtin_ctz(row_vote(best[0] == top))) {
+      pick_e[j] = top != CLOSED ? lane * V + (top & SLOT) : -1;
+      if (top != CLOSED) {
+#pragma unroll
+        for (int q = 0; q + 1 < DEPTH; ++q) best[q] = best[q + 1];
+        best[DEPTH - 1] = CLOSED;
+        ++taken;
       }
-    } else if (lane == 0) {
-      pick_e[j] = -1;
-      pick_l[j] = -INFINITY;
     }
   }
+  const int top = row_max(best[0]);
+  const bool beyond = edge && top != CLOSED && !(last - from_ordered(top) > unit);
+  if (row_vote(beyond || (V > DEPTH && taken == DEPTH))) return ALL;
+  return order ? ORDER : CERTAIN;
+}
+
+// Puts the k + 1 candidates in their exact order: lane j compares candidate j's key (logit, or sigmoid score plus bias in double
+// precision) with the others'.
+template <bool BY_LOGIT>
+__device__ __forceinline__ void settle(const ScoreArgs& a, int lane, const float* logits, int* pick_e) {
+  const int e = lane <= a.k ? pick_e[lane] : -1;
+  double c = e >= 0 ? (double)logits[e] : (double)-INFINITY;
+  if (!BY_LOGIT && e >= 0) c = 1.0 / (1.0 + exp(-c)) + (a.balance != nullptr ? (double)a.balance[e] : 0.0);
+  int rank = 0;
+  for (int i = 0; i <= a.k; ++i) {
+    const double o = __shfl(c, i, SC_LANES);
+    const int oe = __shfl(e, i, SC_LANES);
+    rank += (oe >= 0 && (o > c || (o == c && oe < e))) ? 1 : 0;
+  }
   wave_lds_sync();
-  return close;
+  if (e >= 0) pick_e[rank] = e;
+}
+
+// ---- the choice, exactly ----
+// One token by the whole wave, in double precision, whose scores decide; by the logits as they are where they order the experts.
+template <int CTRL> __device__ __forceinline__ double dpp_of(double v) {
+  const unsigned long long b = (unsigned long long)__double_as_longlong(v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)b, CTRL, 0xf, 0xf, true);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(b >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double((long long)(lo | (unsigned long long)hi << 32));
+}
+__device__ __forceinline__ double wave_max(double v) {   // (no NaN)
+  auto up = [](double a, double b) { return a < b ? b : a; };
+  v = up(v, dpp_of<0x121>(v));   // within rows of 16: rotations by 1, 2, 4, 8
+  v = up(v, dpp_of<0x122>(v));
+  v = up(v, dpp_of<0x124>(v));
+  v = up(v, dpp_of<0x128>(v));
+  v = up(v, __shfl_xor(v, 16, WAVE));
+  return up(v, __shfl_xor(v, 32, WAVE));
+}
+template <int V, bool BY_LOGIT>
+__device__ __forceinline__ void choose_exact(const ScoreArgs& a, int t, int* pick_e) {
+  constexpr int VW = V < 4 ? 1 : V / 4;   // lane i holds the experts from i VW on
+  const int lane = threadIdx.x & (WAVE - 1), e0 = lane * VW;
+  const float* row = a.logits + (size_t)t * a.E;
+  double key[VW];
+  float l[VW];
+#pragma unroll
+  for (int v = 0; v < VW; ++v) {
+    l[v] = e0 + v < a.E ? usable(row[e0 + v]) : -INFINITY;
+    key[v] = l[v];
+  }
+  if constexpr (!BY_LOGIT) {
+    if (a.softmax) {
+      double top = -INFINITY, z = 0;
+#pragma unroll
+      for (int v = 0; v < VW; ++v) top = fmax(top, key[v]);
+      top = wave_max(top);
+#pragma unroll
+      for (int v = 0; v < VW; ++v) {
+        key[v] = l[v] > -INFINITY ? exp(key[v] - top) : 0.0;
+        z += key[v];
+        __builtin_amdgcn_sched_barrier(0);   // one after the other: together they take registers that the tokens' common path pays for
+      }
+#pragma unroll
+      for (int s = 1; s < WAVE; s <<= 1) z += __shfl_xor(z, s, WAVE);
+#pragma unroll
+      for (int v = 0; v < VW; ++v) key[v] = z > 0 ? key[v] / z : 0.0;
+    } else {
+#pragma unroll
+      for (int v = 0; v < VW; ++v) {
+        key[v] = l[v] > -INFINITY ? 1.0 / (1.0 + exp(-key[v])) : 0.0;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < VW; ++v) {
+      if (a.balance != nullptr && e0 + v < a.E) key[v] += (double)a.balance[e0 + v];
+      key[v] = (l[v] > -INFINITY && key[v] > (double)-INFINITY) ? key[v] : (double)-INFINITY;
+    }
+  }
+  if (a.groups > 1) {
+    const int size = a.E / a.groups;
+    double g = -INFINITY;   // lane q: of group q
+    const int run = size / VW;
+    if (size % VW == 0 && (run & (run - 1)) == 0) {   // groups of 2^n whole lanes: all at once
+      double best = -INFINITY, next = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < VW; ++v) merge_two(best, next, key[v], (double)-INFINITY);
+      for (int s = 1; s < run; s <<= 1) merge_two(best, next, __shfl_xor(best, s, WAVE), __shfl_xor(next, s, WAVE));
+      const double sum = a.rank == 2 ? best + next : best;
+      const double mine = __shfl(sum, min(lane * run, WAVE - 1), WAVE);
+      if (lane < a.groups) g = mine;
+    } else for (int q = 0; q < a.groups; ++q) {
+      double best = -INFINITY, next = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < VW; ++v)
+        if (e0 + v >= q * size && e0 + v < (q + 1) * size) merge_two(best, next, key[v], (double)-INFINITY);
+#pragma unroll
+      for (int s = 1; s < WAVE; s <<= 1) merge_two(best, next, __shfl_xor(best, s, WAVE), __shfl_xor(next, s, WAVE));
+      if (lane == q) g = a.rank == 2 ? best + next : best;
+    }
+    int ahead = 0;
+    for (int j = 0; j < a.groups; ++j) {
+      const double o = __shfl(g, j, WAVE);
+      ahead += (o > g || (o == g && j < lane)) ? 1 : 0;
+    }
+    const unsigned long long in = __ballot(lane < a.groups && ahead < a.top_groups);
+#pragma unroll
+    for (int v = 0; v < VW; ++v)
+      if (!((in >> ((e0 + v) / size & 63)) & 1)) key[v] = -INFINITY;
+  }
+  for (int j = 0; j < a.k; ++j) {
+    double mine = key[0];
+#pragma unroll
+    for (int v = 1; v < VW; ++v) mine = fmax(mine, key[v]);
+    const double top = wave_max(mine);
+    const unsigned long long have = __ballot(mine == top);
+    if (lane == __builtin_ctzll(have)) {
+      int e = -1;
+#pragma unroll
+      for (int v = VW - 1; v >= 0; --v)
+        if (key[v] == top) e = e0 + v;
+      if (top > (double)-INFINITY) {
+#pragma unroll
+        for (int v = 0; v < VW; ++v)
+          if (e == e0 + v) key[v] = -INFINITY;
+      } else e = -1;
+      pick_e[j] = e;
+    }
+  }
 }
 
 // Weight (without the scale) of the slot that lane j < k of a token holds; e < 0: an empty one.  z: the softmax's sum over all
@@ -198,26 +411,6 @@ __device__ __forceinline__ float slot_weight(const ScoreArgs& a, bool live, floa
   return s;
 }
 
-// lane i's V logits of token t
-template <int V>
-__device__ __forceinline__ void load_logits(const ScoreArgs& a, int t, int lane, float (&l)[V]) {
-  const float* row = a.logits + (size_t)t * a.E;
-  const int e0 = lane * V;
-  if (V >= 4 && (a.E & 3) == 0) {
-#pragma unroll
-    for (int v = 0; v < V; v += 4) {
-      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (e0 + v < a.E) q = *reinterpret_cast<const float4*>(row + e0 + v);
-      l[v] = q.x;
-      if constexpr (V >= 4) { l[v + 1] = q.y; l[v + 2] = q.z; l[v + 3] = q.w; }
-    }
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) l[v] = e0 + v < a.E ? row[e0 + v] : -INFINITY;
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) l[v] = usable(l[v]);
-}
 template <int V>
 __device__ __forceinline__ float top_of(const float (&l)[V]) {
   float m = l[0];
@@ -236,51 +429,102 @@ __device__ __forceinline__ float softmax_sum(const float (&l)[V], float top) {
 
 template <int V, bool BY_LOGIT>
 __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a) {
-  __shared__ double keys[SC_ROWS][SC_LANES * V];   // by the pass in single precision as floats
-  __shared__ int pick_e[SC_ROWS][MOE_MAX_K];
-  __shared__ float pick_l[SC_ROWS][MOE_MAX_K];
+  __shared__ float keys[SC_ROWS][SC_LANES * V];
+  __shared__ int pick_e[SC_ROWS][MOE_MAX_K + 1];
   const int lane = threadIdx.x & (SC_LANES - 1), r = threadIdx.x / SC_LANES;
-  const int t = blockIdx.x * SC_ROWS + r;
-  const bool row = t < a.T;
+  const int t = blockIdx.x * SC_ROWS + r, tc = min(t, a.T - 1);   // tokens past the batch repeat the last one and write nothing
   float l[V];
-  load_logits<V>(a, min(t, a.T - 1), lane, l);   // tokens past the batch repeat the last one and write nothing
+  load_row<V>(a.logits + (size_t)tc * a.E, a.E, lane, -INFINITY, l);
+#pragma unroll
+  for (int v = 0; v < V; ++v) l[v] = usable(l[v]);
   const float top = top_of<V>(l);
-  const bool close = choose<float, V, BY_LOGIT>(a, l, top, lane, reinterpret_cast<float*>(keys[r]), pick_e[r], pick_l[r]);
-  if constexpr (!BY_LOGIT) {
-    // Keys that lie closer together than single precision tells apart are ordered in double precision.
-    if (__ballot(close)) choose<double, V, BY_LOGIT>(a, l, top, lane, keys[r], pick_e[r], pick_l[r]);
+  int open;
+  {
+    // What two keys must differ by for their order to be certain.  A score in single precision: the exponential's argument is
+    // good to 2^-24 of itself, which x e^-x <= 0.37 turns into less than 2^-25 of the largest score; the exponential, the
+    // sum and the reciprocal add 2^-22 at most, the bias 2^-24 of the key; twice, for two keys: 2^-20.8, 5.6e-7, of the largest
+    // score and bias; for two sums of two, with their own roundings, three times that.  The slot's four bits change
+    // a key by up to 15 steps of at most 2^-23 of it, two keys by 30: 4.2e-6 in all.
+    float key[V];
+    const float most = make_keys<V, BY_LOGIT>(a, l, top, lane, key);
+    const bool groups_open = a.groups > 1 && restrict_groups<V>(a, key, lane, keys[r], BY_LOGIT ? 0.f : 1.7e-6f * most);
+    open = pick_fast<V>(a, key, lane, 4.2e-6f * most, pick_e[r]);
+    if (groups_open) open = ALL;
+    if (!BY_LOGIT && open == ORDER && a.softmax) open = ALL;   // a softmax score takes the sum over all experts
   }
-  const int e = lane < a.k ? pick_e[r][lane] : -1;
-  const float le = lane < a.k ? pick_l[r][lane] : -INFINITY;
+  // what the weights need of the logits, before the rare path below wants the registers
   const float z = a.softmax && !a.renorm ? softmax_sum<V>(l, top) : 1.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) keys[r][lane * V + v] = l[v];
+  wave_lds_sync();
+  if (__ballot(open == ORDER)) {
+    if (open == ORDER) settle<BY_LOGIT>(a, lane, keys[r], pick_e[r]);
+  }
+  for (unsigned long long rows = __ballot(open == ALL && t < a.T); rows != 0;) {   // the rest, seldom, one token after the other
+    const int of = __builtin_ctzll(rows) / SC_LANES;
+    rows &= ~(0xffffull << (of * SC_LANES));
+    const int first = (threadIdx.x / WAVE) * (WAVE / SC_LANES) + of;          // the token's place in the block
+    wave_lds_sync();
+    choose_exact<V, BY_LOGIT>(a, blockIdx.x * SC_ROWS + first, pick_e[first]);
+  }
+  wave_lds_sync();
+  const int e = lane < a.k ? pick_e[r][lane] : -1;
+  const float le = e >= 0 ? keys[r][e] : -INFINITY;
   float unused;
   const float w = slot_weight(a, e >= 0, le, top, z, unused);
-  if (row && lane < a.k) {
+  if (t < a.T && lane < a.k) {
     a.topk_idx[(size_t)t * a.k + lane] = e;
     a.topk_w[(size_t)t * a.k + lane] = w * a.scale;
   }
 }
 
-// Gradient of the logits.  The slots' gradients meet their experts in an LDS row, which leaves as whole lines.
+// Gradient of the logits.  The slots' gradients meet their experts in an LDS row, which leaves in pieces of 256 bytes.
 template <int V>
 __global__ __launch_bounds__(256) void score_bwd_kernel(ScoreArgs a, const float* __restrict__ d_topk_w, float* __restrict__ d_logits) {
+  constexpr int P = V < 4 ? V : 4, N = V / P;   // lane i has N pieces of P experts, piece j from (16 j + i) P on
   __shared__ float grad[SC_ROWS][SC_LANES * V];
   const int lane = threadIdx.x & (SC_LANES - 1), r = threadIdx.x / SC_LANES;
   const int t = blockIdx.x * SC_ROWS + r, tc = min(t, a.T - 1);
   const bool dense = a.softmax && !a.renorm;   // the sum over all experts has a gradient too
-  float l[V], top = 0.f, z = 1.f;
-  if (dense) {
-    load_logits<V>(a, tc, lane, l);
-    top = top_of<V>(l);
-    z = softmax_sum<V>(l, top);
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) grad[r][lane * V + v] = 0.f;
+  const bool whole = P == 4 && (a.E & 3) == 0;
+  const float* row = a.logits + (size_t)tc * a.E;
   int e = lane < a.k ? a.topk_idx[(size_t)tc * a.k + lane] : -1;
   if (e >= a.E) e = -1;
-  const float le = e >= 0 ? usable(a.logits[(size_t)tc * a.E + e]) : -INFINITY;
+  const float dw0 = lane < a.k ? d_topk_w[(size_t)tc * a.k + lane] : 0.f;
+  float l[V], top = 0.f, z = 1.f;
+  if (dense) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int c = (j * SC_LANES + lane) * P;
+      if (whole) {
+        float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (c < a.E) q = *reinterpret_cast<const float4*>(row + c);
+        if constexpr (P == 4) { l[j * P] = q.x; l[j * P + 1] = q.y; l[j * P + 2] = q.z; l[j * P + 3] = q.w; }
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) l[j * P + p] = c + p < a.E ? row[c + p] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) l[v] = usable(l[v]);
+    top = top_of<V>(l);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int p = 0; p < P; ++p) grad[r][(j * SC_LANES + lane) * P + p] = 0.f;
+  const float le = e >= 0 ? usable(row[e]) : -INFINITY;
+  if (dense) {
+    z = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      l[v] = l[v] > -INFINITY ? expf(l[v] - top) : 0.f;   // from here on the exponentials
+      z += l[v];
+    }
+    z = row_sum(z);
+  }
   const bool live = le > -INFINITY;
-  const float dw = live ? d_topk_w[(size_t)tc * a.k + lane] : 0.f;
+  const float dw = live ? dw0 : 0.f;
   float one_minus_s;
   const float p = slot_weight(a, live, le, top, z, one_minus_s);
   const float D = row_sum(p * dw);
@@ -289,22 +533,24 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(ScoreArgs a, const float
   wave_lds_sync();
   if (t >= a.T) return;
   float* out = d_logits + (size_t)t * a.E;
-  const int e0 = lane * V;
-  float o[V];
+  const float f = dense ? (z > 0.f ? a.scale / z : 0.f) : 1.f;
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    o[v] = grad[r][e0 + v];
-    if (dense) o[v] = l[v] > -INFINITY ? a.scale * (expf(l[v] - top) / z) * (o[v] - D) : 0.f;
-  }
-  if (V >= 4 && (a.E & 3) == 0) {
+  for (int j = 0; j < N; ++j) {
+    const int c = (j * SC_LANES + lane) * P;
+    float o[P];
 #pragma unroll
-    for (int v = 0; v < V; v += 4)
-      if constexpr (V >= 4)
-        if (e0 + v < a.E) *reinterpret_cast<float4*>(out + e0 + v) = make_float4(o[v], o[v + 1], o[v + 2], o[v + 3]);
-  } else {
+    for (int q = 0; q < P; ++q) {
+      o[q] = grad[r][c + q];
+      if (dense) o[q] = f * l[j * P + q] * (o[q] - D);
+    }
+    if (whole) {
+      if constexpr (P == 4)
+        if (c < a.E) *reinterpret_cast<float4*>(out + c) = make_float4(o[0], o[1], o[2], o[3]);
+    } else {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (e0 + v < a.E) out[e0 + v] = o[v];
+      for (int q = 0; q < P; ++q)
+        if (c + q < a.E) out[c + q] = o[q];
+    }
   }
 }
 
@@ -348,9 +594,14 @@ __global__ __launch_bounds__(256) void score_dx_kernel(const float* __restrict__
   }
 }
 
+static int per_lane(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : 16; }
+static int group_lanes(int E, int groups) {
+  const int size = E / groups, n = size / per_lane(E);
+  return size % per_lane(E) == 0 && (n & (n - 1)) == 0 ? n : 0;
+}
 static ScoreArgs score_args(const moe_cfg* c, const moe_score* sc, const float* logits, const float* balance, int32_t* idx, float* w) {
   return ScoreArgs{logits, balance, idx, w, c->T, c->E, c->k, sc->score == MOE_SCORE_SOFTMAX, sc->groups, sc->top_groups, sc->group_rank,
-                   sc->renorm != 0, sc->scale};
+                   sc->renorm != 0, group_lanes(c->E, sc->groups), sc->scale};
 }
 
 template <int V>
@@ -364,21 +615,25 @@ int launch_score(const moe_cfg* c, const moe_score* sc, const float* logits, con
   const ScoreArgs a = score_args(c, sc, logits, balance, idx, w);
   // Both scores grow with their logit: without a bias, and where no scores are added up, the logits decide
   const bool by_logit = balance == nullptr && (sc->groups == 1 || sc->group_rank == 1);
-  if (c->E <= 16) return launch_score_v<1>(a, by_logit, s);
-  if (c->E <= 32) return launch_score_v<2>(a, by_logit, s);
-  if (c->E <= 64) return launch_score_v<4>(a, by_logit, s);
-  if (c->E <= 128) return launch_score_v<8>(a, by_logit, s);
-  return launch_score_v<16>(a, by_logit, s);
+  switch (per_lane(c->E)) {
+    case 1: return launch_score_v<1>(a, by_logit, s);
+    case 2: return launch_score_v<2>(a, by_logit, s);
+    case 4: return launch_score_v<4>(a, by_logit, s);
+    case 8: return launch_score_v<8>(a, by_logit, s);
+    default: return launch_score_v<16>(a, by_logit, s);
+  }
 }
 
 int launch_score_bwd(const moe_cfg* c, const moe_score* sc, const float* logits, const int32_t* idx, const float* dw, float* d_logits, hipStream_t s) {
   const ScoreArgs a = score_args(c, sc, logits, nullptr, const_cast<int32_t*>(idx), nullptr);
   const unsigned grid = (unsigned)((a.T + SC_ROWS - 1) / SC_ROWS);
-  if (c->E <= 16) score_bwd_kernel<1><<<grid, 256, 0, s>>>(a, dw, d_logits);
-  else if (c->E <= 32) score_bwd_kernel<2><<<grid, 256, 0, s>>>(a, dw, d_logits);
-  else if (c->E <= 64) score_bwd_kernel<4><<<grid, 256, 0, s>>>(a, dw, d_logits);
-  else if (c->E <= 128) score_bwd_kernel<8><<<grid, 256, 0, s>>>(a, dw, d_logits);
-  else score_bwd_kernel<16><<<grid, 256, 0, s>>>(a, dw, d_logits);
+  switch (per_lane(c->E)) {
+    case 1: score_bwd_kernel<1><<<grid, 256, 0, s>>>(a, dw, d_logits); break;
+    case 2: score_bwd_kernel<2><<<grid, 256, 0, s>>>(a, dw, d_logits); break;
+    case 4: score_bwd_kernel<4><<<grid, 256, 0, s>>>(a, dw, d_logits); break;
+    case 8: score_bwd_kernel<8><<<grid, 256, 0, s>>>(a, dw, d_logits); break;
+    default: score_bwd_kernel<16><<<grid, 256, 0, s>>>(a, dw, d_logits);
+  }
   return launch_status();
 }
 
