@@ -84,13 +84,15 @@ __device__ __forceinline__ void decode8(const uint2& code, unsigned scale, float
   }
 }
 
-// The ranges in LDS, one first row and one last per expert (everything: one range).
+// Which rows take part, from LDS: with slices the experts' first rows and ends, without them the one end of all rows.
 struct RangeTable {
-  const int32_t* t;   // offsets [E + 1], then nothing; with slices: first rows [E], ends [E]
+  const int32_t* t;   // [E] first rows, [E] ends
   int E;
-  bool all;
+  bool all, sliced;
+  long long end;
+  __device__ __forceinline__ long long limit(long long rows) const { return all ? rows : end; }
   __device__ __forceinline__ bool live(long long row) const {
-    if (all) return true;
+    if (!sliced) return all || row < end;
     int lo = 0, hi = E;   // the last range that starts at or before the row
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -100,8 +102,10 @@ struct RangeTable {
   }
 };
 __device__ __forceinline__ RangeTable load_range(const RowRange& r, int32_t* lds) {
-  RangeTable t = {lds, r.E, r.offsets == nullptr};
+  RangeTable t = {lds, r.E, r.offsets == nullptr, r.lo != nullptr, 0};
   if (t.all) return t;
+  t.end = (long long)r.offsets[r.E - 1] + r.kept[r.E - 1];   // the experts' rows follow each other
+  if (!t.sliced) return t;
   for (int e = threadIdx.x; e < r.E; e += blockDim.x) {
     int l, h;
     share_of(r.lo, r.hi, r.kept[e], e, l, h);
