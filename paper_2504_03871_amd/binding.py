@@ -131,13 +131,12 @@ def make_cfg(T, d_model, d_ff, E, k, dtype=DTYPE_BF16, act=ACT_GELU, capacity=0)
 
 
 def _ptr(t):
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return ctypes.c_void_p(t)
+    """A tensor's address (or None, or an address as it is); the argument types make a pointer of it."""
+    if t is None or t.__class__ is int:
+        return t
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _nbytes(t):
@@ -149,9 +148,18 @@ def _nbytes(t):
     return t.numel() * t.element_size()
 
 
+_raw_stream = None
+
+
 def _stream():
-    import torch
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """Address of torch's current stream on the current device."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        # the address alone: a Stream object per call takes longer than a short kernel
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+        _raw_stream = (lambda: raw(device())) if raw is not None else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream()
 
 
 def _check(name, rc):
