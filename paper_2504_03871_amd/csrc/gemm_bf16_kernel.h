@@ -784,7 +784,7 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
     if constexpr (DUAL && DENSE) put_sums(acc2, part_sums + BM * BN);   // the second matrix's behind the first's
     return;
   }
-  if constexpr (MODE == MODE_TN) {   // fp32 weight gradient of expert e; M is a multiple of 64: whole bands
+  if constexpr (MODE == MODE_TN && EPI == EPI_DW) {   // fp32 weight gradient of expert e; M is a multiple of 64: whole bands
     static_assert(TNN % 2 == 0, "pairs of column tiles");
     const size_t first = ((size_t)e * g.M + m0) * g.N + n0;
     const __amdgpu_buffer_rsrc_t rc = out_rsrc(reinterpret_cast<float*>(second ? g.C2 : g.C) + first, ((size_t)mvalid * g.N - n0) * 4);
@@ -829,9 +829,10 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
     // Bias, activation and residual on the fp32 sums: eight columns per lane, the residual requested AHEAD row tiles ahead.
     constexpr int NH = TNN / 2, AHEAD = TNN == 4 ? 3 : 4;   // stores per row tile: of 8 rows x 128 bytes, or one of 16 x 64
     typedef Half16<ST> H;
-    const size_t first = (size_t)row0 * g.N + n0, bytes = ((size_t)mvalid * g.N - n0) * 2;
+    // (MODE_TN: a weight gradient in the storage type, of the whole of the rows: no bias, no residual, C or C2)
+    const size_t first = (size_t)(MODE == MODE_TN ? m0 : row0) * g.N + n0, bytes = ((size_t)mvalid * g.N - n0) * 2;
     auto plane = [&](const void* p) { return out_rsrc(reinterpret_cast<const ST*>(p) + (p != nullptr ? first : 0), p != nullptr ? bytes : 0); };
-    const __amdgpu_buffer_rsrc_t oy = plane(g.C3), oz = plane(g.C), oz2 = plane(DUAL ? g.C2 : g.C), res = plane(g.S1);
+    const __amdgpu_buffer_rsrc_t oy = plane(MODE == MODE_TN ? (second ? g.C2 : g.C) : g.C3), oz = plane(MODE == MODE_TN ? nullptr : g.C), oz2 = plane(DUAL ? g.C2 : nullptr), res = plane(g.S1);
     const unsigned pitch = (unsigned)g.N * 2u, lane_col = (unsigned)(wn * C + (TNN == 4 ? right * 32 : 0) + lane_col8(grp));
     auto at = [&](int i, int h) {
       const int m = band_row(i) + (TNN == 4 ? h * 8 + r8 : (lane & 15));

@@ -19,7 +19,7 @@ inline BiasGeom bias_geom(long long T, int N) {
   const long long want = 2048 / g.col_blocks > 0 ? 2048 / g.col_blocks : 1;
   long long rows = (T + want - 1) / want;
   rows = (rows + rp - 1) / rp * rp;
-  if (rows < 4 * rp) rows = 4 * rp;
+  if (rows < rp) rows = rp;
   while ((T + rows - 1) / rows > 65535) rows *= 2;
   g.rows = (int)rows;
   g.row_blocks = (int)((T + rows - 1) / rows);

@@ -63,13 +63,12 @@ static int dw_segments(const moe_linear* c, int mats) {
     slots = F32_LOW_TILES;
     per_row = 0.06;
   }
-  const bool direct = c->grad == MOE_DTYPE_F32;   // one segment: the product writes the gradient itself
   int best = least;
   double cost = 1e30;
   for (int s = least; s <= std::max(least, 16) && (s == least || T / s >= 256); ++s) {
     const double rounds = (double)((tiles * s + slots - 1) / slots);
     double us = rounds * per_row * (double)((T + s - 1) / s);
-    if (s > 1 || !direct) us += 3.0 + (double)out * 4 * s * 2 / 4e6;
+    if (s > 1) us += 3.0 + (double)out * 4 * s * 2 / 4e6;
     if (us < cost * 0.97) { cost = us; best = s; }
   }
   return best;
@@ -105,7 +104,7 @@ LinearPlan linear_plan(const moe_linear* c) {
   p.segs = c->T > 0 ? dw_segments(c, mats) : 1;
   p.seg = seg_rows(c->T, p.segs);
   p.segs = c->T > 0 ? (c->T + p.seg - 1) / p.seg : 1;
-  p.dw_direct = p.segs == 1 && c->grad == MOE_DTYPE_F32;
+  p.dw_direct = p.segs == 1;   // the product writes the gradient itself
   if (!p.dw_direct) off += align_up((size_t)mats * p.segs * c->d_in * N * 4, 256);
   p.total = std::max(align_up(fwd, 256), off);
   return p;
@@ -245,29 +244,40 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
     if constexpr (FMT == MOE_PACK_NONE) load(p, r, v);
     else decode8<ST, FMT>(*reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(p) + r * blocks * BLOCK8 + c), sc[r * blocks + c / BLOCK8], v);
   };
+  // U rows of a thread are requested together; a row past the end repeats the last one and counts for nothing
+  constexpr int U = sizeof(ST) == 4 ? 1 : 2;
   if (n > 0)
-    for (long long r = r0 + rl; r < r1; r += rp) {
-      float dy[8] = {}, z[8] = {}, z2[8] = {};
-      load(a.dy, r, dy);
-      if constexpr (ACT != MOE_ACT_NONE) load_pre(a.pre, a.scales, r, z);
-      if constexpr (DUAL) load_pre(a.pre2, a.scales2, r, z2);
-      float g[8], g2[8];
+    for (long long ra = r0 + rl; ra < r1; ra += (long long)rp * U) {
+      float dy[U][8] = {}, z[U][8] = {}, z2[U][8] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (DUAL) {
-          const float sg = sizeof(ST) == 4 ? sigmoid_f(z[i]) : sigmoid_fast(z[i]);
-          g[i] = dy[i] * z2[i] * sg * fmaf(z[i], 1.f - sg, 1.f);
-          g2[i] = dy[i] * z[i] * sg;
-          sum2[i] += g2[i];
-        } else if constexpr (ACT == MOE_ACT_GELU) {
-          g[i] = dy[i] * (sizeof(ST) == 4 ? gelu_grad_f(z[i]) : gelu_grad_fast(z[i]));
-        } else {
-          g[i] = dy[i];
-        }
-        sum[i] += g[i];
+      for (int u = 0; u < U; ++u) {
+        const long long r = min(ra + (long long)u * rp, r1 - 1);
+        load(a.dy, r, dy[u]);
+        if constexpr (ACT != MOE_ACT_NONE) load_pre(a.pre, a.scales, r, z[u]);
+        if constexpr (DUAL) load_pre(a.pre2, a.scales2, r, z2[u]);
       }
-      if constexpr (ACT != MOE_ACT_NONE) store(a.dz, r, g);
-      if constexpr (DUAL) store(a.dz2, r, g2);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long r = ra + (long long)u * rp;
+        if (r >= r1) break;
+        float g[8], g2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if constexpr (DUAL) {
+            const float sg = sizeof(ST) == 4 ? sigmoid_f(z[u][i]) : sigmoid_fast(z[u][i]);
+            g[i] = dy[u][i] * z2[u][i] * sg * fmaf(z[u][i], 1.f - sg, 1.f);
+            g2[i] = dy[u][i] * z[u][i] * sg;
+            sum2[i] += g2[i];
+          } else if constexpr (ACT == MOE_ACT_GELU) {
+            g[i] = dy[u][i] * (sizeof(ST) == 4 ? gelu_grad_f(z[u][i]) : gelu_grad_fast(z[u][i]));
+          } else {
+            g[i] = dy[u][i];
+          }
+          sum[i] += g[i];
+        }
+        if constexpr (ACT != MOE_ACT_NONE) store(a.dz, r, g);
+        if constexpr (DUAL) store(a.dz2, r, g2);
+      }
     }
   if (a.sums == nullptr) return;
 #pragma unroll
@@ -311,6 +321,28 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(JoinArgs a) {
     const float v = s[q] + (a.accumulate ? to_f32(out[q]) : 0.f);
     out[q] = from_f32<OT>(v);
   }
+}
+
+// The same for short rows, many of them: 16 threads of four columns by 16 rows at a time, whose sums are added in order.
+template <typename OT>
+__global__ __launch_bounds__(256) void sum_many_rows_kernel(JoinArgs a) {
+  __shared__ f32x4 part[16][17];
+  const int cl = threadIdx.x & 15, rl = threadIdx.x >> 4;
+  const size_t i = ((size_t)blockIdx.x * 16 + cl) * 4;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (i < a.n) {
+    const float* src = a.parts[blockIdx.y] + i;
+#pragma unroll 8
+    for (int r = rl; r < a.rows; r += 16) s += *reinterpret_cast<const f32x4*>(src + (size_t)r * a.n);
+  }
+  part[rl][cl] = s;
+  __syncthreads();
+  if (rl != 0 || i >= a.n) return;
+#pragma unroll
+  for (int r = 1; r < 16; ++r) s += part[r][cl];
+  OT* out = reinterpret_cast<OT*>(a.out[blockIdx.y]) + i;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) out[q] = from_f32<OT>(s[q] + (a.accumulate ? to_f32(out[q]) : 0.f));
 }
 
 __global__ void linear_zero_kernel(uint32_t* p, size_t n) {
@@ -407,12 +439,16 @@ static int act_bwd_for(int act, const ActBwdArgs& a, int fmt, hipStream_t s) {
          : act == MOE_ACT_GELU ? launch_act_bwd<ST, MOE_ACT_GELU>(a, fmt, s)
                                : launch_act_bwd<ST, MOE_ACT_NONE>(a, fmt, s);
 }
-static int launch_sum_rows(const JoinArgs& a, int mats, int type, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n / 4 + 255) / 256), mats);
-  if (type == MOE_DTYPE_BF16) sum_rows_kernel<bf16><<<grid, 256, 0, s>>>(a);
-  else if (type == MOE_DTYPE_F16) sum_rows_kernel<f16><<<grid, 256, 0, s>>>(a);
-  else sum_rows_kernel<float><<<grid, 256, 0, s>>>(a);
+template <typename OT>
+static int sum_rows_for(const JoinArgs& a, int mats, bool many, hipStream_t s) {
+  if (many) sum_many_rows_kernel<OT><<<dim3((unsigned)((a.n / 4 + 15) / 16), mats), 256, 0, s>>>(a);
+  else sum_rows_kernel<OT><<<dim3((unsigned)((a.n / 4 + 255) / 256), mats), 256, 0, s>>>(a);
   return launch_status();
+}
+static int launch_sum_rows(const JoinArgs& a, int mats, int type, bool many, hipStream_t s) {
+  return type == MOE_DTYPE_BF16 ? sum_rows_for<bf16>(a, mats, many, s)
+         : type == MOE_DTYPE_F16 ? sum_rows_for<f16>(a, mats, many, s)
+                                 : sum_rows_for<float>(a, mats, many, s);
 }
 static int zero(void* p, size_t bytes, hipStream_t s) {
   if (p == nullptr) return MOE_OK;
@@ -455,7 +491,7 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
                                     : act_bwd_for<bf16>(c->act, a, c->pre_pack, s));
     if (dbias != nullptr) {
       const JoinArgs j = {{a.sums, a.sums2}, {dbias, dbias_b}, (size_t)N, p.bias_geom.row_blocks, accumulate};
-      TRY(launch_sum_rows(j, mats, c->grad, s));
+      TRY(launch_sum_rows(j, mats, c->grad, true, s));
     }
   }
   GemmArgs g = {};
@@ -482,11 +518,14 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
   g.M = d; g.N = N; g.K = c->T; g.E = p.segs; g.seg = p.seg;
   g.accumulate = p.dw_direct && accumulate;
   if (es == 4) TRY(launch_linear_f32(MODE_TN, EPI_DW, false, g, s));
+  else if (p.dw_direct && c->grad != MOE_DTYPE_F32)
+    TRY(c->dtype == MOE_DTYPE_F16 ? (launch_rows_bm<f16, MODE_TN, EPI_LIN_NONE, false, false, 256>(g, 0, s))
+                                  : (launch_rows_bm<bf16, MODE_TN, EPI_LIN_NONE, false, false, 256>(g, 0, s)));
   else if (c->dtype == MOE_DTYPE_F16) TRY((launch_rows_bm<f16, MODE_TN, EPI_DW, false, false, 256>(g, 0, s)));
   else TRY((launch_rows_bm<bf16, MODE_TN, EPI_DW, false, false, 256>(g, 0, s)));
   if (p.dw_direct) return MOE_OK;
   const JoinArgs j = {{sums, sums + out * p.segs}, {dW, dWb}, out, p.segs, accumulate};
-  return launch_sum_rows(j, mats, c->grad, s);
+  return launch_sum_rows(j, mats, c->grad, false, s);
 }
 
 }  // namespace moe
