@@ -304,7 +304,7 @@ struct GemmArgs {
   int tile_rows; // row-tile GEMMs: rows per entry of the tile map
   // Dense products, one matrix and no experts, know their tiles without a map.  Row-tile GEMMs: M rows; tiles from split_first on
   // are cut along K into split_parts (1: none).  Weight gradients: K rows in E segments of `seg`, each with a gradient of its own.
-  int split_first, split_parts, seg;
+  int split_first, split_parts, seg, tile_cols;
   const void* bias;    // storage type, may be NULL
   const void* bias2;
 };

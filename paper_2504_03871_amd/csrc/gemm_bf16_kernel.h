@@ -585,7 +585,8 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
     // scheduler may not move instructions across (sched_barrier).  Region i holds the MFMAs of row tile i;
     // behind them, the read of row tile i's A fragment for the NEXT K step, into the same registers (their
     // last use has just been issued, and the fragment is not needed for another TM - 1 regions), in the
-    // first TNN regions one B fragment of the next step (into the other of two B register sets), and this
+    // first TNN regions one B fragment of the next step (into the other of two B register sets; with fewer regions
+    // than fragments several), and this
     // region's share of the global -> LDS loads.  LDS reads and, above all, the global loads then arrive as a
     // steady trickle: loads issued in one burst fill the address FIFO of the memory pipe, and a wave that
     // cannot issue a load cannot issue the MFMAs behind it either.
@@ -646,7 +647,8 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
       }                                                                                                     \
       if (DO_NEXT_) {                                                                                       \
         MOE_FRAG_A(r__, rabuf_, rks_);                                                                      \
-        if (r__ < TNN) MOE_FRAG_B((set_) ^ 1, r__ < TNN ? r__ : 0, rbbuf_, rks_);                           \
+        _Pragma("unroll") for (int j__ = 0; j__ < TNN; ++j__)                                               \
+          if (j__ % NR == r__) MOE_FRAG_B((set_) ^ 1, j__, rbbuf_, rks_);                                   \
       }                                                                                                     \
       _Pragma("unroll") for (int q__ = 0; q__ < L; ++q__)                                                   \
         if (q__ >= (Q0_) && q__ < (Q1_) && load_region(q__) == r__)                                         \

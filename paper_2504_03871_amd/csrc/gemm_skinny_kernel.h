@@ -21,39 +21,26 @@ constexpr int skinny_stage_bytes() { return SKINNY_ROWS * BKT * 2 + SKINNY_BN * 
 template <bool DUAL>
 constexpr int skinny_stages() { return 80 * 1024 / skinny_stage_bytes<DUAL>(); }   // two blocks per compute unit
 
-// DENSE: one matrix instead of one per expert and at most SKINNY_ROWS rows; every tile is cut along K into g.split_parts parts whose
-// sums go to the workspace, [matrix][part][row][column].
-template <typename ST, int EPI, bool DUAL, bool DENSE = false>
-__device__ __forceinline__ void gemm_skinny_tile(const GemmArgs& g, char* smem) {
+template <typename ST, int EPI, bool DUAL>
+__global__ __launch_bounds__(256, 2) void gemm_skinny_kernel(GemmArgs g) {
   constexpr int BM = SKINNY_ROWS, BN = SKINNY_BN, A_BYTES = BM * BKT * 2, B_BYTES = BN * BKT * 2;
   constexpr int STAGE = skinny_stage_bytes<DUAL>(), NB = skinny_stages<DUAL>(), AHEAD = NB - 1;
   constexpr int TM = BM / 16, TN = BN / 64;                      // 16 x 16 tiles of a wave: all rows, BN / 4 columns
   constexpr int CHA = BM * BKT / 8 / 256, CHB = BN * BKT / 8 / 256, L = CHA + CHB * (DUAL ? 2 : 1);
+  extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
+  const int ntn = (g.N + BN - 1) / BN, n_rt = g.ntiles[0];
   constexpr bool CAN_SPLIT = EPI == EPI_STORE;
+  const SkinnyOrder so = skinny_order(n_rt, g.ntiles[2] != 0, g.E, CAN_SPLIT && g.split_all);
+  const int parts = 1 << so.shift;
   RowBlock rb;
-  RowTile t;
-  int parts, k0, k1;
-  const int stages = g.K / BKT;
-  if constexpr (DENSE) {   // neighbours: the K parts of a tile, then its next columns, so that the chip reads whole weight rows
-    parts = g.split_parts;
-    rb = RowBlock{0, (int)blockIdx.x / parts, 0, (int)blockIdx.x % parts};
-    t = RowTile{0, 0, g.M, 0};
-    k0 = __builtin_amdgcn_readfirstlane(rb.ksplit * stages / parts);
-    k1 = __builtin_amdgcn_readfirstlane((rb.ksplit + 1) * stages / parts);
-  } else {
-    const int ntn = (g.N + BN - 1) / BN, n_rt = g.ntiles[0];
-    const SkinnyOrder so = skinny_order(n_rt, g.ntiles[2] != 0, g.E, CAN_SPLIT && g.split_all);
-    parts = 1 << so.shift;
-    if (!skinny_block(blockIdx.x, so, ntn, rb)) return;
-    t = g.tiles[rb.rt];
-    k0 = __builtin_amdgcn_readfirstlane((rb.ksplit * stages) >> so.shift);
-    k1 = __builtin_amdgcn_readfirstlane(((rb.ksplit + 1) * stages) >> so.shift);
-  }
+  if (!skinny_block(blockIdx.x, so, ntn, rb)) return;
+  const RowTile t = g.tiles[rb.rt];
   const bool shared = __builtin_amdgcn_readfirstlane(t.mates) != 0;
-  const int kbase = k0 * BKT, KT = k1 - k0;
+  const int stages = g.K / BKT, k0 = __builtin_amdgcn_readfirstlane((rb.ksplit * stages) >> so.shift), kbase = k0 * BKT;
+  const int KT = __builtin_amdgcn_readfirstlane(((rb.ksplit + 1) * stages) >> so.shift) - k0;
   const int n0 = rb.nt * BN, mvalid = t.nrows, ni = (mvalid + 15) / 16;   // ni: row tiles with valid rows
 
   const rsrc_t ra = make_rsrc(reinterpret_cast<const bf16*>(g.A) + (size_t)t.row0 * g.K + kbase, ((size_t)mvalid * g.K - kbase) * 2);
@@ -148,25 +135,6 @@ __device__ __forceinline__ void gemm_skinny_tile(const GemmArgs& g, char* smem) 
   static_assert(TN == 2, "one pair of column tiles per wave");
   const int c0 = wave * (BN / 4);
   if (n0 + c0 >= g.N) return;
-  if constexpr (DENSE) {
-    const int r8 = lane & 7, right = (lane >> 3) & 1;
-    auto put_sums = [&](f32x4 (&a)[TM][TN], int matrix) {
-      float* sums = g.split_ws + (size_t)(matrix * parts + rb.ksplit) * mvalid * g.N + n0 + c0 + right * 16 + grp * 4;
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-        if (i < ni) {
-          swap8(a[i][0], a[i][1]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int m = i * 16 + h * 8 + r8;
-            if (m < mvalid) *reinterpret_cast<f32x4*>(sums + (size_t)m * g.N) = a[i][h];
-          }
-        }
-    };
-    put_sums(acc, 0);
-    if constexpr (DUAL) put_sums(acc2, 1);
-    return;
-  }
   if (CAN_SPLIT && rb.split_tile >= 0) {   // fp32 partial sums of this block's K part
     const int r8 = lane & 7, right = (lane >> 3) & 1;
     float* sums = g.split_ws + ((size_t)rb.split_tile * parts + rb.ksplit) * SKINNY_ROWS * g.N + n0 + c0 + right * 16 + grp * 4;
@@ -190,12 +158,6 @@ __device__ __forceinline__ void gemm_skinny_tile(const GemmArgs& g, char* smem) 
       const unsigned off[1] = {m < mvalid ? ((unsigned)m * g.N + c0 + lane_col8(grp)) * 2u : OUT_OF_RANGE};
       epilogue_fwd<ST, EPI, 1, 0>(o, off, acc[i], acc2[DUAL ? i : 0], g.gelu_tab);
     }
-}
-
-template <typename ST, int EPI, bool DUAL>
-__global__ __launch_bounds__(256, 2) void gemm_skinny_kernel(GemmArgs g) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  gemm_skinny_tile<ST, EPI, DUAL>(g, smem);
 }
 
 }  // namespace moe

@@ -4,8 +4,8 @@
 
 namespace moe {
 
-// Row tiles of a 16-bit product: tiles from `first` on are cut along K into `parts`.
-struct RowCut { long long tiles, first; int tile_rows, parts; };
+// Tiles of a 16-bit product, rows x cols (of either matrix, where there are two): those from `first` on are cut along K into `parts`.
+struct RowCut { long long tiles, first; int rows, cols, parts; };
 
 // Blocks of the pass over dy: cg threads (a power of two) of eight columns each span a block's columns, `rows` rows per block.
 struct BiasGeom { int cg, rows, col_blocks, row_blocks; };
@@ -27,11 +27,10 @@ inline BiasGeom bias_geom(long long T, int N) {
 }
 
 struct LinearPlan {
-  bool skinny;        // forward: few rows
-  int parts;          // ... cut along K
   RowCut fwd, dx;
   BiasGeom bias_geom;
-  int segs, seg;      // weight gradient: segments of the tokens, rows of one
+  int dw_rows;        // weight gradient: edge of its tiles
+  int segs, seg;      // ... segments of the tokens, rows of one
   bool dw_direct;     // ... written by the product itself
   size_t dz, db, split, dw, total;   // workspace: byte offsets of the backward's regions; the forward has it to itself
 };

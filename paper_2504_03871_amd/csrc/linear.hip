@@ -1,14 +1,13 @@
 // Dense products with a fused epilogue, y = act(x W + bias) + residual, and their backward (the shared expert of an MoE block).
 //
-// The products run on the tiles of the grouped GEMMs (gemm_bf16_kernel.h, gemm_skinny_kernel.h, gemm_f32.hip) with one matrix and
-// no tile map; bias, activation, residual and the rounding to the storage type sit in their epilogues, on the fp32 sums.  Where the
-// sums of a tile are cut along K, so that few tiles fill the chip, the kernel that adds the parts has the epilogue.
-//   forward   up to SKINNY_ROWS rows: 64 x 128 tiles, every one cut along K (a read of the weights: HBM);
-//             more: 160- or 256-row tiles (matrix cores), the last round cut along K
-//   backward  dz = dy act'(pre) and its column sums in one pass (HBM); dx = dz W^T on row tiles; dW = x^T dz on 256 x 256 tiles, the
-//             tokens cut into segments where the gradient has few tiles, whose sums a last pass adds up
-#include "gemm_bf16_kernel.h"
-#include "gemm_skinny_kernel.h"
+// The products run on the tiles of the grouped GEMMs (gemm_bf16_kernel.h, gemm_f32.hip) with one matrix and no tile map; bias,
+// activation, residual and the rounding to the storage type sit in their epilogues, on the fp32 sums.  Where the sums of a
+// tile are cut along K, so that few tiles fill the chip, the kernel that adds the parts has the epilogue.
+//   forward   tiles of 64 x 128 to 256 x 256 by a cost model fitted to measurements, the last round cut along K; up to 64 rows the
+//             weights are streamed (HBM), beyond that the matrix cores bound it
+//   backward  dz = dy act'(pre) and its column sums in one pass (HBM); dx = dz W^T as the forward; dW = x^T dz on tiles of 256 x 256 or
+//             128 x 128, the tokens cut into segments where the gradient has few tiles, whose sums a last pass adds up
+#include "gemm.h"
 #include "linear.h"
 #include "pack8.h"
 #include <algorithm>
@@ -16,62 +15,82 @@
 namespace moe {
 
 int launch_linear_f32(int mode, int epi, bool chain, const GemmArgs& g, hipStream_t s);   // gemm_f32.hip
+int linear_forward_bf16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);   // linear_bf16.hip
+int linear_input_grad_bf16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);
+int linear_weight_grad_bf16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s);
+int linear_forward_f16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);    // linear_f16.hip
+int linear_input_grad_f16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);
+int linear_weight_grad_f16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s);
+
+constexpr int K_STAGE = 64;   // K values per stage of the 16-bit kernels
 
 // ---- how a product is cut ------------------------------------------------------------------------------------------
-// Tiles of the last round of 256 are cut along K as tail_split does, by the same model (tenths of a microsecond: a round takes
-// K / 4, a slot 1, the adding launch 20), but of any K: here the host knows the number of tiles.
-constexpr int PART_STAGES = 4;   // K stages of 64 that a part has at least
-static RowCut cut_rows(long long T, int N, int K, bool dual, int stages_of) {
-  RowCut c;
-  c.tile_rows = T <= MID_AVERAGE_FEW ? MID_ROWS : 256;   // the line of mid_applies for one expert
-  const int bn = dual ? 128 : 256;
-  c.tiles = (T + c.tile_rows - 1) / c.tile_rows * ((N + bn - 1) / bn);
-  c.first = c.tiles;
-  c.parts = 1;
-  const int r = (int)(c.tiles % TAIL_SLOTS), round = stages_of * 16;
-  int best = round - 20;
-  for (int p = 2; r > 0 && p <= TAIL_MAX_PARTS && p * r <= TAIL_SLOTS && stages_of >= p * PART_STAGES; ++p)
-    if (round / p + p * r < best) { best = round / p + p * r; c.parts = p; }
-  if (c.parts > 1) c.first = c.tiles - r;
-  (void)K;
-  return c;
-}
-static size_t cut_bytes(const RowCut& c) { return (size_t)(c.tiles - c.first) * c.parts * c.tile_rows * 256 * 4; }
-
-// Few rows: K parts per 128-column tile so that two blocks per compute unit are on their way
-static int skinny_parts(int N, int K) {
-  const int tiles = (N + SKINNY_BN - 1) / SKINNY_BN, stages = K / BKT;
-  return std::max(1, std::min({512 / tiles, stages / 2, 16}));
-}
-
-// Segments of the tokens for the weight gradient.  16-bit: rounds of 256 tiles of 26 us per 1024 tokens against writing and
-// reading the segments' sums at about 4 TB/s.  A segment stays below 4 GiB of either operand (32-bit offsets).
-static int dw_segments(const moe_linear* c, int mats) {
-  const long long T = c->T;
-  const bool half = c->dtype != MOE_DTYPE_F32;
-  const long long out = (long long)c->d_in * c->d_out * mats;
-  const long long row_bytes = (long long)std::max(c->d_in, c->d_out) * (half ? 2 : 4);
-  const int least = (int)((T * row_bytes) / 0xf0000000ll) + 1;
-  long long tiles, slots;
-  double per_row;   // us of a round per token
-  if (half) {
-    tiles = (long long)((c->d_in + 255) / 256) * ((c->d_out + 255) / 256) * mats;
-    slots = 256;
-    per_row = 26.0 / 1024;
-  } else {
-    tiles = (long long)((c->d_in + 63) / 64) * ((c->d_out + 63) / 64) * mats;
-    slots = F32_LOW_TILES;
-    per_row = 0.06;
+// A tile shape of the 16-bit products: rows and columns (two matrices: of both together), how many tiles run at a time, and what a
+// round of them takes, us: `fixed` in front of and behind the K loop, and per 64 K values `alone` where few tiles run and `full` where
+// all do (tiles of 64 x 128: `alone` up to one on every compute unit, `full` with two).  Launch: 2 us.  Fitted to T x d x n:
+//   one matrix    1024 x 1024 x 1024: 24.5 | 17.6 | 15.6 | 9.2 us in the order below;   300 x 4096 x 4096: 73 | 49 | 43 | 22;
+//                 8192 x 4096 x 1024: 78 | 56 | 55 | 74;   8192 x 1024 x 4096: 58 | 73 | 64 | 91;   8192 x 2048 x 8192: 200 | 229 | 239 | 312
+//   two           1024 x 1024 x 2048: 25.7 | 17.8 | 15.6 | 13.7;   4096 x 2048 x 4096: 101 | 125 | 111 | 157;   8192 x 2048 x 8192: 409 | 440 | 451 | 607
+//   x^T dz        2048 x 1024 x 1024: 43 | 17;   8192 x 1024 x 4096: 143 | 63;   4096 x 2048 x 4096: 76 | 65;   4096 x 2048 x 8192: 96 | 128
+// Few rows, weights that come from memory, parts as chosen: 1 x 4096 x 14336 (two) 41.5 us, 16 x 14336 x 4096 24.5: 5.7 and 4.8 TB/s.
+struct Shape {
+  int rows, cols, slots;
+  double fixed, alone, full;
+  double tiles_us(long long tiles, int stages) const {   // whole rounds of them, and the rest
+    const long long r = tiles % slots, rounds = tiles / slots;
+    double us = rounds * (fixed + stages * full);
+    if (r > 0) us += fixed + stages * (slots > 256 ? (r <= 256 ? alone : full) : alone + (full - alone) * r / slots);
+    return us;
   }
-  int best = least;
-  double cost = 1e30;
-  for (int s = least; s <= std::max(least, 16) && (s == least || T / s >= 256); ++s) {
-    const double rounds = (double)((tiles * s + slots - 1) / slots);
-    double us = rounds * per_row * (double)((T + s - 1) / s);
-    if (s > 1) us += 3.0 + (double)out * 4 * s * 2 / 4e6;
-    if (us < cost * 0.97) { cost = us; best = s; }
+};
+constexpr Shape SHAPES[] = {{256, 256, 256, 6.5, 1.0, 1.37}, {160, 256, 256, 5.0, 0.65, 0.91}, {128, 256, 256, 4.2, 0.58, 0.78}, {64, 128, 512, 2.5, 0.28, 0.54}};
+constexpr Shape SHAPES_DUAL[] = {{256, 256, 256, 6.5, 1.07, 1.37}, {160, 256, 256, 5.5, 0.62, 0.86}, {128, 256, 256, 4.2, 0.6, 0.73}, {64, 256, 256, 3.3, 0.38, 0.5}};
+constexpr Shape SHAPES_DW[] = {{256, 256, 256, 6.5, 1.05, 1.42}, {128, 128, 256, 3.5, 0.34, 0.44}};
+constexpr double JOIN_US = 3.0, JOIN_US_PER_MB = 0.35;   // the adding launch; fp32 sums written and read again
+constexpr int PART_STAGES = 4, MAX_PARTS = 16;   // K stages of 64 that a part has at least; parts at most
+
+// How `stages` K stages of T x N sums are cut: the shape, and the K parts of its last round, that take the least time.
+static RowCut cut_rows(long long T, int N, bool dual, int stages) {
+  RowCut best{};
+  double least = 1e30;
+  for (const Shape& s : dual ? SHAPES_DUAL : SHAPES) {
+    RowCut c;
+    c.rows = s.rows;
+    c.cols = dual ? s.cols / 2 : s.cols;
+    c.tiles = (T + c.rows - 1) / c.rows * ((N + c.cols - 1) / c.cols);
+    const long long r = c.tiles % s.slots;
+    for (int p = 1; p <= MAX_PARTS; ++p) {
+      if (p > 1 && (r == 0 || p * r > s.slots || stages < p * PART_STAGES)) break;
+      double us = s.tiles_us(c.tiles - r, stages) + s.tiles_us(r * p, (stages + p - 1) / p);
+      if (p > 1) us += JOIN_US + JOIN_US_PER_MB * (double)r * p * s.rows * s.cols * 4 / 1e6;
+      c.parts = p;
+      c.first = p > 1 ? c.tiles - r : c.tiles;
+      if (us < least) { least = us; best = c; }
+    }
   }
   return best;
+}
+static size_t cut_bytes(const RowCut& c, int mats) { return (size_t)(c.tiles - c.first) * c.parts * c.rows * c.cols * mats * 4; }
+
+// Tiles of the weight gradient and segments of the tokens: the least time, the segments' sums counted as above.  A segment stays
+// below 4 GiB of either operand (32-bit offsets).  fp32: 64 x 64 tiles, three on a compute unit, 2 us per 32 tokens.
+static void cut_weight_grad(const moe_linear* c, int mats, LinearPlan& p) {
+  const long long T = c->T;
+  const bool half = c->dtype != MOE_DTYPE_F32;
+  const double out_mb = (double)c->d_in * c->d_out * mats * 4 / 1e6;
+  const long long row_bytes = (long long)std::max(c->d_in, c->d_out) * (half ? 2 : 4);
+  const int first = (int)((T * row_bytes) / 0xf0000000ll) + 1;
+  double least = 1e30;
+  auto tiles_of = [&](int rows) { return (long long)((c->d_in + rows - 1) / rows) * ((c->d_out + rows - 1) / rows) * mats; };
+  auto consider = [&](int rows, int segs, double us) {
+    if (segs > 1) us += JOIN_US + JOIN_US_PER_MB * out_mb * segs;
+    if (us < least) { least = us; p.dw_rows = rows; p.segs = segs; }
+  };
+  for (int segs = first; segs <= std::max(first, 16) && (segs == first || T / segs >= 256); ++segs) {
+    const long long rows = (T + segs - 1) / segs;
+    if (half) for (const Shape& s : SHAPES_DW) consider(s.rows, segs, s.tiles_us(tiles_of(s.rows) * segs, (int)((rows + K_STAGE - 1) / K_STAGE)));
+    else consider(64, segs, (double)((tiles_of(64) * segs + F32_LOW_TILES - 1) / F32_LOW_TILES) * 0.06 * rows);
+  }
 }
 static int seg_rows(long long T, int segs) { return (int)(((T + segs - 1) / segs + 63) / 64 * 64); }
 
@@ -81,13 +100,9 @@ LinearPlan linear_plan(const moe_linear* c) {
   const int mats = c->act == MOE_ACT_SWIGLU ? 2 : 1;
   const size_t es = half ? 2 : 4, T = c->T, N = c->d_out;
   size_t fwd = 0, off = 0;
-  p.skinny = half && c->T <= SKINNY_ROWS;
-  if (p.skinny) {
-    p.parts = skinny_parts(c->d_out, c->d_in);
-    fwd = (size_t)mats * p.parts * T * N * 4;
-  } else if (half) {
-    p.fwd = cut_rows(c->T, c->d_out, c->d_in, mats == 2, c->d_in / BKT);
-    fwd = cut_bytes(p.fwd);
+  if (half) {
+    p.fwd = cut_rows(c->T, c->d_out, mats == 2, c->d_in / K_STAGE);
+    fwd = cut_bytes(p.fwd, mats);
   }
   // backward
   p.dz = off;
@@ -97,11 +112,12 @@ LinearPlan linear_plan(const moe_linear* c) {
   off += align_up((size_t)mats * p.bias_geom.row_blocks * N * 4, 256);
   p.split = off;
   if (half) {
-    p.dx = cut_rows(c->T, c->d_in, c->d_out, false, mats * (c->d_out / BKT));
-    off += align_up(cut_bytes(p.dx), 256);
+    p.dx = cut_rows(c->T, c->d_in, false, mats * (c->d_out / K_STAGE));
+    off += align_up(cut_bytes(p.dx, 1), 256);
   }
   p.dw = off;
-  p.segs = c->T > 0 ? dw_segments(c, mats) : 1;
+  p.segs = 1;
+  if (c->T > 0) cut_weight_grad(c, mats, p);
   p.seg = seg_rows(c->T, p.segs);
   p.segs = c->T > 0 ? (c->T + p.seg - 1) / p.seg : 1;
   p.dw_direct = p.segs == 1;   // the product writes the gradient itself
@@ -111,92 +127,6 @@ LinearPlan linear_plan(const moe_linear* c) {
 }
 
 // ---- kernels -------------------------------------------------------------------------------------------------------
-template <typename ST, int MODE, int EPI, bool DUAL, bool CHAIN, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(WGM* WGN * 64, 1) void linear_rows_kernel(GemmArgs g) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  gemm_bf16_tile<ST, MODE, EPI, DUAL, CHAIN, BM, BN, WGM, WGN, false, false, true>(g, blockIdx.x, smem);
-}
-template <typename ST, bool DUAL>
-__global__ __launch_bounds__(256, 2) void linear_few_kernel(GemmArgs g) {
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  gemm_skinny_tile<ST, EPI_STORE, DUAL, true>(g, smem);
-}
-
-// Adds the parts of split tiles in part order and applies the epilogue; a thread owns eight adjacent columns of a row.
-// few: the layout of linear_few_kernel, every row and column; else that of the split row tiles.
-template <typename ST, int EPI>
-__global__ __launch_bounds__(256) void linear_join_kernel(GemmArgs g, int few) {
-  constexpr bool DUAL = EPI == EPI_LIN_SWIGLU;
-  const float *src, *src2;
-  size_t pitch;      // floats between the parts
-  long long row;
-  int col;
-  const int parts = g.split_parts;
-  if (few) {
-    const int per_row = g.N / 8;
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= g.M * per_row) return;
-    row = i / per_row;
-    col = (i % per_row) * 8;
-    pitch = (size_t)g.M * g.N;
-    src = g.split_ws + (size_t)row * g.N + col;
-    src2 = src + pitch * parts;
-  } else {
-    constexpr int BN = DUAL ? 128 : 256, TPR = BN / 8, RPB = 256 / TPR;   // threads per row, rows per block
-    const int per_tile = g.tile_rows / RPB;
-    const int q = blockIdx.x / per_tile, m = (blockIdx.x % per_tile) * RPB + threadIdx.x / TPR, n = (threadIdx.x % TPR) * 8;
-    int rt, nt;
-    if (!block_to_tile(g.split_first + q, (g.M + g.tile_rows - 1) / g.tile_rows, g.M / g.tile_rows, (g.N + BN - 1) / BN, g.chunked != 0, rt, nt)) return;
-    row = (long long)rt * g.tile_rows + m;
-    col = nt * BN + n;
-    if (row >= g.M || col >= g.N) return;
-    pitch = (size_t)g.tile_rows * 256;
-    src = g.split_ws + (size_t)q * parts * pitch + m * BN + n;
-    src2 = src + (size_t)g.tile_rows * BN;
-  }
-  float z[8] = {}, z2[8] = {};
-  for (int p = 0; p < parts; ++p) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(src + p * pitch + 4 * h);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[4 * h + i] += v[i];
-      if constexpr (DUAL) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(src2 + p * pitch + 4 * h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z2[4 * h + i] += w[i];
-      }
-    }
-  }
-  const size_t at = (size_t)row * g.N + col;
-  Vec16<ST> q;
-  float f[8];
-  auto add = [&](const void* p, size_t off, float (&to)[8]) {
-    if (p == nullptr) return;
-    q.load(reinterpret_cast<const ST*>(p) + off);
-    q.unpack(f);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) to[i] += f[i];
-  };
-  auto put = [&](void* p, const float (&v)[8]) {
-    q.pack(v);
-    q.store(reinterpret_cast<ST*>(p) + at);
-  };
-  add(g.bias, col, z);
-  if (EPI != EPI_LIN_NONE && g.C != nullptr) put(g.C, z);
-  if constexpr (DUAL) {
-    add(g.bias2, col, z2);
-    if (g.C != nullptr) put(g.C2, z2);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = z[i] * sigmoid_fast(z[i]) * z2[i];
-  } else if constexpr (EPI == EPI_LIN_GELU) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = z[i] * phi_fast(z[i]);
-  }
-  add(g.S1, at, z);
-  put(g.C3, z);
-}
-
 // dz = dy act'(pre), rounded to the storage type, and the column sums of the unrounded dz, one row of partial sums per block.
 // A thread owns eight adjacent columns and walks down the rows of its block; cg threads span a block's columns.
 struct ActBwdArgs {
@@ -264,7 +194,7 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           if constexpr (DUAL) {
-            const float sg = sizeof(ST) == 4 ? sigmoid_f(z[u][i]) : sigmoid_fast(z[u][i]);
+            const float sg = sizeof(ST) == 4 ? sigmoid_f(z[u][i]) : __builtin_amdgcn_rcpf(1.f + __expf(-z[u][i]));
             g[i] = dy[u][i] * z2[u][i] * sg * fmaf(z[u][i], 1.f - sg, 1.f);
             g2[i] = dy[u][i] * z[u][i] * sg;
             sum2[i] += g2[i];
@@ -351,68 +281,6 @@ __global__ void linear_zero_kernel(uint32_t* p, size_t n) {
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
-template <typename K>
-static int more_lds(K kern, int lds) {   // above 64 KB, on every launch: nothing is remembered
-  const hipError_t err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  return err == hipSuccess ? MOE_OK : set_hip_error(err);
-}
-
-template <typename ST, int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
-static int launch_rows_bm(const GemmArgs& g, long long tiles, hipStream_t s) {
-  constexpr int BN = DUAL ? 128 : 256, WGM = DUAL && BM == 256 ? 4 : 2;
-  constexpr int lds = gemm_bf16_lds_bytes<BM, BN, DUAL>();
-  auto kern = linear_rows_kernel<ST, MODE, EPI, DUAL, CHAIN, BM, BN, WGM, 8 / WGM>;
-  const int rc = more_lds(kern, lds);
-  if (rc != MOE_OK) return rc;
-  const long long blocks = MODE == MODE_TN ? dw_blocks(g, BM, BN) : g.split_first + (tiles - g.split_first) * g.split_parts;
-  if (blocks > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
-  kern<<<dim3((unsigned)blocks), 512, lds, s>>>(g);
-  return launch_status();
-}
-template <typename ST, int EPI>
-static int launch_join(const GemmArgs& g, long long blocks, int few, hipStream_t s) {
-  linear_join_kernel<ST, EPI><<<dim3((unsigned)blocks), 256, 0, s>>>(g, few);
-  return launch_status();
-}
-template <typename ST, int MODE, int EPI, bool CHAIN>
-static int launch_rows(GemmArgs g, const RowCut& cut, float* split_ws, hipStream_t s) {
-  constexpr bool DUAL = EPI == EPI_LIN_SWIGLU;
-  constexpr int BN = DUAL ? 128 : 256;
-  if (cut.tiles > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
-  g.tile_rows = cut.tile_rows;
-  g.split_first = (int)cut.first;
-  g.split_parts = cut.parts;
-  g.split_ws = split_ws;
-  int rc = cut.tile_rows == MID_ROWS ? launch_rows_bm<ST, MODE, EPI, DUAL, CHAIN, MID_ROWS>(g, cut.tiles, s)
-                                     : launch_rows_bm<ST, MODE, EPI, DUAL, CHAIN, 256>(g, cut.tiles, s);
-  if (rc != MOE_OK || cut.parts == 1) return rc;
-  return launch_join<ST, EPI>(g, (cut.tiles - cut.first) * (cut.tile_rows * BN / 8 / 256), 0, s);
-}
-template <typename ST, int EPI>
-static int launch_few(GemmArgs g, int parts, float* split_ws, hipStream_t s) {
-  constexpr bool DUAL = EPI == EPI_LIN_SWIGLU;
-  constexpr int lds = skinny_stages<DUAL>() * skinny_stage_bytes<DUAL>();
-  auto kern = linear_few_kernel<ST, DUAL>;
-  const int rc = more_lds(kern, lds);
-  if (rc != MOE_OK) return rc;
-  g.split_parts = parts;
-  g.split_ws = split_ws;
-  kern<<<dim3((unsigned)((g.N + SKINNY_BN - 1) / SKINNY_BN * parts)), 256, lds, s>>>(g);
-  const int rc2 = launch_status();
-  if (rc2 != MOE_OK) return rc2;
-  return launch_join<ST, EPI>(g, ((long long)g.M * (g.N / 8) + 255) / 256, 1, s);
-}
-template <typename ST, int EPI>
-static int fwd_half(const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s) {
-  return p.skinny ? launch_few<ST, EPI>(g, p.parts, ws, s) : launch_rows<ST, MODE_NN, EPI, false>(g, p.fwd, ws, s);
-}
-template <typename ST>
-static int fwd_half_act(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s) {
-  return act == MOE_ACT_SWIGLU ? fwd_half<ST, EPI_LIN_SWIGLU>(g, p, ws, s)
-         : act == MOE_ACT_GELU ? fwd_half<ST, EPI_LIN_GELU>(g, p, ws, s)
-                               : fwd_half<ST, EPI_LIN_NONE>(g, p, ws, s);
-}
-
 int launch_linear_fwd(const moe_linear* c, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,
                       const void* residual, void* pre, void* pre_b, void* y, void* ws, hipStream_t s) {
   const LinearPlan p = linear_plan(c);
@@ -422,7 +290,7 @@ int launch_linear_fwd(const moe_linear* c, const void* x, const void* W, const v
   g.chunked = row_tiles_chunked(c->T, c->d_in, c->d_out, 1, Wb != nullptr ? 2 : 1, c->dtype == MOE_DTYPE_F32 ? 4 : 2);
   if (c->dtype == MOE_DTYPE_F32)
     return launch_linear_f32(MODE_NN, c->act == MOE_ACT_SWIGLU ? EPI_LIN_SWIGLU : c->act == MOE_ACT_GELU ? EPI_LIN_GELU : EPI_LIN_NONE, false, g, s);
-  return c->dtype == MOE_DTYPE_F16 ? fwd_half_act<f16>(c->act, g, p, (float*)ws, s) : fwd_half_act<bf16>(c->act, g, p, (float*)ws, s);
+  return c->dtype == MOE_DTYPE_F16 ? linear_forward_f16(c->act, g, p, (float*)ws, s) : linear_forward_bf16(c->act, g, p, (float*)ws, s);
 }
 
 template <typename ST, int ACT>
@@ -502,10 +370,7 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
     g.chunked = row_tiles_chunked(c->T, N, d, 1, mats, (int)es);
     float* split = reinterpret_cast<float*>(w + p.split);
     if (es == 4) TRY(launch_linear_f32(MODE_NT, EPI_LIN_NONE, mats == 2, g, s));
-    else if (c->dtype == MOE_DTYPE_F16)
-      TRY(mats == 2 ? (launch_rows<f16, MODE_NT, EPI_LIN_NONE, true>(g, p.dx, split, s)) : (launch_rows<f16, MODE_NT, EPI_LIN_NONE, false>(g, p.dx, split, s)));
-    else
-      TRY(mats == 2 ? (launch_rows<bf16, MODE_NT, EPI_LIN_NONE, true>(g, p.dx, split, s)) : (launch_rows<bf16, MODE_NT, EPI_LIN_NONE, false>(g, p.dx, split, s)));
+    else TRY(c->dtype == MOE_DTYPE_F16 ? linear_input_grad_f16(mats == 2, g, p, split, s) : linear_input_grad_bf16(mats == 2, g, p, split, s));
   }
   if (dW == nullptr) return MOE_OK;
   // dW = x^T dz, dWb = x^T dz2: both in one launch
@@ -518,11 +383,10 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
   g.M = d; g.N = N; g.K = c->T; g.E = p.segs; g.seg = p.seg;
   g.accumulate = p.dw_direct && accumulate;
   if (es == 4) TRY(launch_linear_f32(MODE_TN, EPI_DW, false, g, s));
-  else if (p.dw_direct && c->grad != MOE_DTYPE_F32)
-    TRY(c->dtype == MOE_DTYPE_F16 ? (launch_rows_bm<f16, MODE_TN, EPI_LIN_NONE, false, false, 256>(g, 0, s))
-                                  : (launch_rows_bm<bf16, MODE_TN, EPI_LIN_NONE, false, false, 256>(g, 0, s)));
-  else if (c->dtype == MOE_DTYPE_F16) TRY((launch_rows_bm<f16, MODE_TN, EPI_DW, false, false, 256>(g, 0, s)));
-  else TRY((launch_rows_bm<bf16, MODE_TN, EPI_DW, false, false, 256>(g, 0, s)));
+  else {
+    const bool in_type = p.dw_direct && c->grad != MOE_DTYPE_F32;
+    TRY(c->dtype == MOE_DTYPE_F16 ? linear_weight_grad_f16(in_type, g, p, s) : linear_weight_grad_bf16(in_type, g, p, s));
+  }
   if (p.dw_direct) return MOE_OK;
   const JoinArgs j = {{sums, sums + out * p.segs}, {dW, dWb}, out, p.segs, accumulate};
   return launch_sum_rows(j, mats, c->grad, false, s);

@@ -1,0 +1,10 @@
+// The dense products' kernels with bf16 storage (linear_half.h).
+#include "linear_half.h"
+
+namespace moe {
+
+int linear_forward_bf16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s) { return LinearHalf<bf16>::forward(act, g, p, ws, s); }
+int linear_input_grad_bf16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s) { return LinearHalf<bf16>::input_grad(two, g, p, ws, s); }
+int linear_weight_grad_bf16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s) { return LinearHalf<bf16>::weight_grad(in_type, g, p, s); }
+
+}  // namespace moe
