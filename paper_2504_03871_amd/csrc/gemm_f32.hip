@@ -128,6 +128,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), band = wave % BANDS, kh = wave / BANDS;
   const int ntn = (g.N + SB - 1) / SB;
   int e, row0, mvalid, klen, m0 = 0, nt;
+  int part = 0;   // DENSE row tiles: which K part of the tile
   bool second_grad = false;
   if constexpr (MODE == MODE_TN) {
     int slot, mt;
@@ -150,7 +151,8 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
     RowBlock rb;
     RowTile t;
     if constexpr (DENSE) {
-      if (!row_tile_block(vb, (g.M + BM - 1) / BM, g.M / BM, 0, ntn, false, rb)) return;
+      part = vb % g.split_parts;
+      if (!row_tile_block(vb / g.split_parts, (g.M + BM - 1) / BM, g.M / BM, 0, ntn, false, rb)) return;
       t = RowTile{0, rb.rt * BM, min(BM, g.M - rb.rt * BM), 0};
     } else {
       if (!row_tile_block(vb, g.ntiles[0], g.ntiles[1], 0, ntn, false, rb)) return;
@@ -186,7 +188,12 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   const rsrc_t rb = make_rsrc(reinterpret_cast<const float*>(second_grad ? g.B2 : g.B) + boff, bbytes);
   const rsrc_t ra2 = make_rsrc(reinterpret_cast<const float*>(CHAIN ? g.A2 : g.A) + aoff, abytes);
   const rsrc_t rb2 = make_rsrc(reinterpret_cast<const float*>(CHAIN || DUAL ? g.B2 : g.B) + boff, bbytes);
-  const int KT1 = (klen + SK - 1) / SK, KT = CHAIN ? 2 * KT1 : KT1;   // a chained GEMM runs its two operand pairs back to back
+  const int KT1 = (klen + SK - 1) / SK;
+  int KT = CHAIN ? 2 * KT1 : KT1, skip = 0;   // a chained GEMM runs its two operand pairs back to back
+  if constexpr (DENSE && MODE != MODE_TN) {
+    skip = part * KT / g.split_parts;
+    KT = (part + 1) * KT / g.split_parts - skip;
+  }
   unsigned a_vo[CHA], b_vo[CHB];
   int a_k[CHA], b_k[CHB];
 #pragma unroll
@@ -195,6 +202,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   for (int i = 0; i < CHB; ++i) f32_chunk<B_KC, true, SB>(tid + 256 * i, pb, b_vo[i], b_k[i]);
   const unsigned lds0 = lds_addr(smem) + wave * 1024;   // a wave's load fills 1 KB of the tile
   auto load_stage = [&](int kt, int buf) {
+    kt += skip;
     const bool second = CHAIN && kt >= KT1;
     const unsigned kl = second ? kt - KT1 : kt;
     const int left = klen - (int)kl * SK;   // K values from this stage on; chunks past them must read as zero in both operands
@@ -280,6 +288,19 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmArgs& g, const int vb, c
   }
   if (!active || n0 + c * 4 >= g.N) return;
   // accumulator register v of a lane: row 4 grp + v of the wave's 16, one column of each of the four column tiles
+  if constexpr (DENSE && MODE != MODE_TN) {
+    if (g.split_parts > 1) {   // sums of a K part: [matrix][part][row][column]
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int m = band * 16 + grp * 4 + v;
+        if (m >= mvalid) break;
+        float* to = g.split_ws + ((size_t)part * g.M + row0 + m) * g.N + n0 + c * 4;
+        *reinterpret_cast<f32x4*>(to) = f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]};
+        if constexpr (DUAL) *reinterpret_cast<f32x4*>(to + (size_t)g.split_parts * g.M * g.N) = f32x4{acc2[0][v], acc2[1][v], acc2[2][v], acc2[3][v]};
+      }
+      return;
+    }
+  }
   size_t idx[4];
   f32x4 s1[4], s2[4], bias = {0.f, 0.f, 0.f, 0.f}, bias2 = {0.f, 0.f, 0.f, 0.f};
   if constexpr (EPI >= EPI_LIN_NONE) {
@@ -350,32 +371,83 @@ int launch_gemm_f32(int mode, int epi, bool dual, bool chain, const GemmArgs& g,
   return MOE_ERR_BAD_DTYPE;
 }
 
-// Dense products (linear.hip): g.M rows, or weight gradients over g.E segments of g.seg rows.
+// ---- dense products (linear.hip): g.M rows in tiles of g.tile_rows, g.split_parts K parts each; weight gradients over g.E segments
+// of g.seg rows in tiles of g.tile_rows ----
 template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
 __global__ __launch_bounds__(256, BM == SB ? 3 : 4) void linear_f32_kernel(GemmArgs g) {
   __shared__ __attribute__((aligned(1024))) char smem[f32_lds_bytes<DUAL, BM>()];
   gemm_f32_tile<MODE, EPI, DUAL, CHAIN, BM, true>(g, blockIdx.x, smem);
 }
-template <int MODE, int EPI, bool DUAL, bool CHAIN, int BM>
-static int launch_linear_bm(const GemmArgs& g, hipStream_t s) {
-  const long long ntn = (g.N + SB - 1) / SB, blocks = MODE == MODE_TN ? dw_blocks(g, BM, SB) : ntn * ((g.M + BM - 1) / BM);
-  if (blocks > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
-  linear_f32_kernel<MODE, EPI, DUAL, CHAIN, BM><<<dim3((unsigned)blocks), 256, 0, s>>>(g);
-  return launch_status();
+// the input's gradient and the weights' in one launch, which small problems fill the chip with
+template <bool CHAIN1, int BM1, int BM2>
+__global__ __launch_bounds__(256, BM1 == SB || BM2 == SB ? 3 : 4) void linear_f32_pair_kernel(GemmArgs g1, GemmArgs g2, int first_blocks) {
+  constexpr int lds1 = f32_lds_bytes<false, BM1>(), lds2 = f32_lds_bytes<false, BM2>();
+  __shared__ __attribute__((aligned(1024))) char smem[lds1 > lds2 ? lds1 : lds2];
+  if ((int)blockIdx.x < first_blocks) gemm_f32_tile<MODE_NT, EPI_LIN_NONE, false, CHAIN1, BM1, true>(g1, blockIdx.x, smem);
+  else gemm_f32_tile<MODE_TN, EPI_DW, false, false, BM2, true>(g2, blockIdx.x - first_blocks, smem);
 }
+// Adds the K parts in order and applies the epilogue; a thread owns four adjacent columns of a row.
+template <int EPI>
+__global__ __launch_bounds__(256) void linear_f32_join_kernel(GemmArgs g) {
+  constexpr bool DUAL = EPI == EPI_LIN_SWIGLU;
+  const size_t n = (size_t)g.M * g.N, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  const int col = (int)(i % g.N);
+  auto at = [&](const void* p, size_t o) { return p != nullptr ? *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(p) + o) : f32x4{0.f, 0.f, 0.f, 0.f}; };
+  const f32x4 res = at(g.S1, i), b = at(g.bias, col), b2 = at(DUAL ? g.bias2 : nullptr, col);
+  f32x4 z = {0.f, 0.f, 0.f, 0.f}, z2 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < g.split_parts; ++p) {
+    z += *reinterpret_cast<const f32x4*>(g.split_ws + p * n + i);
+    if constexpr (DUAL) z2 += *reinterpret_cast<const f32x4*>(g.split_ws + (p + g.split_parts) * n + i);
+  }
+  epilogue_f32x4<EPI>(g, i, z, z2, res, f32x4{}, false, b, b2);
+}
+static long long linear_row_blocks(const GemmArgs& g) { return (long long)((g.N + SB - 1) / SB) * ((g.M + g.tile_rows - 1) / g.tile_rows) * g.split_parts; }
 template <int MODE, int EPI, bool DUAL, bool CHAIN>
 static int launch_linear_rows(const GemmArgs& g, hipStream_t s) {
-  const int rows = MODE == MODE_TN ? dw_tile_rows(g) : f32_tile_rows(g.M, 0, g.N);
-  return rows == SB ? launch_linear_bm<MODE, EPI, DUAL, CHAIN, SB>(g, s) : launch_linear_bm<MODE, EPI, DUAL, CHAIN, SB / 2>(g, s);
+  const long long blocks = MODE == MODE_TN ? dw_blocks(g, g.tile_rows, SB) : linear_row_blocks(g);
+  if (blocks > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
+  if (g.tile_rows == SB) linear_f32_kernel<MODE, EPI, DUAL, CHAIN, SB><<<dim3((unsigned)blocks), 256, 0, s>>>(g);
+  else linear_f32_kernel<MODE, EPI, DUAL, CHAIN, SB / 2><<<dim3((unsigned)blocks), 256, 0, s>>>(g);
+  return launch_status();
 }
-int launch_linear_f32(int mode, int epi, bool chain, const GemmArgs& g, hipStream_t s) {
-  if (mode == MODE_NN && epi == EPI_LIN_NONE) return launch_linear_rows<MODE_NN, EPI_LIN_NONE, false, false>(g, s);
-  if (mode == MODE_NN && epi == EPI_LIN_GELU) return launch_linear_rows<MODE_NN, EPI_LIN_GELU, false, false>(g, s);
-  if (mode == MODE_NN && epi == EPI_LIN_SWIGLU) return launch_linear_rows<MODE_NN, EPI_LIN_SWIGLU, true, false>(g, s);
-  if (mode == MODE_NT && chain) return launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, true>(g, s);
-  if (mode == MODE_NT) return launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, false>(g, s);
-  if (mode == MODE_TN) return launch_linear_rows<MODE_TN, EPI_DW, false, false>(g, s);
-  return MOE_ERR_BAD_DTYPE;
+template <int EPI>
+static int launch_linear_join(const GemmArgs& g, hipStream_t s) {
+  if (g.split_parts == 1) return MOE_OK;
+  linear_f32_join_kernel<EPI><<<dim3((unsigned)(((size_t)g.M * g.N / 4 + 255) / 256)), 256, 0, s>>>(g);
+  return launch_status();
+}
+template <int EPI>
+static int linear_f32_forward_for(const GemmArgs& g, hipStream_t s) {
+  const int rc = launch_linear_rows<MODE_NN, EPI, EPI == EPI_LIN_SWIGLU, false>(g, s);
+  return rc != MOE_OK ? rc : launch_linear_join<EPI>(g, s);
+}
+int linear_forward_f32(int act, const GemmArgs& g, hipStream_t s) {
+  return act == MOE_ACT_SWIGLU ? linear_f32_forward_for<EPI_LIN_SWIGLU>(g, s)
+         : act == MOE_ACT_GELU ? linear_f32_forward_for<EPI_LIN_GELU>(g, s)
+                               : linear_f32_forward_for<EPI_LIN_NONE>(g, s);
+}
+template <bool CHAIN1, int BM1, int BM2>
+static int launch_linear_pair(const GemmArgs& g1, const GemmArgs& g2, hipStream_t s) {
+  // a multiple of the XCD count: a tile number still tells the XCD for the second product
+  const long long n1 = (linear_row_blocks(g1) + NUM_XCD - 1) / NUM_XCD * NUM_XCD, n2 = dw_blocks(g2, BM2, SB);
+  if (n1 + n2 > 0x7fffffffll) return MOE_ERR_BAD_SHAPE;
+  linear_f32_pair_kernel<CHAIN1, BM1, BM2><<<dim3((unsigned)(n1 + n2)), 256, 0, s>>>(g1, g2, (int)n1);
+  return launch_status();
+}
+template <bool CHAIN1>
+static int linear_f32_pair_for(const GemmArgs& g1, const GemmArgs& g2, hipStream_t s) {
+  if (g1.tile_rows == SB) return g2.tile_rows == SB ? launch_linear_pair<CHAIN1, SB, SB>(g1, g2, s) : launch_linear_pair<CHAIN1, SB, SB / 2>(g1, g2, s);
+  return g2.tile_rows == SB ? launch_linear_pair<CHAIN1, SB / 2, SB>(g1, g2, s) : launch_linear_pair<CHAIN1, SB / 2, SB / 2>(g1, g2, s);
+}
+// dx (g1 with C3) and the weight gradients (g2 with C), either or both
+int linear_backward_f32(bool two, const GemmArgs& g1, const GemmArgs& g2, hipStream_t s) {
+  int rc;
+  if (g1.C3 != nullptr && g2.C != nullptr) rc = two ? linear_f32_pair_for<true>(g1, g2, s) : linear_f32_pair_for<false>(g1, g2, s);
+  else if (g1.C3 != nullptr) rc = two ? launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, true>(g1, s) : launch_linear_rows<MODE_NT, EPI_LIN_NONE, false, false>(g1, s);
+  else rc = launch_linear_rows<MODE_TN, EPI_DW, false, false>(g2, s);
+  return rc != MOE_OK || g1.C3 == nullptr ? rc : launch_linear_join<EPI_LIN_NONE>(g1, s);
 }
 
 template <int EPI1, bool CHAIN1, int BM1, int BM2>

@@ -26,6 +26,14 @@ inline BiasGeom bias_geom(long long T, int N) {
   return g;
 }
 
+// Few rows whose column sums are wanted: a block takes all rows of 8 to 32 columns, in at most four steps, and writes the sums
+// itself, without a launch that adds up partial ones.  Up to a million values: its pieces of a row are short.
+inline bool bias_few(long long T, int N) { return T <= 1024 && T * N <= 1 << 20; }
+inline BiasGeom bias_geom_few(long long T, int N) {
+  const int cg = T <= 128 ? 4 : T <= 256 ? 2 : 1;
+  return BiasGeom{cg, (int)T, ((N + 7) / 8 + cg - 1) / cg, 1};
+}
+
 struct LinearPlan {
   RowCut fwd, dx;
   BiasGeom bias_geom;

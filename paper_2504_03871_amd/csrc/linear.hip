@@ -14,7 +14,8 @@
 
 namespace moe {
 
-int launch_linear_f32(int mode, int epi, bool chain, const GemmArgs& g, hipStream_t s);   // gemm_f32.hip
+int linear_forward_f32(int act, const GemmArgs& g, hipStream_t s);   // gemm_f32.hip
+int linear_backward_f32(bool two, const GemmArgs& g1, const GemmArgs& g2, hipStream_t s);
 int linear_forward_bf16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);   // linear_bf16.hip
 int linear_input_grad_bf16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);
 int linear_weight_grad_bf16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s);
@@ -43,10 +44,10 @@ struct Shape {
     return us;
   }
 };
-constexpr Shape SHAPES[] = {{256, 256, 256, 6.5, 1.0, 1.37}, {160, 256, 256, 5.0, 0.65, 0.91}, {128, 256, 256, 4.2, 0.58, 0.78}, {64, 128, 512, 2.5, 0.28, 0.54}};
+constexpr Shape SHAPES[] = {{256, 256, 256, 6.5, 1.0, 1.37}, {160, 256, 256, 5.0, 0.65, 0.91}, {128, 256, 256, 4.2, 0.58, 0.79}, {64, 128, 512, 2.5, 0.28, 0.54}};
 constexpr Shape SHAPES_DUAL[] = {{256, 256, 256, 6.5, 1.07, 1.37}, {160, 256, 256, 5.5, 0.62, 0.86}, {128, 256, 256, 4.2, 0.6, 0.73}, {64, 256, 256, 3.3, 0.38, 0.5}};
 constexpr Shape SHAPES_DW[] = {{256, 256, 256, 6.5, 1.05, 1.42}, {128, 128, 256, 3.5, 0.34, 0.44}};
-constexpr double JOIN_US = 3.0, JOIN_US_PER_MB = 0.35;   // the adding launch; fp32 sums written and read again
+constexpr double JOIN_US = 3.0, JOIN_US_PER_MB = 0.28;   // the adding launch; fp32 sums written and read again
 constexpr int PART_STAGES = 4, MAX_PARTS = 16;   // K stages of 64 that a part has at least; parts at most
 
 // How `stages` K stages of T x N sums are cut: the shape, and the K parts of its last round, that take the least time.
@@ -70,6 +71,29 @@ static RowCut cut_rows(long long T, int N, bool dual, int stages) {
   }
   return best;
 }
+// fp32: tiles of 64 or 32 rows (f32_tile_rows) and 64 columns in K stages of 32, every tile cut into `parts`.  A stage takes the matrix
+// cores 0.43 | 0.21 us of a compute unit per tile and at least 0.4 us, the way of its loads.  300 rows, K 1540, 516 columns: 90
+// tiles in one part 23.4 us.
+static RowCut cut_rows_f32(long long T, int N, int mats, int stages) {
+  RowCut best{};
+  double least = 1e30;
+  for (int p = 1; p <= MAX_PARTS && (p == 1 || stages >= 4 * p); ++p) {
+    RowCut c;
+    c.rows = f32_tile_rows(T * p, 0, N);
+    c.cols = F32_TILE_COLS;
+    c.parts = p;
+    c.first = 0;
+    c.tiles = (T + c.rows - 1) / c.rows * ((N + c.cols - 1) / c.cols);
+    const double stage = std::max(0.4, (c.rows == 64 ? 0.43 : 0.21) * mats * c.tiles * p / 256);
+    double us = (stages + p - 1) / p * stage;
+    if (p > 1) us += JOIN_US + JOIN_US_PER_MB * (double)T * N * 4 * p * mats / 1e6;
+    if (us < least) { least = us; best = c; }
+  }
+  return best;
+}
+static size_t cut_bytes_f32(const RowCut& c, long long T, int N, int mats) { return c.parts > 1 ? (size_t)T * N * 4 * c.parts * mats : 0; }
+constexpr int K_STAGE_F32 = 32;
+
 static size_t cut_bytes(const RowCut& c, int mats) { return (size_t)(c.tiles - c.first) * c.parts * c.rows * c.cols * mats * 4; }
 
 // Tiles of the weight gradient and segments of the tokens: the least time, the segments' sums counted as above.  A segment stays
@@ -103,6 +127,9 @@ LinearPlan linear_plan(const moe_linear* c) {
   if (half) {
     p.fwd = cut_rows(c->T, c->d_out, mats == 2, c->d_in / K_STAGE);
     fwd = cut_bytes(p.fwd, mats);
+  } else {
+    p.fwd = cut_rows_f32(c->T, c->d_out, mats, (c->d_in + K_STAGE_F32 - 1) / K_STAGE_F32);
+    fwd = cut_bytes_f32(p.fwd, c->T, c->d_out, mats);
   }
   // backward
   p.dz = off;
@@ -114,10 +141,14 @@ LinearPlan linear_plan(const moe_linear* c) {
   if (half) {
     p.dx = cut_rows(c->T, c->d_in, false, mats * (c->d_out / K_STAGE));
     off += align_up(cut_bytes(p.dx, 1), 256);
+  } else {
+    p.dx = cut_rows_f32(c->T, c->d_in, 1, mats * ((c->d_out + K_STAGE_F32 - 1) / K_STAGE_F32));
+    off += align_up(cut_bytes_f32(p.dx, c->T, c->d_in, 1), 256);
   }
   p.dw = off;
   p.segs = 1;
   if (c->T > 0) cut_weight_grad(c, mats, p);
+  if (!half) p.dw_rows = f32_tile_rows((long long)c->d_in * p.segs, 0, c->d_out);
   p.seg = seg_rows(c->T, p.segs);
   p.segs = c->T > 0 ? (c->T + p.seg - 1) / p.seg : 1;
   p.dw_direct = p.segs == 1;   // the product writes the gradient itself
@@ -135,6 +166,8 @@ struct ActBwdArgs {
   const uint8_t *scales, *scales2;
   void *dz, *dz2;
   float *sums, *sums2;              // [row blocks][N] or NULL
+  void *out, *out2;                 // one row block: the sums themselves, of type `grad`, or NULL
+  int grad, accumulate;
   long long T;
   int N;
   BiasGeom gm;
@@ -143,7 +176,7 @@ template <typename ST, int ACT, int FMT>
 __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
   constexpr int VN = Vec16<ST>::N;
-  __shared__ float s_sum[256][DUAL ? 17 : 9];
+  __shared__ float s_sum[4][64][DUAL ? 17 : 9];
   const int cl = threadIdx.x & (a.gm.cg - 1), rl = threadIdx.x / a.gm.cg, rp = 256 / a.gm.cg;
   const int c = (blockIdx.x * a.gm.cg + cl) * 8;
   const long long r0 = (long long)blockIdx.y * a.gm.rows, r1 = min(r0 + a.gm.rows, a.T);
@@ -209,20 +242,45 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
         if constexpr (DUAL) store(a.dz2, r, g2);
       }
     }
-  if (a.sums == nullptr) return;
+  if (a.sums == nullptr && a.out == nullptr) return;
+  // a wave's rows by exchanges between lanes, then the four waves in order
+  for (int s = a.gm.cg; s < WAVE; s <<= 1)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s_sum[threadIdx.x][i] = sum[i];
-    if constexpr (DUAL) s_sum[threadIdx.x][8 + i] = sum2[i];
+    for (int i = 0; i < 8; ++i) {
+      sum[i] += __shfl_xor(sum[i], s, WAVE);
+      if constexpr (DUAL) sum2[i] += __shfl_xor(sum2[i], s, WAVE);
+    }
+  const int wave = threadIdx.x / WAVE;
+  if ((threadIdx.x & (WAVE - 1)) < a.gm.cg) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s_sum[wave][cl][i] = sum[i];
+      if constexpr (DUAL) s_sum[wave][cl][8 + i] = sum2[i];
+    }
   }
   __syncthreads();
   if (rl != 0 || n <= 0) return;
-  for (int q = 1; q < rp; ++q)   // in row order: deterministic
+  for (int q = 1; q < 4; ++q)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      sum[i] += s_sum[q * a.gm.cg + cl][i];
-      if constexpr (DUAL) sum2[i] += s_sum[q * a.gm.cg + cl][8 + i];
+      sum[i] += s_sum[q][cl][i];
+      if constexpr (DUAL) sum2[i] += s_sum[q][cl][8 + i];
     }
+  if (a.out != nullptr) {
+    auto put = [&](void* p, const float (&v)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) {
+          if (a.grad == MOE_DTYPE_F32) {
+            float* o = reinterpret_cast<float*>(p) + c + i;
+            *o = a.accumulate ? *o + v[i] : v[i];
+          } else reinterpret_cast<ST*>(p)[c + i] = from_f32<ST>(v[i]);   // the storage type
+        }
+    };
+    put(a.out, sum);
+    if constexpr (DUAL) put(a.out2, sum2);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) {
@@ -288,8 +346,12 @@ int launch_linear_fwd(const moe_linear* c, const void* x, const void* W, const v
   g.A = x; g.B = W; g.B2 = Wb; g.C = pre; g.C2 = pre_b; g.C3 = y; g.S1 = residual; g.bias = bias; g.bias2 = bias_b;
   g.M = c->T; g.N = c->d_out; g.K = c->d_in; g.E = 1;
   g.chunked = row_tiles_chunked(c->T, c->d_in, c->d_out, 1, Wb != nullptr ? 2 : 1, c->dtype == MOE_DTYPE_F32 ? 4 : 2);
-  if (c->dtype == MOE_DTYPE_F32)
-    return launch_linear_f32(MODE_NN, c->act == MOE_ACT_SWIGLU ? EPI_LIN_SWIGLU : c->act == MOE_ACT_GELU ? EPI_LIN_GELU : EPI_LIN_NONE, false, g, s);
+  if (c->dtype == MOE_DTYPE_F32) {
+    g.tile_rows = p.fwd.rows;
+    g.split_parts = p.fwd.parts;
+    g.split_ws = (float*)ws;
+    return linear_forward_f32(c->act, g, s);
+  }
   return c->dtype == MOE_DTYPE_F16 ? linear_forward_f16(c->act, g, p, (float*)ws, s) : linear_forward_bf16(c->act, g, p, (float*)ws, s);
 }
 
@@ -349,44 +411,47 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
     a.scales = static_cast<const uint8_t*>(scales); a.scales2 = static_cast<const uint8_t*>(scales_b);
     if (c->act != MOE_ACT_NONE) { a.dz = w + p.dz; dz = a.dz; }
     if (mats == 2) { a.dz2 = w + p.dz + plane; dz2 = a.dz2; }
-    if (dbias != nullptr) {
+    const bool few = dbias != nullptr && bias_few(c->T, N);
+    if (few) { a.out = dbias; a.out2 = dbias_b; a.grad = c->grad; a.accumulate = accumulate; }
+    else if (dbias != nullptr) {
       a.sums = reinterpret_cast<float*>(w + p.db);
       a.sums2 = a.sums + (size_t)p.bias_geom.row_blocks * N;
     }
-    a.T = c->T; a.N = N; a.gm = p.bias_geom;
+    a.T = c->T; a.N = N; a.gm = few ? bias_geom_few(c->T, N) : p.bias_geom;
     TRY(c->dtype == MOE_DTYPE_F32   ? act_bwd_for<float>(c->act, a, c->pre_pack, s)
         : c->dtype == MOE_DTYPE_F16 ? act_bwd_for<f16>(c->act, a, c->pre_pack, s)
                                     : act_bwd_for<bf16>(c->act, a, c->pre_pack, s));
-    if (dbias != nullptr) {
+    if (dbias != nullptr && !few) {
       const JoinArgs j = {{a.sums, a.sums2}, {dbias, dbias_b}, (size_t)N, p.bias_geom.row_blocks, accumulate};
       TRY(launch_sum_rows(j, mats, c->grad, true, s));
     }
   }
-  GemmArgs g = {};
-  g.E = 1;
-  if (dx != nullptr) {   // dx = dz W^T (+ dz2 Wb^T) + dx_add
-    g.A = dz; g.A2 = dz2; g.B = W; g.B2 = Wb; g.C3 = dx; g.S1 = dx_add;
-    g.M = c->T; g.N = d; g.K = N;
-    g.chunked = row_tiles_chunked(c->T, N, d, 1, mats, (int)es);
-    float* split = reinterpret_cast<float*>(w + p.split);
-    if (es == 4) TRY(launch_linear_f32(MODE_NT, EPI_LIN_NONE, mats == 2, g, s));
-    else TRY(c->dtype == MOE_DTYPE_F16 ? linear_input_grad_f16(mats == 2, g, p, split, s) : linear_input_grad_bf16(mats == 2, g, p, split, s));
-  }
-  if (dW == nullptr) return MOE_OK;
+  // dx = dz W^T (+ dz2 Wb^T) + dx_add
+  GemmArgs g1 = {}, g2 = {};
+  g1.A = dz; g1.A2 = dz2; g1.B = W; g1.B2 = Wb; g1.C3 = dx; g1.S1 = dx_add;
+  g1.M = c->T; g1.N = d; g1.K = N; g1.E = 1;
+  g1.chunked = row_tiles_chunked(c->T, N, d, 1, mats, (int)es);
+  float* split = reinterpret_cast<float*>(w + p.split);
   // dW = x^T dz, dWb = x^T dz2: both in one launch
   const size_t out = (size_t)d * N;
   float* sums = reinterpret_cast<float*>(w + p.dw);
-  g = GemmArgs{};
-  g.A = x; g.B = dz; g.B2 = dz2;
-  g.C = p.dw_direct ? dW : sums;
-  if (mats == 2) g.C2 = p.dw_direct ? dWb : static_cast<void*>(sums + out * p.segs);
-  g.M = d; g.N = N; g.K = c->T; g.E = p.segs; g.seg = p.seg;
-  g.accumulate = p.dw_direct && accumulate;
-  if (es == 4) TRY(launch_linear_f32(MODE_TN, EPI_DW, false, g, s));
-  else {
-    const bool in_type = p.dw_direct && c->grad != MOE_DTYPE_F32;
-    TRY(c->dtype == MOE_DTYPE_F16 ? linear_weight_grad_f16(in_type, g, p, s) : linear_weight_grad_bf16(in_type, g, p, s));
+  if (dW != nullptr) {
+    g2.A = x; g2.B = dz; g2.B2 = dz2;
+    g2.C = p.dw_direct ? dW : sums;
+    if (mats == 2) g2.C2 = p.dw_direct ? dWb : static_cast<void*>(sums + out * p.segs);
+    g2.M = d; g2.N = N; g2.K = c->T; g2.E = p.segs; g2.seg = p.seg;
+    g2.accumulate = p.dw_direct && accumulate;
   }
+  if (es == 4) {
+    g1.tile_rows = p.dx.rows; g1.split_parts = p.dx.parts; g1.split_ws = split;
+    g2.tile_rows = p.dw_rows;
+    if (dx != nullptr || dW != nullptr) TRY(linear_backward_f32(mats == 2, g1, g2, s));
+  } else {
+    const bool f16 = c->dtype == MOE_DTYPE_F16, in_type = p.dw_direct && c->grad != MOE_DTYPE_F32;
+    if (dx != nullptr) TRY(f16 ? linear_input_grad_f16(mats == 2, g1, p, split, s) : linear_input_grad_bf16(mats == 2, g1, p, split, s));
+    if (dW != nullptr) TRY(f16 ? linear_weight_grad_f16(in_type, g2, p, s) : linear_weight_grad_bf16(in_type, g2, p, s));
+  }
+  if (dW == nullptr) return MOE_OK;
   if (p.dw_direct) return MOE_OK;
   const JoinArgs j = {{sums, sums + out * p.segs}, {dW, dWb}, out, p.segs, accumulate};
   return launch_sum_rows(j, mats, c->grad, false, s);
