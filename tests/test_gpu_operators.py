@@ -451,6 +451,60 @@ def test_linear_backward_from_packed_pre_activations(dtype, T, d, n, act, fmt):
     check_bwd(linear_case(T, d, n, dtype, act), fmt=fmt)
 
 
+# One size at least for every tile shape of the products and of the weight gradient, whole rounds of tiles, a rest and K parts.  T, d, n of
+# the forward; dx has d columns over n, or over 2 n where two products are chained.
+LARGE = [("bf16", 8192, 1024, 4096, "none"), ("bf16", 8191, 4096, 1024, "none"), ("f16", 4000, 2048, 4160, "swiglu"), ("bf16", 2300, 1088, 1984, "swiglu"),
+         ("bf16", 1024, 4096, 1024, "none"), ("f16", 600, 8192, 320, "swiglu"), ("bf16", 3001, 2880, 1088, "gelu"), ("bf16", 48, 14336, 512, "none"),
+         ("bf16", 20000, 512, 768, "none"), ("f32", 2048, 1024, 516, "swiglu"), ("f32", 150, 2048, 260, "none")]
+
+
+@pytest.mark.parametrize("dtype,T,d,n,act", LARGE)
+def test_linear_large(dtype, T, d, n, act):
+    """Every element against products in 64 bits on the device; tolerances as above."""
+    c = linear_case(T, d, n, dtype, act)
+    y, _ = run_fwd(c, keep=False)
+    hs = half_step(dtype)
+    x, W = c["x"].double(), [w.double() for w in c["W"]]
+    z = [x @ w + b.double() for w, b in zip(W, c["b"])]
+    err = [6 * math.sqrt(d) * U * (x.abs() @ w.abs() + 1) for w in W]
+    if act == "none":
+        want, slack = z[0], err[0]
+    elif act == "gelu":
+        want, slack = torch.nn.functional.gelu(z[0]), 1.2 * err[0] + 8e-7 * z[0].abs()
+    else:
+        sg = torch.sigmoid(z[0])
+        want = z[0] * sg * z[1]
+        slack = 1.2 * z[1].abs() * err[0] + z[0].abs() * err[1] + 2 * err[0] * err[1] + 8e-7 * z[0].abs() * z[1].abs()
+    want = want + c["r"].double()
+    assert ((y.double() - want).abs() <= hs * want.abs() + slack + 2.0 ** -25).all()
+    del z, err, want, slack, y
+    for grad in {"f32", dtype}:
+        dx, dW, db = run_bwd(c, grad=grad)
+        pre, dy = [p.double() for p in c["pre"]], c["dy"].double()
+        if act == "none":
+            dz = [dy]
+        elif act == "gelu":
+            dz = [dy * (0.5 * torch.erfc(-pre[0] / math.sqrt(2)) + pre[0] * torch.exp(-0.5 * pre[0] ** 2) / math.sqrt(2 * math.pi))]
+        else:
+            sg = torch.sigmoid(pre[0])
+            dz = [dy * pre[1] * sg * (1 + pre[0] * (1 - sg)), dy * pre[0] * sg]
+        fuzz, rdz = (0.0, 0.0) if act == "none" else (1e-6, hs)
+        mag = dy.abs() * (1 + sum(p.abs() for p in pre))
+        want = sum(g @ w.t() for g, w in zip(dz, W)) + c["add"].double()
+        walk = sum((g ** 2 @ (w.t() ** 2)).sqrt() for g, w in zip(dz, W))
+        sums = sum(g.abs() @ w.t().abs() for g, w in zip(dz, W)) + 1
+        slope = fuzz * sum(mag @ w.t().abs() for w in W)
+        assert ((dx.double() - want).abs() <= hs * want.abs() + 6 * rdz * walk + 6 * math.sqrt(2 * n) * U * sums + slope + 2.0 ** -25).all()
+        hg = half_step(grad)
+        for m, g in enumerate(dz):
+            want = x.t() @ g
+            tol = hg * want.abs() + 6 * rdz * ((x.t() ** 2) @ (g ** 2)).sqrt() + 6 * math.sqrt(T + 16) * U * (x.t().abs() @ g.abs() + 1) + fuzz * (x.t().abs() @ mag)
+            assert ((dW[m].double() - want).abs() <= tol).all()
+            want = g.sum(dim=0)
+            tol = hg * want.abs() + 6 * math.sqrt(T + 16) * U * (g.abs().sum(dim=0) + 1) + fuzz * mag.sum(dim=0)
+            assert ((db[m].double() - want).abs() <= tol).all()
+
+
 def test_linear_long_token_axis():
     """Weight gradients over many tokens, in segments: few tiles, a token count that no segment divides."""
     for dtype, T, d, n in (("bf16", 9001, 64, 128), ("f32", 4099, 64, 68)):
