@@ -40,6 +40,7 @@ struct LinearPlan {
   int dw_rows;        // weight gradient: edge of its tiles
   int segs, seg;      // ... segments of the tokens, rows of one
   bool dw_direct;     // ... written by the product itself
+  bool pair;          // both gradients in one launch
   size_t dz, db, split, dw, total;   // workspace: byte offsets of the backward's regions; the forward has it to itself
 };
 LinearPlan linear_plan(const moe_linear* c);

@@ -19,9 +19,11 @@ int linear_backward_f32(bool two, const GemmArgs& g1, const GemmArgs& g2, hipStr
 int linear_forward_bf16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);   // linear_bf16.hip
 int linear_input_grad_bf16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);
 int linear_weight_grad_bf16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s);
+int linear_both_grads_bf16(bool two, bool in_type, const GemmArgs& g1, const GemmArgs& g2, const LinearPlan& p, float* ws, hipStream_t s);
 int linear_forward_f16(int act, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);    // linear_f16.hip
 int linear_input_grad_f16(bool two, const GemmArgs& g, const LinearPlan& p, float* ws, hipStream_t s);
 int linear_weight_grad_f16(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s);
+int linear_both_grads_f16(bool two, bool in_type, const GemmArgs& g1, const GemmArgs& g2, const LinearPlan& p, float* ws, hipStream_t s);
 
 constexpr int K_STAGE = 64;   // K values per stage of the 16-bit kernels
 
@@ -47,11 +49,11 @@ struct Shape {
 constexpr Shape SHAPES[] = {{256, 256, 256, 6.5, 1.0, 1.37}, {160, 256, 256, 5.0, 0.65, 0.91}, {128, 256, 256, 4.2, 0.58, 0.79}, {64, 128, 512, 2.5, 0.28, 0.54}};
 constexpr Shape SHAPES_DUAL[] = {{256, 256, 256, 6.5, 1.07, 1.37}, {160, 256, 256, 5.5, 0.62, 0.86}, {128, 256, 256, 4.2, 0.6, 0.73}, {64, 256, 256, 3.3, 0.38, 0.5}};
 constexpr Shape SHAPES_DW[] = {{256, 256, 256, 6.5, 1.05, 1.42}, {128, 128, 256, 3.5, 0.34, 0.44}};
-constexpr double JOIN_US = 3.0, JOIN_US_PER_MB = 0.28;   // the adding launch; fp32 sums written and read again
+constexpr double LAUNCH_US = 2.0, JOIN_US = 3.0, JOIN_US_PER_MB = 0.28;   // the adding launch; fp32 sums written and read again
 constexpr int PART_STAGES = 4, MAX_PARTS = 16;   // K stages of 64 that a part has at least; parts at most
 
 // How `stages` K stages of T x N sums are cut: the shape, and the K parts of its last round, that take the least time.
-static RowCut cut_rows(long long T, int N, bool dual, int stages) {
+static RowCut cut_rows(long long T, int N, bool dual, int stages, double* us_of = nullptr) {
   RowCut best{};
   double least = 1e30;
   for (const Shape& s : dual ? SHAPES_DUAL : SHAPES) {
@@ -69,6 +71,7 @@ static RowCut cut_rows(long long T, int N, bool dual, int stages) {
       if (us < least) { least = us; best = c; }
     }
   }
+  if (us_of != nullptr) *us_of = least;
   return best;
 }
 // fp32: tiles of 64 or 32 rows (f32_tile_rows) and 64 columns in K stages of 32, every tile cut into `parts`.  A stage takes the matrix
@@ -98,7 +101,7 @@ static size_t cut_bytes(const RowCut& c, int mats) { return (size_t)(c.tiles - c
 
 // Tiles of the weight gradient and segments of the tokens: the least time, the segments' sums counted as above.  A segment stays
 // below 4 GiB of either operand (32-bit offsets).  fp32: 64 x 64 tiles, three on a compute unit, 2 us per 32 tokens.
-static void cut_weight_grad(const moe_linear* c, int mats, LinearPlan& p) {
+static double cut_weight_grad(const moe_linear* c, int mats, LinearPlan& p) {
   const long long T = c->T;
   const bool half = c->dtype != MOE_DTYPE_F32;
   const double out_mb = (double)c->d_in * c->d_out * mats * 4 / 1e6;
@@ -115,6 +118,34 @@ static void cut_weight_grad(const moe_linear* c, int mats, LinearPlan& p) {
     if (half) for (const Shape& s : SHAPES_DW) consider(s.rows, segs, s.tiles_us(tiles_of(s.rows) * segs, (int)((rows + K_STAGE - 1) / K_STAGE)));
     else consider(64, segs, (double)((tiles_of(64) * segs + F32_LOW_TILES - 1) / F32_LOW_TILES) * 0.06 * rows);
   }
+  return least;
+}
+// Both gradients in one launch (16-bit; tiles of 64 x 128 and 128 x 128, one on a compute unit): where that takes less time than
+// `apart`.  (So few tiles keep a segment's offsets far below 32 bits.)  One round of blocks: the longer of the two; two rounds: one after the other.  Two launches -> one, us: T x d x n
+// 64 x 256 x 256 11.3 -> 7.8, 300 x 1024 x 1024 14.1 -> 9.2, 1024 x 1024 x 1024 19.1 -> 12.7, SwiGLU (dz included) 33.6 -> 22.7;
+// 512 x 2048 x 1024 SwiGLU, 384 tiles, 26.4 -> 21.3; beyond two rounds 3000 x 1024 x 1024 28.3 -> 31.8.
+constexpr int PAIR_TILES = 512;
+static void try_pair(const moe_linear* c, int mats, double apart, LinearPlan& p) {
+  const int dx_stages = mats * (c->d_out / K_STAGE);
+  const long long dx_tiles = (long long)((c->T + 63) / 64) * ((c->d_in + 127) / 128);
+  const long long dw_tiles = (long long)((c->d_in + 127) / 128) * ((c->d_out + 127) / 128) * mats;
+  const double out_mb = (double)c->d_in * c->d_out * mats * 4 / 1e6;
+  for (int segs = 1; segs <= 4 && (segs == 1 || c->T / segs >= 256); ++segs)
+    for (int parts = 1; parts <= 8 && (parts == 1 || dx_stages >= parts * PART_STAGES); ++parts) {
+      const long long n = dx_tiles * parts + dw_tiles * segs;
+      if (n > PAIR_TILES) break;
+      const double dx = 2.5 + 0.3 * ((dx_stages + parts - 1) / parts), dw = 3.5 + 0.45 * ((c->T + segs * K_STAGE - 1) / (segs * K_STAGE));
+      double us = n <= 256 ? std::max(dx, dw) : dx + dw;
+      if (parts > 1) us += JOIN_US + JOIN_US_PER_MB * (double)dx_tiles * parts * 64 * 128 * 4 / 1e6;
+      if (segs > 1) us += JOIN_US + JOIN_US_PER_MB * out_mb * segs;
+      if (us < apart) {
+        apart = us;
+        p.pair = true;
+        p.dx = RowCut{dx_tiles, parts > 1 ? 0 : dx_tiles, 64, 128, parts};
+        p.dw_rows = 128;
+        p.segs = segs;
+      }
+    }
 }
 static int seg_rows(long long T, int segs) { return (int)(((T + segs - 1) / segs + 63) / 64 * 64); }
 
@@ -137,21 +168,21 @@ LinearPlan linear_plan(const moe_linear* c) {
   p.bias_geom = bias_geom(c->T, c->d_out);
   p.db = off;
   off += align_up((size_t)mats * p.bias_geom.row_blocks * N * 4, 256);
-  p.split = off;
-  if (half) {
-    p.dx = cut_rows(c->T, c->d_in, false, mats * (c->d_out / K_STAGE));
-    off += align_up(cut_bytes(p.dx, 1), 256);
-  } else {
-    p.dx = cut_rows_f32(c->T, c->d_in, 1, mats * ((c->d_out + K_STAGE_F32 - 1) / K_STAGE_F32));
-    off += align_up(cut_bytes_f32(p.dx, c->T, c->d_in, 1), 256);
-  }
-  p.dw = off;
+  double dx_us = 0;
+  if (half) p.dx = cut_rows(c->T, c->d_in, false, mats * (c->d_out / K_STAGE), &dx_us);
+  else p.dx = cut_rows_f32(c->T, c->d_in, 1, mats * ((c->d_out + K_STAGE_F32 - 1) / K_STAGE_F32));
   p.segs = 1;
-  if (c->T > 0) cut_weight_grad(c, mats, p);
-  if (!half) p.dw_rows = f32_tile_rows((long long)c->d_in * p.segs, 0, c->d_out);
-  p.seg = seg_rows(c->T, p.segs);
-  p.segs = c->T > 0 ? (c->T + p.seg - 1) / p.seg : 1;
+  if (c->T > 0) {
+    const double dw_us = cut_weight_grad(c, mats, p);
+    if (half) try_pair(c, mats, dx_us + dw_us + LAUNCH_US, p);
+    else p.dw_rows = f32_tile_rows((long long)c->d_in * p.segs, 0, c->d_out);
+    p.seg = seg_rows(c->T, p.segs);
+    p.segs = (c->T + p.seg - 1) / p.seg;
+  }
   p.dw_direct = p.segs == 1;   // the product writes the gradient itself
+  p.split = off;
+  off += align_up(half ? cut_bytes(p.dx, 1) : cut_bytes_f32(p.dx, c->T, c->d_in, 1), 256);
+  p.dw = off;
   if (!p.dw_direct) off += align_up((size_t)mats * p.segs * c->d_in * N * 4, 256);
   p.total = std::max(align_up(fwd, 256), off);
   return p;
@@ -448,8 +479,11 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
     if (dx != nullptr || dW != nullptr) TRY(linear_backward_f32(mats == 2, g1, g2, s));
   } else {
     const bool f16 = c->dtype == MOE_DTYPE_F16, in_type = p.dw_direct && c->grad != MOE_DTYPE_F32;
-    if (dx != nullptr) TRY(f16 ? linear_input_grad_f16(mats == 2, g1, p, split, s) : linear_input_grad_bf16(mats == 2, g1, p, split, s));
-    if (dW != nullptr) TRY(f16 ? linear_weight_grad_f16(in_type, g2, p, s) : linear_weight_grad_bf16(in_type, g2, p, s));
+    if (p.pair && dx != nullptr && dW != nullptr) TRY(f16 ? linear_both_grads_f16(mats == 2, in_type, g1, g2, p, split, s) : linear_both_grads_bf16(mats == 2, in_type, g1, g2, p, split, s));
+    else {
+      if (dx != nullptr) TRY(f16 ? linear_input_grad_f16(mats == 2, g1, p, split, s) : linear_input_grad_bf16(mats == 2, g1, p, split, s));
+      if (dW != nullptr) TRY(f16 ? linear_weight_grad_f16(in_type, g2, p, s) : linear_weight_grad_bf16(in_type, g2, p, s));
+    }
   }
   if (dW == nullptr) return MOE_OK;
   if (p.dw_direct) return MOE_OK;

@@ -10,6 +10,15 @@ __global__ __launch_bounds__(WGM* WGN * 64, WGM * WGN == 4 ? 2 : 1) void linear_
   extern __shared__ __attribute__((aligned(16))) char smem[];
   gemm_bf16_tile<ST, MODE, EPI, DUAL, CHAIN, BM, BN, WGM, WGN, false, STREAM, true>(g, blockIdx.x, smem);
 }
+// The input's gradient (g1, tiles of 64 x 128) and the weights' (g2, 128 x 128) in one launch, where together they do not fill the chip:
+// they need nothing of each other.
+template <typename ST, bool CHAIN, int EPI2>
+__global__ __launch_bounds__(256, 1) void linear_pair_kernel(GemmArgs g1, GemmArgs g2, int first_blocks) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  if ((int)blockIdx.x < first_blocks) gemm_bf16_tile<ST, MODE_NT, EPI_LIN_NONE, false, CHAIN, 64, 128, 2, 2, false, false, true>(g1, blockIdx.x, smem);
+  else gemm_bf16_tile<ST, MODE_TN, EPI2, false, false, 128, 128, 2, 2, false, false, true>(g2, blockIdx.x - first_blocks, smem);
+}
+
 // Adds the parts of split tiles in part order and applies the epilogue; a thread owns eight adjacent columns of a row.
 template <typename ST, int EPI>
 __global__ __launch_bounds__(256) void linear_join_kernel(GemmArgs g) {
@@ -128,6 +137,25 @@ static int fwd_half_act(int act, const GemmArgs& g, const LinearPlan& p, float* 
 }
 
 
+template <typename ST, bool CHAIN, int EPI2>
+static int launch_pair(GemmArgs g1, const GemmArgs& g2, const LinearPlan& p, float* ws, hipStream_t s) {
+  constexpr int lds1 = gemm_bf16_lds_bytes<64, 128, false>(), lds2 = gemm_bf16_lds_bytes<128, 128, false>(), lds = lds1 > lds2 ? lds1 : lds2;
+  auto kern = linear_pair_kernel<ST, CHAIN, EPI2>;
+  const int rc = more_lds(kern, lds);
+  if (rc != MOE_OK) return rc;
+  g1.tile_rows = p.dx.rows;
+  g1.tile_cols = p.dx.cols;
+  g1.split_first = (int)p.dx.first;
+  g1.split_parts = p.dx.parts;
+  g1.split_ws = ws;
+  // a multiple of the XCD count: a tile number still tells the XCD for the second product
+  const long long n1 = (p.dx.tiles * p.dx.parts + NUM_XCD - 1) / NUM_XCD * NUM_XCD, n2 = dw_blocks(g2, 128, 128);
+  kern<<<dim3((unsigned)(n1 + n2)), 256, lds, s>>>(g1, g2, (int)n1);
+  const int rc2 = launch_status();
+  if (rc2 != MOE_OK || p.dx.parts == 1) return rc2;
+  return launch_join<ST, EPI_LIN_NONE>(g1, p.dx.tiles * (p.dx.rows * p.dx.cols / 8 / 256), s);
+}
+
 // What linear.hip calls for a storage type
 template <typename ST>
 struct LinearHalf {
@@ -138,6 +166,10 @@ struct LinearHalf {
   // in_type: in the storage type instead of fp32
   static int weight_grad(bool in_type, const GemmArgs& g, const LinearPlan& p, hipStream_t s) {
     return in_type ? launch_dw<ST, EPI_LIN_NONE>(g, p.dw_rows, s) : launch_dw<ST, EPI_DW>(g, p.dw_rows, s);
+  }
+  static int both_grads(bool two, bool in_type, const GemmArgs& g1, const GemmArgs& g2, const LinearPlan& p, float* ws, hipStream_t s) {
+    if (two) return in_type ? launch_pair<ST, true, EPI_LIN_NONE>(g1, g2, p, ws, s) : launch_pair<ST, true, EPI_DW>(g1, g2, p, ws, s);
+    return in_type ? launch_pair<ST, false, EPI_LIN_NONE>(g1, g2, p, ws, s) : launch_pair<ST, false, EPI_DW>(g1, g2, p, ws, s);
   }
 };
 
