@@ -147,6 +147,8 @@ static void try_pair(const moe_linear* c, int mats, double apart, LinearPlan& p)
       }
     }
 }
+// the format of the pre-activations that the backward reads
+static int pre_format(const moe_linear* c) { return c->act == MOE_ACT_NONE ? MOE_PACK_NONE : c->pre_pack; }
 static int seg_rows(long long T, int segs) { return (int)(((T + segs - 1) / segs + 63) / 64 * 64); }
 
 LinearPlan linear_plan(const moe_linear* c) {
@@ -165,7 +167,7 @@ LinearPlan linear_plan(const moe_linear* c) {
   // backward
   p.dz = off;
   if (c->act != MOE_ACT_NONE) off += align_up(mats * T * N * es, 256);
-  p.bias_geom = bias_geom(c->T, c->d_out);
+  p.bias_geom = bias_geom(c->T, c->d_out, act_bwd_cols(!half, pre_format(c)));
   p.db = off;
   off += align_up((size_t)mats * p.bias_geom.row_blocks * N * 4, 256);
   double dx_us = 0;
@@ -190,7 +192,7 @@ LinearPlan linear_plan(const moe_linear* c) {
 
 // ---- kernels -------------------------------------------------------------------------------------------------------
 // dz = dy act'(pre), rounded to the storage type, and the column sums of the unrounded dz, one row of partial sums per block.
-// A thread owns eight adjacent columns and walks down the rows of its block; cg threads span a block's columns.
+// A thread owns act_bwd_cols adjacent columns and walks down the rows of its block; cg threads span a block's columns.
 struct ActBwdArgs {
   const void* dy;
   const void *pre, *pre2;           // storage type, or codes
@@ -206,43 +208,43 @@ struct ActBwdArgs {
 template <typename ST, int ACT, int FMT>
 __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
-  constexpr int VN = Vec16<ST>::N;
-  __shared__ float s_sum[4][64][DUAL ? 17 : 9];
+  constexpr int VN = Vec16<ST>::N, CPT = act_bwd_cols(sizeof(ST) == 4, FMT);
+  __shared__ float s_sum[4][64][(DUAL ? 2 : 1) * CPT + 1];
   const int cl = threadIdx.x & (a.gm.cg - 1), rl = threadIdx.x / a.gm.cg, rp = 256 / a.gm.cg;
-  const int c = (blockIdx.x * a.gm.cg + cl) * 8;
+  const int c = (blockIdx.x * a.gm.cg + cl) * CPT;
   const long long r0 = (long long)blockIdx.y * a.gm.rows, r1 = min(r0 + a.gm.rows, a.T);
-  const int n = min(8, a.N - c);                       // columns of this thread: 8, 4 (fp32) or none
+  const int n = min(CPT, a.N - c);                     // columns of this thread: CPT, 4 (fp32) or none
   const int blocks = (a.N + BLOCK8 - 1) / BLOCK8;
-  float sum[8] = {}, sum2[8] = {};
-  auto load = [&](const void* p, long long r, float (&v)[8]) {
+  float sum[CPT] = {}, sum2[CPT] = {};
+  auto load = [&](const void* p, long long r, float (&v)[CPT]) {
     const ST* at = reinterpret_cast<const ST*>(p) + r * a.N + c;
 #pragma unroll
-    for (int i = 0; i < 8; i += VN)
+    for (int i = 0; i < CPT; i += VN)
       if (i < n) {
         Vec16<ST> q;
         q.load_nt(at + i);
         q.unpack(v + i);
       }
   };
-  auto store = [&](void* p, long long r, const float (&v)[8]) {
+  auto store = [&](void* p, long long r, const float (&v)[CPT]) {
     ST* at = reinterpret_cast<ST*>(p) + r * a.N + c;
 #pragma unroll
-    for (int i = 0; i < 8; i += VN)
+    for (int i = 0; i < CPT; i += VN)
       if (i < n) {
         Vec16<ST> q;
         q.pack(v + i);
         q.store_nt(at + i);
       }
   };
-  auto load_pre = [&](const void* p, const uint8_t* sc, long long r, float (&v)[8]) {
+  auto load_pre = [&](const void* p, const uint8_t* sc, long long r, float (&v)[CPT]) {
     if constexpr (FMT == MOE_PACK_NONE) load(p, r, v);
     else decode8<ST, FMT>(*reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(p) + r * blocks * BLOCK8 + c), sc[r * blocks + c / BLOCK8], v);
   };
   // U rows of a thread are requested together; a row past the end repeats the last one and counts for nothing
-  constexpr int U = sizeof(ST) == 4 ? 1 : 2;
+  constexpr int U = CPT > VN ? 1 : 2;
   if (n > 0)
     for (long long ra = r0 + rl; ra < r1; ra += (long long)rp * U) {
-      float dy[U][8] = {}, z[U][8] = {}, z2[U][8] = {};
+      float dy[U][CPT] = {}, z[U][CPT] = {}, z2[U][CPT] = {};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const long long r = min(ra + (long long)u * rp, r1 - 1);
@@ -254,9 +256,9 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
       for (int u = 0; u < U; ++u) {
         const long long r = ra + (long long)u * rp;
         if (r >= r1) break;
-        float g[8], g2[8];
+        float g[CPT], g2[CPT];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < CPT; ++i) {
           if constexpr (DUAL) {
             const float sg = sizeof(ST) == 4 ? sigmoid_f(z[u][i]) : __builtin_amdgcn_rcpf(1.f + __expf(-z[u][i]));
             g[i] = dy[u][i] * z2[u][i] * sg * fmaf(z[u][i], 1.f - sg, 1.f);
@@ -277,30 +279,30 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
   // a wave's rows by exchanges between lanes, then the four waves in order
   for (int s = a.gm.cg; s < WAVE; s <<= 1)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < CPT; ++i) {
       sum[i] += __shfl_xor(sum[i], s, WAVE);
       if constexpr (DUAL) sum2[i] += __shfl_xor(sum2[i], s, WAVE);
     }
   const int wave = threadIdx.x / WAVE;
   if ((threadIdx.x & (WAVE - 1)) < a.gm.cg) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < CPT; ++i) {
       s_sum[wave][cl][i] = sum[i];
-      if constexpr (DUAL) s_sum[wave][cl][8 + i] = sum2[i];
+      if constexpr (DUAL) s_sum[wave][cl][CPT + i] = sum2[i];
     }
   }
   __syncthreads();
   if (rl != 0 || n <= 0) return;
   for (int q = 1; q < 4; ++q)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < CPT; ++i) {
       sum[i] += s_sum[q][cl][i];
-      if constexpr (DUAL) sum2[i] += s_sum[q][cl][8 + i];
+      if constexpr (DUAL) sum2[i] += s_sum[q][cl][CPT + i];
     }
   if (a.out != nullptr) {
-    auto put = [&](void* p, const float (&v)[8]) {
+    auto put = [&](void* p, const float (&v)[CPT]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < CPT; ++i)
         if (i < n) {
           if (a.grad == MOE_DTYPE_F32) {
             float* o = reinterpret_cast<float*>(p) + c + i;
@@ -313,7 +315,7 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(ActBwdArgs a) {
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < CPT; ++i)
     if (i < n) {
       a.sums[(size_t)blockIdx.y * a.N + c + i] = sum[i];
       if constexpr (DUAL) a.sums2[(size_t)blockIdx.y * a.N + c + i] = sum2[i];
@@ -389,7 +391,7 @@ int launch_linear_fwd(const moe_linear* c, const void* x, const void* W, const v
 template <typename ST, int ACT>
 static int launch_act_bwd(const ActBwdArgs& a, int fmt, hipStream_t s) {
   const dim3 grid(a.gm.col_blocks, a.gm.row_blocks);
-  if (ACT == MOE_ACT_NONE || fmt == MOE_PACK_NONE) act_bwd_kernel<ST, ACT, MOE_PACK_NONE><<<grid, 256, 0, s>>>(a);
+  if (fmt == MOE_PACK_NONE) act_bwd_kernel<ST, ACT, MOE_PACK_NONE><<<grid, 256, 0, s>>>(a);
   else if (fmt == MOE_PACK_E4M3) act_bwd_kernel<ST, ACT, ACT == MOE_ACT_NONE ? MOE_PACK_NONE : MOE_PACK_E4M3><<<grid, 256, 0, s>>>(a);
   else act_bwd_kernel<ST, ACT, ACT == MOE_ACT_NONE ? MOE_PACK_NONE : MOE_PACK_I8><<<grid, 256, 0, s>>>(a);
   return launch_status();
@@ -448,10 +450,10 @@ int launch_linear_bwd(const moe_linear* c, const void* dy, const void* x, const 
       a.sums = reinterpret_cast<float*>(w + p.db);
       a.sums2 = a.sums + (size_t)p.bias_geom.row_blocks * N;
     }
-    a.T = c->T; a.N = N; a.gm = few ? bias_geom_few(c->T, N) : p.bias_geom;
-    TRY(c->dtype == MOE_DTYPE_F32   ? act_bwd_for<float>(c->act, a, c->pre_pack, s)
-        : c->dtype == MOE_DTYPE_F16 ? act_bwd_for<f16>(c->act, a, c->pre_pack, s)
-                                    : act_bwd_for<bf16>(c->act, a, c->pre_pack, s));
+    a.T = c->T; a.N = N; a.gm = few ? bias_geom_few(c->T, N, act_bwd_cols(es == 4, pre_format(c))) : p.bias_geom;
+    TRY(c->dtype == MOE_DTYPE_F32   ? act_bwd_for<float>(c->act, a, pre_format(c), s)
+        : c->dtype == MOE_DTYPE_F16 ? act_bwd_for<f16>(c->act, a, pre_format(c), s)
+                                    : act_bwd_for<bf16>(c->act, a, pre_format(c), s));
     if (dbias != nullptr && !few) {
       const JoinArgs j = {{a.sums, a.sums2}, {dbias, dbias_b}, (size_t)N, p.bias_geom.row_blocks, accumulate};
       TRY(launch_sum_rows(j, mats, c->grad, true, s));
