@@ -426,7 +426,7 @@ MOE_API int moe_saved_restore8(const moe_cfg* cfg, int32_t fmt, const void* code
  * pre_b_scales.  moe_linear.grad: type of dW, dWb, dbias, dbias_b: MOE_DTYPE_F32 (accumulate != 0 adds to them) or the storage
  * type (accumulate must be 0).
  * Shapes: T >= 0 (0: fp32 gradients are left as they are or zeroed); d_in, d_out multiples of 64 (16-bit) or 4 (fp32), and
- * d_in * d_out * 4 < 2^32; T <= 2^24.
+ * up to 2^20, and d_in * d_out * 4 < 2^32; T <= 2^24.
  * `ws` holds moe_linear_workspace_bytes and is free again when the call is done.
  */
 enum { MOE_ACT_NONE = 2 };   /* moe_linear only */

@@ -479,7 +479,8 @@ static int check_linear(const moe_linear* c) {
   if (c->grad != MOE_DTYPE_F32 && c->grad != c->dtype) return MOE_ERR_BAD_DTYPE;
   const int mult = c->dtype == MOE_DTYPE_F32 ? 4 : 64;
   if (c->T < 0 || c->T > (1 << 24) || c->d_in < 1 || c->d_out < 1 || c->d_in % mult != 0 || c->d_out % mult != 0) return MOE_ERR_BAD_SHAPE;
-  if ((long long)c->d_in * c->d_out * 4 >= (1ll << 32)) return MOE_ERR_BAD_SHAPE;
+  // 32-bit offsets: the weights, the 256 rows of a tile, and segments of whole tokens (linear.hip) stay below 4 GiB
+  if ((long long)c->d_in * c->d_out * 4 >= (1ll << 32) || c->d_in > (1 << 20) || c->d_out > (1 << 20)) return MOE_ERR_BAD_SHAPE;
   return MOE_OK;
 }
 

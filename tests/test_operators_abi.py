@@ -124,3 +124,13 @@ def test_linear_workspace_covers_every_cut():
             for T in (1, 63, 64, 65, 160, 161, 511, 512, 513, 4096, 100000):
                 n = B.moe_linear_workspace_bytes(B.make_linear(T, 256, 512, dtype, act))
                 assert 0 < n < (1 << 30) + 16 * T * 512 * 4, (T, n)
+
+
+def test_linear_widths_keep_a_tile_below_32_bits():
+    """256 rows of 2^20 16-bit values are half a GiB; twice as wide a row and its tile's gradient sums would need offsets past 2^31."""
+    for dtype, d in ((B.DTYPE_BF16, 64), (B.DTYPE_F32, 4)):
+        wide = 1 << 20
+        assert B.moe_linear_workspace_bytes(B.make_linear(256, d, wide, dtype, B.ACT_GELU)) > 0
+        assert B.moe_linear_workspace_bytes(B.make_linear(256, wide, d, dtype, B.ACT_GELU)) > 0
+        refused(-2, B.moe_linear_workspace_bytes, B.make_linear(256, d, wide + 64, dtype, B.ACT_GELU))
+        refused(-2, B.moe_linear_workspace_bytes, B.make_linear(256, wide + 64, d, dtype, B.ACT_GELU))
