@@ -97,7 +97,7 @@ int launch_combine_bwd(const moe_cfg*, const void*, const void*, const float*, c
 int launch_wr_transpose(const moe_cfg*, const float*, float*, hipStream_t);
 int launch_score(const moe_cfg*, const moe_score*, const float*, const float*, int32_t*, float*, hipStream_t);
 int launch_score_bwd(const moe_cfg*, const moe_score*, const float*, const int32_t*, const float*, float*, hipStream_t);
-int launch_score_dx(const moe_cfg*, const float*, const float*, void*, hipStream_t);
+int launch_score_dx(const moe_cfg*, const moe_score*, const int32_t*, const float*, const float*, void*, hipStream_t);
 bool input_grad_has_dwr(const moe_cfg*);
 int launch_input_grad(const moe_cfg*, const moe_layer_bufs*, const float*, float*, bool, hipStream_t);
 int launch_gate_dwr(const moe_cfg*, const void*, const float*, float*, int, float*, bool, hipStream_t);
@@ -401,7 +401,7 @@ int moe_route_scored_bwd(const moe_cfg* cfg, const moe_score* score, const void*
   if (dx != nullptr) {
     float* WrT = reinterpret_cast<float*>(static_cast<char*>(ws) + w.route_wrt);
     CHECK(launch_wr_transpose(cfg, Wr, WrT, s));
-    CHECK(launch_score_dx(cfg, d_logits, WrT, dx, s));
+    CHECK(launch_score_dx(cfg, score, topk_idx, d_logits, WrT, dx, s));
   }
   if (dWr == nullptr) return MOE_OK;
   return launch_gate_dwr(cfg, x, d_logits, dWr, accumulate, reinterpret_cast<float*>(static_cast<char*>(ws) + w.route_partials), false, s);

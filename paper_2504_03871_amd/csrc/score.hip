@@ -14,6 +14,7 @@
 
 namespace moe {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int SC_LANES = 16, SC_ROWS = 256 / SC_LANES;   // lanes per token, tokens per block
 
 struct ScoreArgs {
@@ -554,44 +555,101 @@ __global__ __launch_bounds__(256) void score_bwd_kernel(ScoreArgs a, const float
   }
 }
 
-// dx += d_logits Wr^T.  A block owns SDX_TOK tokens and 256 4-column groups; the weight's transpose [E][d] is read once per
-// block, for the experts that any of the tokens has a gradient for.
-constexpr int SDX_TOK = 8;
+// dx += d_logits Wr^T, over the chosen experts: a wave per token adds up their rows of the weight's transpose [E][d].
+// For gradients that only the chosen experts have; bound by those rows, which come from the L2s: 32768 tokens x 4096, 8 of
+// 256 experts, 259 us: 4.3 GB of rows, 16.6 TB/s, and 0.5 GB of dx.
 template <typename T>
-__global__ __launch_bounds__(256) void score_dx_kernel(const float* __restrict__ d_logits, const float* __restrict__ WrT, T* __restrict__ dx,
-                                                       int Tn, int d, int E) {
-  __shared__ float dl[MOE_MAX_E][SDX_TOK];
-  const int t0 = blockIdx.x * SDX_TOK;
-  for (int i = threadIdx.x; i < E * SDX_TOK; i += 256) {
-    const int e = i % E, q = i / E;
-    dl[e][q] = t0 + q < Tn ? d_logits[(size_t)(t0 + q) * E + e] : 0.f;
+__global__ __launch_bounds__(256) void score_dx_chosen_kernel(const float* __restrict__ d_logits, const int32_t* __restrict__ topk_idx,
+                                                              const float* __restrict__ WrT, T* __restrict__ dx, int Tn, int d, int E, int k) {
+  constexpr int VN = Vec16<T>::N, U = 4;   // 16-byte pieces of a row of dx per lane in flight
+  const int lane = threadIdx.x & (WAVE - 1), t = (int)((blockIdx.x * blockDim.x + threadIdx.x) / WAVE);
+  if (t >= Tn) return;
+  float g[MOE_MAX_K];
+  int at[MOE_MAX_K];
+#pragma unroll
+  for (int j = 0; j < MOE_MAX_K; ++j)
+    if (j < k) {
+      const int e = topk_idx[(size_t)t * k + j];
+      const bool live = e >= 0 && e < E;
+      at[j] = live ? e : 0;
+      g[j] = live ? d_logits[(size_t)t * E + e] : 0.f;
+    }
+  T* row = dx + (size_t)t * d;
+  for (int c0 = lane * VN; c0 < d; c0 += WAVE * VN * U) {
+    Vec16<T> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + u * WAVE * VN < d) v[u].load_nt(row + c0 + u * WAVE * VN);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + u * WAVE * VN;
+      if (c >= d) break;
+      float sum[VN];
+      v[u].unpack(sum);
+#pragma unroll
+      for (int j = 0; j < MOE_MAX_K; ++j)
+        if (j < k) {
+#pragma unroll
+          for (int i = 0; i < VN; i += 4) {
+            const f32x4 w = *reinterpret_cast<const f32x4*>(WrT + (size_t)at[j] * d + c + i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[i + q] = fmaf(g[j], w[q], sum[i + q]);
+          }
+        }
+      v[u].pack(sum);
+      v[u].store_nt(row + c);
+    }
+  }
+}
+
+// The same over all experts, on the matrix cores in fp32: tokens as M, columns as N, experts as K.  A block: 32 tokens x 256 columns,
+// a wave 32 x 64.  Of every 16 experts lane group g = lane / 16 supplies 4 g + s in step s, and lane c = lane % 16 holds columns
+// 4 c .. 4 c + 3 as column tiles 0 .. 3: one 16-byte read of the gradients serves four steps, one of the weights four tiles, and the
+// sums leave as four adjacent columns.  8192 tokens, 64 experts, d 1024 | 4096: 20 | 61 us with the transpose, of which dx itself is
+// 6 | 24 at the rate of a copy; by multiply-adds, eight tokens x four columns per thread, 37 | 128.  Tokens past the batch and experts past E count with a gradient of zero.
+constexpr int SDX_TOK = 32, SDX_COLS = 256;
+template <typename T>
+__global__ __launch_bounds__(256) void score_dx_all_kernel(const float* __restrict__ d_logits, const float* __restrict__ WrT, T* __restrict__ dx,
+                                                           int Tn, int d, int E) {
+  extern __shared__ __attribute__((aligned(16))) float dl[];   // [32][pitch]: sixteen rows' 16 bytes in different banks
+  const int steps = (E + 15) / 16, pitch = steps * 16 + 4;
+  const int t0 = blockIdx.x * SDX_TOK, lane = threadIdx.x & (WAVE - 1), c = lane & 15, grp = lane >> 4;
+  for (int i = threadIdx.x; i < SDX_TOK * steps * 16; i += 256) {
+    const int q = i / (steps * 16), e = i - q * (steps * 16);
+    dl[q * pitch + e] = t0 + q < Tn && e < E ? d_logits[(size_t)(t0 + q) * E + e] : 0.f;
   }
   __syncthreads();
-  for (int c = threadIdx.x * 4; c < d; c += 1024) {
-    float acc[SDX_TOK][4] = {};
-    for (int e = 0; e < E; ++e) {
-      float g[SDX_TOK];
-      bool any = false;
+  const int col = blockIdx.y * SDX_COLS + threadIdx.x / WAVE * 64 + c * 4;
+  const float* w = WrT + min(col, d - 4);   // columns past the row repeat its last four and are not stored
+  f32x4 acc[2][4] = {};
+  for (int q = 0; q < steps; ++q) {
+    const f32x4 a0 = *reinterpret_cast<const f32x4*>(dl + c * pitch + q * 16 + grp * 4);
+    const f32x4 a1 = *reinterpret_cast<const f32x4*>(dl + (16 + c) * pitch + q * 16 + grp * 4);
+    f32x4 b[4];
 #pragma unroll
-      for (int q = 0; q < SDX_TOK; ++q) { g[q] = dl[e][q]; any |= g[q] != 0.f; }
-      if (!any) continue;
-      const float4 w = *reinterpret_cast<const float4*>(WrT + (size_t)e * d + c);
+    for (int s = 0; s < 4; ++s) b[s] = *reinterpret_cast<const f32x4*>(w + (size_t)min(q * 16 + grp * 4 + s, E - 1) * d);
 #pragma unroll
-      for (int q = 0; q < SDX_TOK; ++q) {
-        acc[q][0] = fmaf(g[q], w.x, acc[q][0]);
-        acc[q][1] = fmaf(g[q], w.y, acc[q][1]);
-        acc[q][2] = fmaf(g[q], w.z, acc[q][2]);
-        acc[q][3] = fmaf(g[q], w.w, acc[q][3]);
-      }
-    }
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int q = 0; q < SDX_TOK; ++q)
-      if (t0 + q < Tn) {
-        T* o = dx + (size_t)(t0 + q) * d + c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = from_f32<T>(to_f32(o[i]) + acc[q][i]);
+      for (int j = 0; j < 4; ++j) {
+        acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a0[s], b[s][j], acc[0][j], 0, 0, 0);
+        acc[1][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a1[s], b[s][j], acc[1][j], 0, 0, 0);
       }
   }
+  if (col >= d) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {   // register v of a lane: token 4 grp + v
+      const int t = t0 + h * 16 + grp * 4 + v;
+      if (t >= Tn) break;
+      T* o = dx + (size_t)t * d + col;
+      T was[4];
+      __builtin_memcpy(was, o, sizeof was);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) was[j] = from_f32<T>(to_f32(was[j]) + acc[h][j][v]);
+      __builtin_memcpy(o, was, sizeof was);
+    }
 }
 
 static int per_lane(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : 16; }
@@ -637,12 +695,24 @@ int launch_score_bwd(const moe_cfg* c, const moe_score* sc, const float* logits,
   return launch_status();
 }
 
-int launch_score_dx(const moe_cfg* c, const float* d_logits, const float* WrT, void* dx, hipStream_t s) {
-  const unsigned grid = (unsigned)((c->T + SDX_TOK - 1) / SDX_TOK);
-  if (c->dtype == MOE_DTYPE_BF16) score_dx_kernel<bf16><<<grid, 256, 0, s>>>(d_logits, WrT, (bf16*)dx, c->T, c->d_model, c->E);
-  else if (c->dtype == MOE_DTYPE_F16) score_dx_kernel<f16><<<grid, 256, 0, s>>>(d_logits, WrT, (f16*)dx, c->T, c->d_model, c->E);
-  else score_dx_kernel<float><<<grid, 256, 0, s>>>(d_logits, WrT, (float*)dx, c->T, c->d_model, c->E);
+template <typename T>
+static int launch_score_dx_for(const moe_cfg* c, bool all, const int32_t* idx, const float* d_logits, const float* WrT, T* dx, hipStream_t s) {
+  if (all) {
+    const size_t lds = SDX_TOK * ((c->E + 15) / 16 * 16 + 4) * sizeof(float);   // 33 KB at most
+    const dim3 grid((c->T + SDX_TOK - 1) / SDX_TOK, (c->d_model + SDX_COLS - 1) / SDX_COLS);
+    score_dx_all_kernel<T><<<grid, 256, lds, s>>>(d_logits, WrT, dx, c->T, c->d_model, c->E);
+  } else {
+    score_dx_chosen_kernel<T><<<dim3((c->T + 3) / 4), 256, 0, s>>>(d_logits, idx, WrT, dx, c->T, c->d_model, c->E, c->k);
+  }
   return launch_status();
+}
+int launch_score_dx(const moe_cfg* c, const moe_score* sc, const int32_t* idx, const float* d_logits, const float* WrT, void* dx, hipStream_t s) {
+  // where only the chosen have one, their rows alone are faster at every ratio of E to k (T x d x E, k, us, chosen | all):
+  // 8192 x 1024 x 8, 2 7 | 7; 8192 x 1024 x 64, 6 13 | 20; 8192 x 4096 x 128, 8 67 | 108; 32768 x 4096 x 256, 8 259 | 849
+  const bool all = sc->score == MOE_SCORE_SOFTMAX && !sc->renorm;
+  if (c->dtype == MOE_DTYPE_BF16) return launch_score_dx_for(c, all, idx, d_logits, WrT, (bf16*)dx, s);
+  if (c->dtype == MOE_DTYPE_F16) return launch_score_dx_for(c, all, idx, d_logits, WrT, (f16*)dx, s);
+  return launch_score_dx_for(c, all, idx, d_logits, WrT, (float*)dx, s);
 }
 
 }  // namespace moe

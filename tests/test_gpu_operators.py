@@ -193,6 +193,30 @@ def test_scored_routing_from_the_gate_product(dtype, T, d, E, k):
         assert np.all(np.abs(f64(dx) - want) <= half_step(dtype) * np.abs(want) + 8 * math.sqrt(E) * U * size + 2.0 ** -25)
 
 
+@pytest.mark.parametrize("kind,renorm", [(B.SCORE_SIGMOID, 1), (B.SCORE_SIGMOID, 0), (B.SCORE_SOFTMAX, 0)])
+@pytest.mark.parametrize("T,d,E,k", [(33, 68, 3, 1), (5, 516, 17, 8), (64, 260, 33, 3), (1, 4, 2, 2)])
+def test_scored_input_gradient_odd_sizes(T, d, E, k, kind, renorm):
+    """dx += d_logits Wr^T in fp32 where no tile of tokens, columns or experts is whole; a token without experts adds nothing."""
+    r = np.random.default_rng(100 * T + E)
+    lg = r.normal(0, 1, (T, E)).astype(np.float32)
+    if T > 1:
+        lg[T // 2] = -np.inf
+    logits, Wr = dev(lg), dev(r.normal(0, 1, (d, E)))
+    cfg, sc = B.make_cfg(T, d, 64, E, k, DT["f32"]), B.make_score(kind, 1, 1, 1, renorm, 1.5)
+    ws = torch.empty(B.moe_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    idx, w = torch.empty(T, k, dtype=torch.int32, device=DEV), torch.empty(T, k, device=DEV)
+    B.moe_route_scored(cfg, sc, None, None, None, None, logits, None, idx, w, ws)
+    dw, dl, dx = dev(r.normal(0, 1, (T, k))), torch.empty(T, E, device=DEV), dev(r.normal(0, 1, (T, d)))
+    before = f64(dx)
+    B.moe_route_scored_bwd(cfg, sc, None, Wr, logits, idx, dw, dl, None, dx, ws)
+    g = f64(dl)
+    want, size = before + g @ f64(Wr).T, np.abs(before) + np.abs(g) @ np.abs(f64(Wr)).T
+    # fp32 sums of at most E + 1 terms
+    assert np.all(np.abs(f64(dx) - want) <= (E + 2) * U * size)
+    if T > 1:
+        assert np.array_equal(f64(dx)[T // 2], before[T // 2])
+
+
 def test_empty_slots_travel_through_the_layer():
     """Tokens without an expert: dropped by dispatch, nothing in the output, no gradient."""
     from paper_2504_03871_amd.layer import MoELayer
