@@ -828,7 +828,9 @@ __device__ __forceinline__ void gemm_bf16_tile(const GemmArgs& g, const int vb, 
         }
     }
   } else if constexpr (EPI >= EPI_LIN_NONE) {
-    // Bias, activation and residual on the fp32 sums: eight columns per lane, the residual requested AHEAD row tiles ahead.
+    // Bias, activation and residual on the fp32 sums: eight columns per lane, the residual requested AHEAD row tiles ahead.  Two
+    // roundings, each of a result: y, and the pre-activation where the caller keeps it, in half the bytes for the backward; the
+    // activation works on the sums before that.
     constexpr int NH = TNN / 2, AHEAD = TNN == 4 ? 3 : 4;   // stores per row tile: of 8 rows x 128 bytes, or one of 16 x 64
     typedef Half16<ST> H;
     // (MODE_TN: a weight gradient in the storage type, of the whole of the rows: no bias, no residual, C or C2)

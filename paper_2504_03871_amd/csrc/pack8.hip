@@ -54,8 +54,7 @@ struct Pack8Args {
 
 // Work items are eight adjacent values of a row, four to a block; item i's codes are bytes 8 i .. 8 i + 7 of the plane's, its scale
 // byte i / 4.  DENSE: rows without gaps between them or between their blocks, so that item i is elements 8 i .. 8 i + 7 of the plane
-// and no row has to be known.  A thread takes U items, 256 apart, and requests them all before it uses the first (U = 1 -> the
-// figure here, us: packing two planes of 32768 x 8192 bf16 407 -> see below).
+// and no row has to be known.  A thread takes U items, 256 apart, and requests them all before it uses the first.
 struct Item { long long g; long long row; int c, q; };   // block, row, first column, part of the block
 template <bool DENSE>
 __device__ __forceinline__ Item item_of(const Pack8Args& a, long long i) {
@@ -71,7 +70,8 @@ __device__ __forceinline__ Item item_of(const Pack8Args& a, long long i) {
   return t;
 }
 
-// Four lanes hold a block.  blockIdx.y: plane.
+// Four lanes hold a block.  blockIdx.y: plane.  Bound by HBM: two planes of 32768 x 8192 bf16, 1.07 GB read and 0.55 GB written,
+// 258 us = 6.3 TB/s; with the row of every item found by a division and one item per thread 407.
 template <typename T, int FMT, bool DENSE, bool VEC, int U>
 __global__ __launch_bounds__(256) void pack8_kernel(Pack8Args a) {
   __shared__ int32_t s_range[2 * MOE_MAX_E];
@@ -138,7 +138,8 @@ __global__ __launch_bounds__(256) void unpack8_kernel(Pack8Args a) {
   }
 }
 
-// Packed pre-activations -> every saved plane: A | gelu(A), or G | U | silu(G) U.
+// Packed pre-activations -> every saved plane: A | gelu(A), or G | U | silu(G) U.  Bound by HBM's writes: 0.55 GB read, 1.61 GB
+// written, 413 us = 5.2 TB/s, the rate of a fill.
 template <typename T, int FMT, bool SWIGLU, bool DENSE, int U>
 __global__ __launch_bounds__(256) void restore8_kernel(Pack8Args a) {
   __shared__ int32_t s_range[2 * MOE_MAX_E];
@@ -188,7 +189,8 @@ __global__ __launch_bounds__(256) void restore8_kernel(Pack8Args a) {
   }
 }
 
-// Items per thread: one where the chip has fewer than it can hold at a time.
+// Items per thread: one where the chip has fewer than it can hold at a time.  (Then a launch is all there is: 300 x 516 fp32, pack 3.2,
+// unpack 2.7 us.)
 constexpr int PACK_U = 4;
 static dim3 pack_grid(long long items, int u, int planes) { return dim3((unsigned)((items + 256 * u - 1) / (256 * u)), planes); }
 constexpr long long PACK_FEW = 256 * 2048;

@@ -428,6 +428,8 @@ __device__ __forceinline__ float softmax_sum(const float (&l)[V], float top) {
   return row_sum(z);
 }
 
+// The choice.  Bound by its instructions (vector ALUs busy 95 % of the cycles), not by the one pass over the logits: 32768 tokens, 8 of 256 experts, four of eight groups,
+// 23.6 us for 36 MB; 8191 tokens, 6 of 64, 4.9 us, and a call of four tokens 5.5, both the length of one wave's work.
 template <int V, bool BY_LOGIT>
 __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a) {
   __shared__ float keys[SC_ROWS][SC_LANES * V];
@@ -480,6 +482,8 @@ __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a) {
 }
 
 // Gradient of the logits.  The slots' gradients meet their experts in an LDS row, which leaves in pieces of 256 bytes.
+// Bound by HBM: 32768 tokens, 8 of 256 experts, 33.6 MB written and 19 MB read (the chosen logits' lines), 8.3 us = 6.3 TB/s; over
+// all experts, 8191 tokens of 64, 3.8 us.
 template <int V>
 __global__ __launch_bounds__(256) void score_bwd_kernel(ScoreArgs a, const float* __restrict__ d_topk_w, float* __restrict__ d_logits) {
   constexpr int P = V < 4 ? V : 4, N = V / P;   // lane i has N pieces of P experts, piece j from (16 j + i) P on
