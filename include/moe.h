@@ -354,7 +354,7 @@ MOE_API int moe_layer_expert_dw(const moe_cfg* cfg, const moe_layer_bufs* const*
  * finite number.  A slot for which no expert is left has topk_idx = -1 and topk_w = 0, which every later call treats as a dropped
  * assignment.  (A group with fewer than group_rank experts that can be chosen scores minus infinity.)
  * The order is that of double precision scores: where single precision cannot tell two keys apart they are compared in double.
- * The product with Wr is moe_route's; bias is added to the logits as there.  If logits_in is given the product is skipped, x and Wr
+ * The product with Wr is moe_route's, for few tokens one of its own (fp32 sums in another order); bias is added to the logits as there.  If logits_in is given the product is skipped, x and Wr
  * may be NULL and logits_out is not written.  1 <= groups <= 16 and divides E; group_rank <= E / groups; top_groups <= groups and
  * top_groups * (E / groups) >= k, else MOE_ERR_BAD_SHAPE.  scale must be finite.
  */

@@ -97,6 +97,8 @@ int launch_combine_bwd(const moe_cfg*, const void*, const void*, const float*, c
 int launch_wr_transpose(const moe_cfg*, const float*, float*, hipStream_t);
 int launch_score(const moe_cfg*, const moe_score*, const float*, const float*, int32_t*, float*, hipStream_t);
 int launch_score_bwd(const moe_cfg*, const moe_score*, const float*, const int32_t*, const float*, float*, hipStream_t);
+bool score_logits_few(const moe_cfg*);
+int launch_score_logits(const moe_cfg*, const void*, const float*, const float*, float*, hipStream_t);
 int launch_score_dx(const moe_cfg*, const moe_score*, const int32_t*, const float*, const float*, void*, hipStream_t);
 bool input_grad_has_dwr(const moe_cfg*);
 int launch_input_grad(const moe_cfg*, const moe_layer_bufs*, const float*, float*, bool, hipStream_t);
@@ -373,7 +375,8 @@ int moe_route_scored(const moe_cfg* cfg, const moe_score* score, const void* x, 
   if (logits_in == nullptr) {   // the gate's product; what its own selection writes is overwritten
     void* wfrag = ws != nullptr ? static_cast<char*>(ws) + ws_layout(cfg).route_wrt : nullptr;
     ProfScope ps(cfg, MOE_PROF_ROUTE, s);
-    CHECK(launch_route(cfg, x, Wr, bias, nullptr, logits_out, topk_idx, topk_w, wfrag, s));
+    if (score_logits_few(cfg)) CHECK(launch_score_logits(cfg, x, Wr, bias, logits_out, s));
+    else CHECK(launch_route(cfg, x, Wr, bias, nullptr, logits_out, topk_idx, topk_w, wfrag, s));
     logits_in = logits_out;
   }
   return launch_score(cfg, score, logits_in, balance, topk_idx, topk_w, s);

@@ -656,6 +656,51 @@ __global__ __launch_bounds__(256) void score_dx_all_kernel(const float* __restri
     }
 }
 
+// logits = x Wr + bias for few tokens: a block takes all of d for 16 experts and up to TT tokens.  A thread has four adjacent experts
+// and every 256th run of four rows of Wr, so that d is walked in d / 1024 steps; its sums meet in the wave, then in LDS, in order.
+// Bound by the latency of those steps: one token, d 4096, 256 experts, 4.2 MB of weights, the call with the choice 10 us.
+constexpr int SL_COLS = 16, SL_THREADS = 1024;
+template <typename T, int TT>
+__global__ __launch_bounds__(SL_THREADS) void score_logits_kernel(const T* __restrict__ x, const float* __restrict__ Wr,
+                                                                  const float* __restrict__ bias, float* __restrict__ logits, int Tn, int d, int E) {
+  constexpr int WAVES = SL_THREADS / WAVE;
+  __shared__ float part[WAVES][4][TT * 4 + 1];
+  const int g = threadIdx.x & 3, q = threadIdx.x >> 2, e = blockIdx.x * SL_COLS + g * 4, t0 = blockIdx.y * TT;
+  f32x4 acc[TT] = {};
+  if (e < E)
+#pragma unroll 2
+    for (int c = q * 4; c < d; c += SL_THREADS) {
+      f32x4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const f32x4*>(Wr + (size_t)(c + i) * E + e);
+#pragma unroll
+      for (int s = 0; s < TT; ++s) {
+        T v[4];
+        __builtin_memcpy(v, x + (size_t)min(t0 + s, Tn - 1) * d + c, sizeof v);   // tokens past the batch repeat the last one
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = to_f32(v[i]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[s][j] = fmaf(f, w[i][j], acc[s][j]);
+        }
+      }
+    }
+#pragma unroll
+  for (int s = 0; s < TT; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v = acc[s][j];
+      for (int lanes = 4; lanes < WAVE; lanes <<= 1) v += __shfl_xor(v, lanes, WAVE);
+      if ((threadIdx.x & (WAVE - 1)) < 4) part[threadIdx.x / WAVE][g][s * 4 + j] = v;
+    }
+  __syncthreads();
+  const int s = threadIdx.x / SL_COLS, col = threadIdx.x % SL_COLS, to = blockIdx.x * SL_COLS + col;
+  if (s >= TT || t0 + s >= Tn || to >= E) return;
+  float sum = bias != nullptr ? bias[to] : 0.f;
+  for (int w = 0; w < WAVES; ++w) sum += part[w][col >> 2][s * 4 + (col & 3)];
+  logits[(size_t)(t0 + s) * E + to] = sum;
+}
+
 static int per_lane(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : E <= 64 ? 4 : E <= 128 ? 8 : 16; }
 static int group_lanes(int E, int groups) {
   const int size = E / groups, n = size / per_lane(E);
@@ -717,6 +762,29 @@ int launch_score_dx(const moe_cfg* c, const moe_score* sc, const int32_t* idx, c
   if (c->dtype == MOE_DTYPE_BF16) return launch_score_dx_for(c, all, idx, d_logits, WrT, (bf16*)dx, s);
   if (c->dtype == MOE_DTYPE_F16) return launch_score_dx_for(c, all, idx, d_logits, WrT, (f16*)dx, s);
   return launch_score_dx_for(c, all, idx, d_logits, WrT, (float*)dx, s);
+}
+
+template <typename T>
+static int launch_score_logits_for(const moe_cfg* c, const T* x, const float* Wr, const float* bias, float* logits, hipStream_t s) {
+  const int tt = c->T == 1 ? 1 : c->T <= 4 ? 4 : 8;
+  const dim3 grid((c->E + SL_COLS - 1) / SL_COLS, (c->T + tt - 1) / tt);
+  if (tt == 1) score_logits_kernel<T, 1><<<grid, SL_THREADS, 0, s>>>(x, Wr, bias, logits, c->T, c->d_model, c->E);
+  else if (tt == 4) score_logits_kernel<T, 4><<<grid, SL_THREADS, 0, s>>>(x, Wr, bias, logits, c->T, c->d_model, c->E);
+  else score_logits_kernel<T, 8><<<grid, SL_THREADS, 0, s>>>(x, Wr, bias, logits, c->T, c->d_model, c->E);
+  return launch_status();
+}
+// Against moe_route's product (E > 32: a block per 16 or more tokens that walks all of d), the whole call, T x d x E, us, this | that:
+// bf16 1 x 4096 x 256 10 | 73, 256 x 4096 x 256 35 | 82, 512 x 1024 x 64 14 | 19, 1024 x 1024 x 64 24 | 19, 512 x 1024 x 256 43 | 45;
+// fp32 4 x 4096 x 64 12 | 149, 1024 x 1024 x 256 76 | 95, 2048 x 1024 x 256 144 | 98; up to 32 experts (another kernel there)
+// 4 x 4096 x 32 12 | 15, 16 x 4096 x 32 17 | 16, 64 x 1024 x 8 13 | 11.
+bool score_logits_few(const moe_cfg* c) {
+  const bool f32 = c->dtype == MOE_DTYPE_F32;
+  return c->E % 4 == 0 && (c->T <= 4 || (c->E > 32 && (long long)c->T * c->E <= (f32 ? 1 << 18 : 1 << 16) && (f32 || c->T <= 512)));
+}
+int launch_score_logits(const moe_cfg* c, const void* x, const float* Wr, const float* bias, float* logits, hipStream_t s) {
+  if (c->dtype == MOE_DTYPE_BF16) return launch_score_logits_for(c, (const bf16*)x, Wr, bias, logits, s);
+  if (c->dtype == MOE_DTYPE_F16) return launch_score_logits_for(c, (const f16*)x, Wr, bias, logits, s);
+  return launch_score_logits_for(c, (const float*)x, Wr, bias, logits, s);
 }
 
 }  // namespace moe

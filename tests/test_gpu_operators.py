@@ -193,6 +193,26 @@ def test_scored_routing_from_the_gate_product(dtype, T, d, E, k):
         assert np.all(np.abs(f64(dx) - want) <= half_step(dtype) * np.abs(want) + 8 * math.sqrt(E) * U * size + 2.0 ** -25)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,d,E,k,bias", [(1, 4096, 256, 8, True), (4, 64, 36, 3, False), (9, 1088, 100, 8, True), (3, 2880, 8, 2, False),
+                                          (256, 1024, 256, 8, True), (2, 64, 4, 1, True), (513, 128, 64, 6, False)])
+def test_scored_routing_of_few_tokens(dtype, T, d, E, k, bias):
+    """Product and choice for decode batches and on both sides of the line between the two products."""
+    r = np.random.default_rng(T + d)
+    x, Wr, b = dev(r.normal(0, 1, (T, d)), TD[dtype]), dev(r.normal(0, d ** -0.5, (d, E))), dev(r.normal(0, 0.3, E)) if bias else None
+    cfg, sc = B.make_cfg(T, d, 64, E, k, DT[dtype]), B.make_score(B.SCORE_SIGMOID, 1, 1, 1, 1, 2.5)
+    ws = torch.empty(B.moe_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+    logits, idx, w = torch.full((T, E), 7.0, device=DEV), torch.empty(T, k, dtype=torch.int32, device=DEV), torch.empty(T, k, device=DEV)
+    B.moe_route_scored(cfg, sc, x, Wr, b, None, None, logits, idx, w, ws)
+    ref = f64(x) @ f64(Wr) + (f64(b) if bias else 0)
+    size = np.abs(f64(x)) @ np.abs(f64(Wr)) + 1
+    term = 2.0 ** -17 if dtype != "f32" else 0.0   # the weight as two 16-bit terms, where the matrix cores take it
+    assert np.all(np.abs(f64(logits) - ref) <= (8 * math.sqrt(d) * U + term) * size)
+    ridx, rw = O.route(logits.cpu().numpy(), "sigmoid", k, renorm=1, scale=2.5)
+    assert np.array_equal(idx.cpu().numpy(), ridx)
+    assert np.allclose(f64(w), rw, rtol=60 * U, atol=0)
+
+
 @pytest.mark.parametrize("kind,renorm", [(B.SCORE_SIGMOID, 1), (B.SCORE_SIGMOID, 0), (B.SCORE_SOFTMAX, 0)])
 @pytest.mark.parametrize("T,d,E,k", [(33, 68, 3, 1), (5, 516, 17, 8), (64, 260, 33, 3), (1, 4, 2, 2)])
 def test_scored_input_gradient_odd_sizes(T, d, E, k, kind, renorm):
