@@ -20,7 +20,7 @@ def test_no_product_kernel_spills_registers(tmp_path):
         for line in listing.splitlines():
             if m := re.match(r"[0-9a-f]+ <(\S+)>:", line):
                 name = m[1]
-            elif re.search(r"linear_(rows|f32)|score_kernel|pack8", name):
+            elif re.search(r"linear_(rows|f32|pair|join)|score_(kernel|bwd|dx|logits)|act_bwd|sum_(many_)?rows|pack8|restore8", name):
                 found.add(name)
                 if line.strip().startswith("scratch_"):
                     spilled.add(name)
