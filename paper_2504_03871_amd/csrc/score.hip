@@ -81,19 +81,16 @@ __device__ __forceinline__ void load_row(const float* __restrict__ row, int E, i
 
 // ---- the choice, in single precision ----
 // Keys c (-inf: cannot be chosen) and what they are made of: the largest score plus the largest finite bias.  BY_LOGIT: the scores
-// grow with the logits and nothing is added to them, so the logits themselves are the keys.
+// grow with the logits and nothing is added to them, so the logits themselves are the keys, exact ones (0 is returned); minus
+// zero, which equals zero, becomes it.
 template <int V, bool BY_LOGIT>
 __device__ __forceinline__ float make_keys(const ScoreArgs& a, const float (&l)[V], float row_top, int lane, float (&key)[V]) {
-  float top_s = 0.f, top_b = 0.f;
   if constexpr (BY_LOGIT) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      key[v] = l[v];
-      top_s = fmaxf(top_s, l[v] > -INFINITY ? fabsf(l[v]) : 0.f);
-    }
-    return row_max(top_s);
+    for (int v = 0; v < V; ++v) key[v] = l[v] + 0.f;
+    return 0.f;
   } else {
-    float b[V];
+    float b[V], top_s = 0.f, top_b = 0.f;
     if (a.balance != nullptr) load_row<V>(a.balance, a.E, lane, 0.f, b);
     if (a.softmax) {
       float z = 0.f;
@@ -202,7 +199,9 @@ __device__ __forceinline__ bool restrict_groups(const ScoreArgs& a, float (&key)
 }
 
 // The k + 1 largest keys, best first, to pick_e in LDS (-1: none left), and what is not certain about them: ORDER, keys within `unit`
-// of each other among them; ALL, more than them.
+// of each other among them; ALL, more than them.  Exact keys (BY_LOGIT) have an order that is certain unless they agree but for the
+// bits that the slot takes: what lies far from the choice, a mask of -1e9 say, does not widen a bound.  (32768 tokens, 8 of 256, a
+// twentieth masked so: 11 us; by a bound from the largest logit, under which every token was uncertain, 43.  All logits equal: 42.)
 // Every lane keeps the best DEPTH of its keys in order, with the slot in place of the lowest bits, so that taking the
 // token's best is a step within its 16 lanes and a shift in one of them.  (Going through all V keys per choice: 32768
 // tokens, 8 of 256 experts in 8 groups, 77 us, with every uncertain token in double precision 43; as it is 24.)  A lane whose list runs out while
@@ -223,7 +222,7 @@ __device__ __forceinline__ int row_max(int v) {
   v = max(v, row_ror<4>(v));
   return max(v, row_ror<8>(v));
 }
-template <int V>
+template <int V, bool BY_LOGIT>
 __device__ __forceinline__ int pick_fast(const ScoreArgs& a, const float (&key)[V], int lane, float unit, int* pick_e) {
   constexpr int DEPTH = V < 8 ? V : 8;   // (six: 34.9 us with the gradient instead of 33.1; four: 51.6)
   constexpr int SLOT = V - 1, CLOSED = (int)0x80000000u;   // below any key
@@ -239,14 +238,16 @@ __device__ __forceinline__ int pick_fast(const ScoreArgs& a, const float (&key)[
     best[0] = max(best[0], x);
   }
   bool order = false, edge = false;   // edge: of the last key that is chosen and the first that is not
-  float last = INFINITY;
-  int taken = 0;
+  int last = CLOSED, taken = 0;
+  float last_f = INFINITY;
+  // whether the order of the last key and a key `top` that can be chosen is open (no key has the upper bits of CLOSED)
+  auto near_last = [&](int top) { return BY_LOGIT ? (unsigned)(last ^ top) <= (unsigned)SLOT : !(last_f - from_ordered(top) > unit); };
   for (int j = 0; j <= a.k; ++j) {
     const int top = row_max(best[0]);
-    const float f = from_ordered(top);
-    edge = top != CLOSED && !(last - f > unit);
+    edge = top != CLOSED && near_last(top);
     order |= edge;
-    last = f;
+    last = top;
+    last_f = from_ordered(top);
     if (lane == __builtin_ctz(row_vote(best[0] == top))) {
       pick_e[j] = top != CLOSED ? lane * V + (top & SLOT) : -1;
       if (top != CLOSED) {
@@ -258,7 +259,7 @@ __device__ __forceinline__ int pick_fast(const ScoreArgs& a, const float (&key)[
     }
   }
   const int top = row_max(best[0]);
-  const bool beyond = edge && top != CLOSED && !(last - from_ordered(top) > unit);
+  const bool beyond = edge && top != CLOSED && near_last(top);
   if (row_vote(beyond || (V > DEPTH && taken == DEPTH))) return ALL;
   return order ? ORDER : CERTAIN;
 }
@@ -447,11 +448,13 @@ __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a) {
     // good to 2^-24 of itself, which x e^-x <= 0.37 turns into less than 2^-25 of the largest score; the exponential, the
     // sum and the reciprocal add 2^-22 at most, the bias 2^-24 of the key; twice, for two keys: 2^-20.8, 5.6e-7, of the largest
     // score and bias; for two sums of two, with their own roundings, three times that.  The slot's four bits change
-    // a key by up to 15 steps of at most 2^-23 of it, two keys by 30: 4.2e-6 in all.
+    // a key by up to 15 steps of at most 2^-23 of it, two keys by 30: 4.2e-6 in all.  Next to zero steps stay as they are: a
+    // sigmoid below 2^-126 may come out as zero, the slot's bits are 15 steps of 2^-149, which is below 2^-124 for two keys and
+    // below 2^-122 for two sums of two.
     float key[V];
     const float most = make_keys<V, BY_LOGIT>(a, l, top, lane, key);
-    const bool groups_open = a.groups > 1 && restrict_groups<V>(a, key, lane, keys[r], BY_LOGIT ? 0.f : 1.7e-6f * most);
-    open = pick_fast<V>(a, key, lane, 4.2e-6f * most, pick_e[r]);
+    const bool groups_open = a.groups > 1 && restrict_groups<V>(a, key, lane, keys[r], BY_LOGIT ? 0.f : fmaxf(1.7e-6f * most, 0x1p-122f));
+    open = pick_fast<V, BY_LOGIT>(a, key, lane, fmaxf(4.2e-6f * most, 0x1p-124f), pick_e[r]);
     if (groups_open) open = ALL;
     if (!BY_LOGIT && open == ORDER && a.softmax) open = ALL;   // a softmax score takes the sum over all experts
   }

@@ -705,3 +705,67 @@ def test_tensors_must_be_contiguous():
     B.moe_pack8(B.DTYPE_BF16, B.PACK_I8, 8, 40, 64, big[:, :40], codes, scales)          # a view of rows that are 64 apart
     with pytest.raises(ValueError):
         B.moe_pack8(B.DTYPE_BF16, B.PACK_I8, 8, 40, 40, big[:, :40], codes, scales)      # the pitch says something else
+
+
+# ---- choices among keys of zero, next to it and beyond the finite numbers -------------------------------------------
+
+def zero_rows(E, seed):
+    """Rows whose open logits are all zero, of either sign, or a few steps of 2^-149 from it: all experts, runs of 16, scattered ones."""
+    r = np.random.default_rng(seed)
+    rows = []
+    for sign in (0.0, -0.0):
+        rows.append(np.full(E, sign))
+        for first in range(0, E, 16):
+            row = np.full(E, -np.inf)
+            row[first:first + 16] = sign
+            rows.append(row)
+    for share in (0.1, 0.5, 1.0):
+        row = np.where(r.random(E) < 0.5, 0.0, -0.0)
+        rows.append(np.where(r.random(E) < share, row, -np.inf))
+        row = r.integers(-20, 21, E) * 2.0 ** -149
+        rows.append(np.where(r.random(E) < share, row, -np.inf))
+    return np.array(rows, dtype=np.float32)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [3, 16, 17, 18, 19, 33, 36, 39, 64, 72, 129, 144, 256])
+def test_equal_logits_of_zero(E, kind):
+    """Equal logits by ascending expert, whatever their size: a router whose weights start at zero, tokens of zeros."""
+    l = zero_rows(E, E)
+    for k in sorted({1, min(4, E), min(7, E), min(8, E)}):
+        check_route(l, kind, k, None, 1, 1, 1, 1, 1.0)
+    for groups in (2, 3, 4, 8, 16):
+        if E % groups == 0 and E // groups >= 2:
+            top = (groups + 1) // 2
+            for rank in (1, 2):
+                check_route(l, kind, min(8, E // groups * top), None, groups, top, rank, 1, 1.0)
+
+
+@pytest.mark.parametrize("E,groups", [(18, 1), (36, 4), (64, 8), (144, 3), (256, 8)])
+def test_sigmoid_scores_below_the_smallest_fp32_number(E, groups):
+    """Scores that single precision rounds to zero, with a balance of zeros and summed up in groups: equal ones by ascending expert,
+    different ones by their double precision scores (but for scores that are zero there too)."""
+    r = np.random.default_rng(E)
+    l = np.concatenate([np.full((4, E), -100.0), np.full((4, E), -800.0), r.uniform(-140, -86, (24, E)), r.choice([-90.0, -95.0, -800.0, -900.0], (24, E))])
+    l[r.random(l.shape) < 0.2] = -np.inf
+    l[0], l[4] = -100.0, -800.0
+    for rank in (1, 2):
+        for balance in (np.zeros(E, np.float32), None) if groups > 1 and rank == 2 else (np.zeros(E, np.float32),):
+            top = (groups + 1) // 2
+            for k in (1, min(8, E // groups * top)):
+                check_route(l.astype(np.float32), "sigmoid", k, balance, groups, top, rank, 1, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_finite_masks_and_logits_of_any_size(kind):
+    """Experts closed by a large finite number instead of minus infinity: open ones first, then closed ones by ascending expert."""
+    r = np.random.default_rng(7)
+    for E, k, groups, top in ((64, 6, 1, 1), (256, 8, 8, 4), (40, 8, 1, 1)):
+        l = route_inputs(60, E, E, "plain")
+        l[:20][r.random((20, E)) < 0.97] = -1e9
+        l[20:40][r.random((20, E)) < 0.3] = -F32_MAX
+        l[40:, ::3] = np.nextafter(np.float32(0.5), np.float32(1))      # neighbours in single precision, and equal ones
+        l[40:, 1::3] = 0.5
+        l[50:, 2::3] = np.nextafter(np.float32(0.5), np.float32(0))
+        idx = run_route(l, kind, k, None, groups, top, 1, 1, 1.0)[0]
+        assert np.array_equal(idx, O.route(l, kind, k, None, groups, top, 1, 1, 1.0)[0])
