@@ -350,8 +350,8 @@ MOE_API int moe_layer_expert_dw(const moe_cfg* cfg, const moe_layer_bufs* const*
  *   (group_rank 2), and only the top_groups best groups stay (equal scores: lower group);
  *   the k best c among them are chosen, best first, equal values by ascending expert id;
  *   topk_w[t][j] = scale * s_j / (renorm ? sum of the chosen s : 1).
- * An expert whose logit (or balance) is minus infinity or NaN is never chosen; a logit of plus infinity counts as the largest
- * finite number.  A slot for which no expert is left has topk_idx = -1 and topk_w = 0, which every later call treats as a dropped
+ * An expert whose logit (or balance) is minus infinity or NaN is never chosen; a logit or balance of plus infinity counts as the
+ * largest finite number.  A slot for which no expert is left has topk_idx = -1 and topk_w = 0, which every later call treats as a dropped
  * assignment.  (A group with fewer than group_rank experts that can be chosen scores minus infinity.)
  * The order is that of double precision scores: where single precision cannot tell two keys apart they are compared in double.
  * The product with Wr is moe_route's, for few tokens one of its own (fp32 sums in another order); bias is added to the logits as there.  If logits_in is given the product is skipped, x and Wr

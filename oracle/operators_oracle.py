@@ -39,7 +39,7 @@ def route(logits, kind, k, balance=None, groups=1, top_groups=1, rank=1, renorm=
     for t in range(T):
         # without a bias the scores grow with the logits: the logits order the experts, also where scores round to the same number
         by_logit = balance is None and (groups == 1 or rank == 1)
-        key = l[t].copy() if by_logit else s[t] + (0.0 if balance is None else np.asarray(balance, dtype=np.float64))
+        key = l[t].copy() if by_logit else s[t] + (0.0 if balance is None else np.minimum(np.asarray(balance, dtype=np.float64), np.finfo(np.float32).max))
         key[~(l[t] > -np.inf)] = -np.inf
         key[np.isnan(key)] = -np.inf
         if groups > 1:

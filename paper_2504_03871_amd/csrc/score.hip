@@ -55,7 +55,8 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// A logit that takes part: minus infinity and NaN do not, plus infinity counts as the largest number.
+// A logit or a bias that takes part: minus infinity and NaN do not, plus infinity counts as the largest number (so that sums of two
+// keys are numbers or minus infinity).
 __device__ __forceinline__ float usable(float l) { return l > -INFINITY ? fminf(l, 3.4028234663852886e38f) : -INFINITY; }
 
 // lane i's V values of a row of E, `rest` past its end
@@ -80,7 +81,7 @@ __device__ __forceinline__ void load_row(const float* __restrict__ row, int E, i
 }
 
 // ---- the choice, in single precision ----
-// Keys c (-inf: cannot be chosen) and what they are made of: the largest score plus the largest finite bias.  BY_LOGIT: the scores
+// Keys c (-inf: cannot be chosen) and what they are made of: the largest score plus the largest bias.  BY_LOGIT: the scores
 // grow with the logits and nothing is added to them, so the logits themselves are the keys, exact ones (0 is returned); minus
 // zero, which equals zero, becomes it.
 template <int V, bool BY_LOGIT>
@@ -112,13 +113,15 @@ __device__ __forceinline__ float make_keys(const ScoreArgs& a, const float (&l)[
     if (a.balance != nullptr) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const float mag = fabsf(b[v]);
-        top_b = fmaxf(top_b, mag < INFINITY ? mag : 0.f);
-        key[v] += b[v] > -INFINITY ? b[v] : -INFINITY;   // (not a NaN)
+        const bool open = b[v] > -INFINITY;   // usable(), with one selection for both
+        const float u = fminf(b[v], 3.4028234663852886e38f);
+        top_b = fmaxf(top_b, open ? fabsf(u) : 0.f);
+        key[v] = l[v] > -INFINITY && open ? key[v] + u : -INFINITY;
       }
-    }
+    } else {
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? key[v] : -INFINITY;
+      for (int v = 0; v < V; ++v) key[v] = l[v] > -INFINITY ? key[v] : -INFINITY;
+    }
     return row_max(top_s) + row_max(top_b);
   }
 }
@@ -270,7 +273,7 @@ template <bool BY_LOGIT>
 __device__ __forceinline__ void settle(const ScoreArgs& a, int lane, const float* logits, int* pick_e) {
   const int e = lane <= a.k ? pick_e[lane] : -1;
   double c = e >= 0 ? (double)logits[e] : (double)-INFINITY;
-  if (!BY_LOGIT && e >= 0) c = 1.0 / (1.0 + exp(-c)) + (a.balance != nullptr ? (double)a.balance[e] : 0.0);
+  if (!BY_LOGIT && e >= 0) c = 1.0 / (1.0 + exp(-c)) + (a.balance != nullptr ? (double)usable(a.balance[e]) : 0.0);
   int rank = 0;
   for (int i = 0; i <= a.k; ++i) {
     const double o = __shfl(c, i, SC_LANES);
@@ -335,8 +338,8 @@ __device__ __forceinline__ void choose_exact(const ScoreArgs& a, int t, int* pic
     }
 #pragma unroll
     for (int v = 0; v < VW; ++v) {
-      if (a.balance != nullptr && e0 + v < a.E) key[v] += (double)a.balance[e0 + v];
-      key[v] = (l[v] > -INFINITY && key[v] > (double)-INFINITY) ? key[v] : (double)-INFINITY;
+      if (a.balance != nullptr && e0 + v < a.E) key[v] += (double)usable(a.balance[e0 + v]);
+      key[v] = l[v] > -INFINITY ? key[v] : (double)-INFINITY;
     }
   }
   if (a.groups > 1) {

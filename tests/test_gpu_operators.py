@@ -769,3 +769,27 @@ def test_finite_masks_and_logits_of_any_size(kind):
         l[50:, 2::3] = np.nextafter(np.float32(0.5), np.float32(0))
         idx = run_route(l, kind, k, None, groups, top, 1, 1, 1.0)[0]
         assert np.array_equal(idx, O.route(l, kind, k, None, groups, top, 1, 1, 1.0)[0])
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k,groups,top,rank", [(64, 4, 1, 1, 1), (256, 8, 1, 1, 1), (64, 6, 8, 3, 2), (36, 3, 4, 2, 2), (64, 4, 4, 1, 1), (40, 8, 5, 3, 2)])
+def test_balance_of_any_size(E, k, groups, top, rank, kind):
+    """Plus infinity counts as the largest number: such experts come first, by ascending expert, and a group whose others are closed
+    still scores minus infinity in a sum of two.  Finite numbers up to the largest."""
+    r = np.random.default_rng(E + k)
+    for trial in range(12):
+        l = route_inputs(40, E, trial, "masked" if trial % 2 else "plain")
+        bal = np.where(r.random(E) < 0.5, 0.01, -0.02).astype(np.float32)
+        bal[r.choice(E, max(2, E // 8), replace=False)] = np.inf if trial % 3 else F32_MAX
+        if trial % 3 != 1:  # else no finite number is large
+            bal[r.choice(E, 2, replace=False)] = -F32_MAX
+        if trial % 4 == 3:
+            bal[r.choice(E, E // 3, replace=False)] = -np.inf
+        if trial >= 8:      # the first group: one expert that can be chosen, with a balance of plus infinity
+            size = E // groups
+            l[:, :size], bal[0] = -np.inf, np.inf
+            l[:, 0] = 0.5
+        idx, w, _, _ = run_route(l, kind, k, bal, groups, top, rank, 1, 1.0)
+        ridx, rw = O.route(l, kind, k, np.minimum(bal, np.float32(F32_MAX)), groups, top, rank, 1, 1.0)
+        assert np.array_equal(idx, ridx), trial
+        assert np.allclose(w, rw, rtol=100 * U, atol=0)
