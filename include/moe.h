@@ -353,10 +353,15 @@ MOE_API int moe_layer_expert_dw(const moe_cfg* cfg, const moe_layer_bufs* const*
  * An expert whose logit (or balance) is minus infinity or NaN is never chosen; a logit or balance of plus infinity counts as the
  * largest finite number.  A slot for which no expert is left has topk_idx = -1 and topk_w = 0, which every later call treats as a dropped
  * assignment.  (A group with fewer than group_rank experts that can be chosen scores minus infinity.)
- * The order is that of double precision scores: where single precision cannot tell two keys apart they are compared in double.
- * The product with Wr is moe_route's, for few tokens one of its own (fp32 sums in another order); bias is added to the logits as there.  If logits_in is given the product is skipped, x and Wr
- * may be NULL and logits_out is not written.  1 <= groups <= 16 and divides E; group_rank <= E / groups; top_groups <= groups and
- * top_groups * (E / groups) >= k, else MOE_ERR_BAD_SHAPE.  scale must be finite.
+ * The order of the c, and of groups, is that of double precision: where single precision cannot tell two apart they are compared in
+ * double, and c that are equal there are equal.  Without a balance (NULL), where no c are added up (one group, or group_rank 1),
+ * the logits themselves order the experts and groups: a score grows with its logit, also where double precision rounds two scores to
+ * the same number (sigmoids of 40 and 60 are both 1, softmax scores far below the largest both 0).  So NULL and a balance of zeros
+ * may choose differently among such experts.
+ * The product with Wr is moe_route's, for few tokens one of its own (fp32 sums in another order); bias is added to the logits as
+ * there.  If logits_in is given the product is skipped, x and Wr may be NULL and logits_out is not written.  1 <= groups <= 16 and
+ * divides E; group_rank <= E / groups; top_groups <= groups and top_groups * (E / groups) >= k, else MOE_ERR_BAD_SHAPE.  scale must
+ * be finite.
  */
 #define MOE_MAX_GROUPS 16
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
@@ -377,7 +382,8 @@ MOE_API int moe_route_scored(const moe_cfg* cfg, const moe_score* score, const v
  * dx += d_logits Wr^T (NULL: skipped).  `logits` are those the choice was made on.  ws is needed for dWr and dx only.
  * With p_j = topk_w[j] / scale and D = sum_j p_j d_topk_w[j], d_logits of the chosen experts is, renorm: scale p_j (dw_j - D),
  * for sigmoid times 1 - s_j; else sigmoid: scale s_j (1 - s_j) dw_j; zero for the others.  Softmax without renorm has a gradient for
- * every expert: scale s_e ([e chosen] dw_e - D).  Experts that cannot be chosen get zero.
+ * every expert whose score takes part in the sum: scale s_e ([e chosen] dw_e - D).  Experts with a logit of minus infinity or NaN get
+ * zero.
  */
 MOE_API int moe_route_scored_bwd(const moe_cfg* cfg, const moe_score* score, const void* x, const float* Wr, const float* logits,
                      const int32_t* topk_idx, const float* d_topk_w, float* d_logits, float* dWr, void* dx, int32_t accumulate,

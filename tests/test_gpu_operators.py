@@ -793,3 +793,22 @@ def test_balance_of_any_size(E, k, groups, top, rank, kind):
         ridx, rw = O.route(l, kind, k, np.minimum(bal, np.float32(F32_MAX)), groups, top, rank, 1, 1.0)
         assert np.array_equal(idx, ridx), trial
         assert np.allclose(w, rw, rtol=100 * U, atol=0)
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_order_where_scores_round_to_the_same_number(kind):
+    """Without a balance the logits order the experts, with one (of zeros too) the double precision keys, equal ones by expert."""
+    T, E, k = 48, 64, 6
+    r = np.random.default_rng(4)
+    l = (r.normal(0, 1, (T, E)) + (60 if kind == "sigmoid" else -900)).astype(np.float32)   # sigmoids of exactly 1, softmax scores of exactly 0
+    if kind == "softmax":
+        l[:, 5] = 0.0
+    by_logit = np.argsort(-l, axis=1, kind="stable")[:, :k]
+    by_score = np.tile(np.arange(k), (T, 1))
+    if kind == "softmax":
+        by_score[:, 0], by_score[:, 1:] = 5, np.arange(k - 1)
+    for groups, top in ((1, 1), (4, 4)):
+        for rank in (1, 2):
+            logits_decide = groups == 1 or rank == 1
+            assert np.array_equal(run_route(l, kind, k, None, groups, top, rank, 1, 1.0)[0], by_logit if logits_decide else by_score)
+            assert np.array_equal(run_route(l, kind, k, np.zeros(E, np.float32), groups, top, rank, 1, 1.0)[0], by_score)
