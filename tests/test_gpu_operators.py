@@ -812,3 +812,14 @@ def test_order_where_scores_round_to_the_same_number(kind):
             logits_decide = groups == 1 or rank == 1
             assert np.array_equal(run_route(l, kind, k, None, groups, top, rank, 1, 1.0)[0], by_logit if logits_decide else by_score)
             assert np.array_equal(run_route(l, kind, k, np.zeros(E, np.float32), groups, top, rank, 1, 1.0)[0], by_score)
+
+
+def test_pack_scales_at_the_largest_element():
+    """The scale doubles where the largest magnitude would saturate: above 448 (e4m3), from 127.5 64ths on (which would round to 128)."""
+    for fmt, most, up in (("e4m3", 448.0, np.nextafter(np.float32(448), np.float32(500))), ("i8", np.nextafter(np.float32(127.5 / 64), np.float32(0)), 127.5 / 64)):
+        v = torch.zeros(2, 32, device=DEV)
+        v[0, 3], v[1, 3] = float(most), float(up)
+        codes, scales = (torch.empty(m, dtype=torch.uint8, device=DEV) for m in B.moe_pack8_bytes(2, 32))
+        B.moe_pack8(B.DTYPE_F32, FMT[fmt], 2, 32, 32, v, codes, scales)
+        assert scales.tolist() == [127, 128]
+        assert codes.view(2, 32)[:, 3].tolist() == ([0x7e, 0x76] if fmt == "e4m3" else [127, 64])
