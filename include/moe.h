@@ -395,8 +395,8 @@ MOE_API int moe_route_scored_bwd(const moe_cfg* cfg, const moe_score* score, con
  * (MOE_PACK_E4M3) or a two's complement number of 64ths (MOE_PACK_I8); the MXFP8 and MXINT8 formats of the OCP microscaling
  * specification.  The scale is the smallest from 2^-127 to 2^127 with which the block's largest magnitude m does not saturate: e4m3,
  * m <= 448 times the scale; numbers of 64ths, m < 127.5 / 64 times it, which is what rounds to the largest element 127 / 64 (next
- * to 2^128 they saturate).  Codes are rounded to nearest, ties to even.  A block with an infinity or NaN gets scale 255 and unpacks to NaN.  Unpacked values are clamped
- * to the largest finite number of their type.
+ * to 2^128 they saturate).  Codes are rounded to nearest, ties to even.  A block with an infinity or NaN gets scale 255 and unpacks to NaN, as
+ * the NaN codes of e4m3 do, which packing does not write.  Unpacked values are clamped to the largest finite number of their type.
  * moe_pack8 / moe_unpack8: any dense matrix of `rows` rows and `width` columns of storage type `dtype`, `pitch` (>= width)
  * elements from row to row; rows that start at multiples of 16 bytes are moved 16 bytes at a time.  rows * pitch <= 2^40.
  */

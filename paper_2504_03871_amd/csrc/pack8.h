@@ -60,7 +60,8 @@ template <> __device__ __forceinline__ float largest_finite<float>() { return 3.
 template <> __device__ __forceinline__ float largest_finite<bf16>() { return 3.3895313892515355e38f; }
 template <> __device__ __forceinline__ float largest_finite<f16>() { return 65504.f; }
 
-// What eight codes stand for, none beyond T's largest finite number (a value that was rounded up may be).
+// What eight codes stand for, none beyond T's largest finite number (a value that was rounded up may be).  The NaN codes of e4m3,
+// which encode8 does not write but another program may, stay NaN.
 template <typename T, int FMT>
 __device__ __forceinline__ void decode8(const uint2& code, unsigned scale, float (&v)[8]) {
   const unsigned w[2] = {code.x, code.y};
@@ -79,7 +80,8 @@ __device__ __forceinline__ void decode8(const uint2& code, unsigned scale, float
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float x = __builtin_amdgcn_ldexpf(s[j], e), m = largest_finite<T>();
-      v[4 * h + j] = scale == 255u ? __uint_as_float(0x7fc00000u) : fminf(fmaxf(x, -m), m);
+      const float y = FMT == MOE_PACK_E4M3 && x != x ? x : fminf(fmaxf(x, -m), m);
+      v[4 * h + j] = scale == 255u ? __uint_as_float(0x7fc00000u) : y;
     }
   }
 }

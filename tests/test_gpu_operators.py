@@ -823,3 +823,27 @@ def test_pack_scales_at_the_largest_element():
         B.moe_pack8(B.DTYPE_F32, FMT[fmt], 2, 32, 32, v, codes, scales)
         assert scales.tolist() == [127, 128]
         assert codes.view(2, 32)[:, 3].tolist() == ([0x7e, 0x76] if fmt == "e4m3" else [127, 64])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_unpack_of_every_code(dtype, fmt):
+    """Codes from elsewhere too: e4m3's two NaN codes, which pack never writes, -128 64ths, every code under scales of any size."""
+    scales = torch.tensor([0, 1, 60, 118, 127, 135, 200, 246, 254, 255], dtype=torch.uint8)
+    codes = torch.arange(256, dtype=torch.int32).to(torch.uint8).repeat(len(scales), 1)
+    n = B.moe_pack8_bytes(len(scales), 256)
+    assert n == (codes.numel(), len(scales) * 8)
+    out = torch.empty(len(scales), 256, dtype=TD[dtype], device=DEV)
+    B.moe_unpack8(DT[dtype], FMT[fmt], len(scales), 256, 256, codes.to(DEV), scales.repeat_interleave(8).to(DEV), out)
+    value = codes.view(torch.int8).double() / 64
+    if fmt == "e4m3":
+        a = codes.long() & 127
+        m, e = (a & 7).double(), (a >> 3).double()
+        value = torch.where(a < 8, m * 2.0 ** -9, (8 + m) * torch.exp2(e - 10)) * torch.where(codes > 127, -1.0, 1.0)
+        value = torch.where(a == 127, math.nan, value)
+    most = torch.finfo(TD[dtype]).max
+    want = torch.clamp(value * torch.exp2(scales.double() - 127)[:, None], -most, most)
+    want[scales == 255] = math.nan
+    got = out.cpu()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(torch.nan_to_num(got.double()), torch.nan_to_num(want.to(TD[dtype]).double()))
