@@ -433,7 +433,8 @@ MOE_API int moe_saved_restore8(const moe_cfg* cfg, int32_t fmt, const void* code
  * type (accumulate must be 0).
  * Shapes: T >= 0 (0: fp32 gradients are left as they are or zeroed); d_in, d_out multiples of 64 (16-bit) or 4 (fp32), and
  * up to 2^20, and d_in * d_out * 4 < 2^32; T <= 2^24.
- * `ws` holds moe_linear_workspace_bytes and is free again when the call is done.
+ * `ws` holds moe_linear_workspace_bytes, which does for either call, and is free again when the call is done.  The forward alone, for
+ * inference, needs moe_linear_fwd_workspace_bytes: sums of K parts, 256 bytes where the product has none.
  */
 enum { MOE_ACT_NONE = 2 };   /* moe_linear only */
 typedef struct moe_linear {
@@ -444,6 +445,7 @@ typedef struct moe_linear {
   int32_t grad;       /* MOE_DTYPE_F32 or dtype */
 } moe_linear;
 MOE_API int moe_linear_workspace_bytes(const moe_linear* lin, size_t* bytes);
+MOE_API int moe_linear_fwd_workspace_bytes(const moe_linear* lin, size_t* bytes);
 MOE_API int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,
                    const void* residual, void* pre, void* pre_b, void* y, void* ws, size_t ws_bytes, void* stream);
 MOE_API int moe_linear_bwd(const moe_linear* lin, const void* dy, const void* x, const void* W, const void* Wb, const void* pre,

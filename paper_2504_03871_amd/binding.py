@@ -24,7 +24,7 @@ SYMBOLS = ("moe_error_string", "moe_last_hip_error", "moe_workspace_bytes", "moe
            "moe_route_bwd", "moe_layer_fwd", "moe_layer_bwd", "moe_layer_bwd_inputs_ws_bytes", "moe_layer_bwd_inputs",
            "moe_layer_bwd_inputs_room_bytes", "moe_layer_bwd_inputs_in",
            "moe_layer_expert_dw", "moe_route_scored", "moe_route_scored_bwd", "moe_pack8_bytes", "moe_pack8", "moe_unpack8",
-           "moe_saved_pack8_bytes", "moe_saved_pack8", "moe_saved_restore8", "moe_linear_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
+           "moe_saved_pack8_bytes", "moe_saved_pack8", "moe_saved_restore8", "moe_linear_workspace_bytes", "moe_linear_fwd_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
 
 PROF = {"gemm1_fwd": 0, "gemm2_fwd": 1, "dh_bwd": 2, "dw2_bwd": 3, "dw1_bwd": 4, "dx_bwd": 5, "gather": 6,
         "combine": 7, "combine_bwd": 8, "route": 9}
@@ -109,6 +109,7 @@ def lib():
             "moe_saved_pack8": [cfgp, i32] + [p] * 8,
             "moe_saved_restore8": [cfgp, i32] + [p] * 8,
             "moe_linear_workspace_bytes": [ctypes.POINTER(MoeLinear), ctypes.POINTER(sz)],
+            "moe_linear_fwd_workspace_bytes": [ctypes.POINTER(MoeLinear), ctypes.POINTER(sz)],
             "moe_linear_fwd": [ctypes.POINTER(MoeLinear)] + [p] * 10 + [sz, p],
             "moe_linear_bwd": [ctypes.POINTER(MoeLinear)] + [p] * 14 + [i32, p, sz, p],
             "moe_asymea_plan": [i32] * 4 + [ctypes.c_double] * 3 + [i32, i32, ctypes.POINTER(i32)],
@@ -397,8 +398,16 @@ def make_linear(T, d_in, d_out, dtype=DTYPE_BF16, act=ACT_NONE, pre=PACK_NONE, g
 
 
 def moe_linear_workspace_bytes(lin) -> int:
+    """For moe_linear_fwd and moe_linear_bwd."""
     n = ctypes.c_size_t(0)
     _check("moe_linear_workspace_bytes", lib().moe_linear_workspace_bytes(ctypes.byref(lin), ctypes.byref(n)))
+    return n.value
+
+
+def moe_linear_fwd_workspace_bytes(lin) -> int:
+    """For moe_linear_fwd alone (inference)."""
+    n = ctypes.c_size_t(0)
+    _check("moe_linear_fwd_workspace_bytes", lib().moe_linear_fwd_workspace_bytes(ctypes.byref(lin), ctypes.byref(n)))
     return n.value
 
 

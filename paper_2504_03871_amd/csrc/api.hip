@@ -494,6 +494,13 @@ int moe_linear_workspace_bytes(const moe_linear* lin, size_t* bytes) {
   return MOE_OK;
 }
 
+int moe_linear_fwd_workspace_bytes(const moe_linear* lin, size_t* bytes) {
+  CHECK(check_linear(lin));
+  REQUIRE(bytes);
+  *bytes = linear_plan(lin).fwd_total;
+  return MOE_OK;
+}
+
 int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,
                    const void* residual, void* pre, void* pre_b, void* y, void* ws, size_t ws_bytes, void* stream) {
   CHECK(check_linear(lin));
@@ -505,7 +512,7 @@ int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, const vo
   if (lin->act == MOE_ACT_NONE && pre != nullptr) return MOE_ERR_BAD_DTYPE;
   if (two && (pre == nullptr) != (pre_b == nullptr)) return MOE_ERR_NULL;
   ALIGNED(x); ALIGNED(W); ALIGNED(Wb); ALIGNED(bias); ALIGNED(bias_b); ALIGNED(residual); ALIGNED(pre); ALIGNED(pre_b); ALIGNED(y); ALIGNED(ws);
-  const size_t need = linear_plan(lin).total;
+  const size_t need = linear_plan(lin).fwd_total;
   if (need > 0) REQUIRE(ws);
   if (ws_bytes < need) return MOE_ERR_WORKSPACE;
   return launch_linear_fwd(lin, x, W, Wb, bias, bias_b, residual, pre, pre_b, y, ws, (hipStream_t)stream);

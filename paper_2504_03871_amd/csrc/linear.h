@@ -47,7 +47,8 @@ struct LinearPlan {
   int segs, seg;      // ... segments of the tokens, rows of one
   bool dw_direct;     // ... written by the product itself
   bool pair;          // both gradients in one launch
-  size_t dz, db, split, dw, total;   // workspace: byte offsets of the backward's regions; the forward has it to itself
+  size_t dz, db, split, dw, total;   // the backward's workspace: byte offsets of its regions, all of it
+  size_t fwd_total;                  // the forward's, which it has to itself
 };
 LinearPlan linear_plan(const moe_linear* c);
 int launch_linear_fwd(const moe_linear* c, const void* x, const void* W, const void* Wb, const void* bias, const void* bias_b,

@@ -186,7 +186,8 @@ LinearPlan linear_plan(const moe_linear* c) {
   off += align_up(half ? cut_bytes(p.dx, 1) : cut_bytes_f32(p.dx, c->T, c->d_in, 1), 256);
   p.dw = off;
   if (!p.dw_direct) off += align_up((size_t)mats * p.segs * c->d_in * N * 4, 256);
-  p.total = std::max(align_up(fwd, 256), off);
+  p.fwd_total = c->T > 0 ? std::max(align_up(fwd, 256), (size_t)256) : 0;   // whole products need none; a call without one is a mistake still
+  p.total = std::max(p.fwd_total, off);
   return p;
 }
 

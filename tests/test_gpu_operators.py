@@ -847,3 +847,16 @@ def test_unpack_of_every_code(dtype, fmt):
     got = out.cpu()
     assert torch.equal(got.isnan(), want.isnan())
     assert torch.equal(torch.nan_to_num(got.double()), torch.nan_to_num(want.to(TD[dtype]).double()))
+
+
+@pytest.mark.parametrize("dtype,T,d,n,act", [("bf16", 16, 4096, 256, "gelu"), ("f16", 300, 2048, 320, "swiglu"), ("bf16", 700, 256, 512, "none"),
+                                             ("f32", 70, 1024, 132, "swiglu"), ("f32", 300, 64, 100, "gelu")])
+def test_linear_forward_in_its_own_workspace(dtype, T, d, n, act):
+    c = linear_case(T, d, n, dtype, act)
+    whole, _ = run_fwd(c, keep=False)
+    lin = B.make_linear(T, d, n, DT[dtype], ACTS[act])
+    need = B.moe_linear_fwd_workspace_bytes(lin)
+    ws = torch.full((need + 4096,), 0xAB, dtype=torch.uint8, device=DEV)
+    y = torch.full_like(whole, 77.0)
+    B.moe_linear_fwd(lin, c["x"], *two(c["W"]), *two(c["b"]), c["r"], None, None, y, ws, ws_bytes=need)
+    assert torch.equal(y, whole) and (ws[need:] == 0xAB).all()

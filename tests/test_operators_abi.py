@@ -134,3 +134,21 @@ def test_linear_widths_keep_a_tile_below_32_bits():
         assert B.moe_linear_workspace_bytes(B.make_linear(256, wide, d, dtype, B.ACT_GELU)) > 0
         refused(-2, B.moe_linear_workspace_bytes, B.make_linear(256, d, wide + 64, dtype, B.ACT_GELU))
         refused(-2, B.moe_linear_workspace_bytes, B.make_linear(256, wide + 64, d, dtype, B.ACT_GELU))
+
+
+def test_linear_forward_needs_its_own_workspace_only():
+    """Inference brings room for the sums of K parts, none for gradients: 1.9 GB of dz at 32768 x 14336 SwiGLU are the backward's."""
+    lin = B.make_linear(32768, 4096, 14336, B.DTYPE_BF16, B.ACT_SWIGLU)
+    assert B.moe_linear_workspace_bytes(lin) > 2 * 32768 * 14336 * 2
+    assert B.moe_linear_fwd_workspace_bytes(lin) < 256 << 20
+    for dtype in (B.DTYPE_F32, B.DTYPE_BF16, B.DTYPE_F16):
+        for act in (B.ACT_NONE, B.ACT_GELU, B.ACT_SWIGLU):
+            for T, d, n in ((0, 64, 64), (1, 64, 64), (1, 4096, 1024), (64, 2048, 256), (300, 1024, 192), (4096, 256, 512), (100000, 64, 128)):
+                lin = B.make_linear(T, d, n, dtype, act)
+                need, both = B.moe_linear_fwd_workspace_bytes(lin), B.moe_linear_workspace_bytes(lin)
+                assert need % 256 == 0 and (need >= 256 or T == 0) and need <= both
+                if T == 0:
+                    continue
+                Wb = P if act == B.ACT_SWIGLU else None
+                refused(-7, B.moe_linear_fwd, lin, P, P, Wb, None, None, None, None, None, P, P, stream=S, ws_bytes=need - 1)
+                refused(-7, B.moe_linear_bwd, lin, P, P, P, Wb, P, Wb, None, None, None, P, P, Wb, P, Wb, 0, P, stream=S, ws_bytes=both - 1)
