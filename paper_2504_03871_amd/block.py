@@ -6,7 +6,8 @@
 
 Owns the buffers and issues the library calls in order, as layer.MoELayer does; nothing is computed here but the update of the
 balance bias.  With `fmt` (binding.PACK_E4M3 or PACK_I8) the pre-activations of both experts are kept in 8 bits between forward and
-backward, and `saved` may be one buffer that several blocks share.
+backward, and the planes that they are computed in, `moe.saved` and `pre`, are free in between: several blocks that run one after
+the other share one set of them, which is what saves memory (a block alone has its codes on top).
 """
 from __future__ import annotations
 
@@ -18,13 +19,13 @@ from .layer import MoELayer
 
 class SharedExpertMoE:
     def __init__(self, T, d_model, d_ff, d_shared, E, k, score, dtype=B.DTYPE_BF16, act=B.ACT_SWIGLU, capacity=0, fmt=B.PACK_NONE,
-                 saved=None, device="cuda:0"):
-        """`score`: binding.make_score(...); `d_shared`: hidden width of the shared expert; `saved`: another block's buffer of that
-        name, free between its backward and its next forward."""
+                 saved=None, pre=None, device="cuda:0"):
+        """`score`: binding.make_score(...); `d_shared`: hidden width of the shared expert; `saved`, `pre`: another block's
+        moe.saved and pre, with `fmt` only."""
+        if fmt == B.PACK_NONE and (saved is not None or pre is not None):
+            raise ValueError("without a pack format a block's planes hold what its backward reads: they cannot be shared")
         self.score, self.fmt, self.T = score, fmt, T
-        m = self.moe = MoELayer(T, d_model, d_ff, E, k, dtype=dtype, act=act, capacity=capacity, device=device)
-        if saved is not None:
-            m.saved = saved
+        m = self.moe = MoELayer(T, d_model, d_ff, E, k, dtype=dtype, act=act, capacity=capacity, device=device, saved=saved)
         td, dev = m.tdtype, m.device
         e = lambda *s, dtype=td: torch.empty(*s, dtype=dtype, device=dev)  # noqa: E731
         self.balance = torch.zeros(E, dtype=torch.float32, device=dev)
@@ -35,7 +36,11 @@ class SharedExpertMoE:
         self.down = B.make_linear(T, d_shared, d_model, dtype, B.ACT_NONE)
         self.ws = e(max(256, B.moe_linear_workspace_bytes(self.up), B.moe_linear_workspace_bytes(self.down)), dtype=torch.uint8)
         self.h, self.dh = e(T, d_shared), e(T, d_shared)
-        self.pre, self.scales = [e(T, d_shared), e(T, d_shared)], [None, None]
+        if pre is not None:
+            good = lambda p: p is not None and p.shape == (T, d_shared) and p.dtype == td and p.device == m.x.device and p.is_contiguous()  # noqa: E731
+            if len(pre) != 2 or not all(map(good, pre)) or pre[0].data_ptr() == pre[1].data_ptr():
+                raise ValueError(f"pre must be two contiguous planes [{T}, {d_shared}] of {td} on {dev}")
+        self.pre, self.scales = [e(T, d_shared), e(T, d_shared)] if pre is None else list(pre), [None, None]
         if fmt != B.PACK_NONE:
             self.dtype = dtype
             n = B.moe_pack8_bytes(T, d_shared)

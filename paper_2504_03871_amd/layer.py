@@ -13,10 +13,11 @@ from . import binding as B
 
 class MoELayer:
     def __init__(self, T, d_model, d_ff, E, k, dtype=B.DTYPE_BF16, act=B.ACT_GELU, capacity=0, device="cuda:0",
-                 params=None, defer_dw=False):
+                 params=None, defer_dw=False, saved=None):
         """`params`: another MoELayer whose weights and weight-gradient buffers this one aliases (one
         layer seen by several micro-batches, each with activation buffers of its own).  `defer_dw`: backward_inputs
-        will be used, with room for it behind the workspace."""
+        will be used, with room for it behind the workspace.  `saved`: a buffer for the saved activations, moe_saved_bytes at least,
+        instead of one of its own."""
         self.cfg = B.make_cfg(T, d_model, d_ff, E, k, dtype, act, capacity)
         self.T, self.d, self.f, self.E, self.k, self.act = T, d_model, d_ff, E, k, act
         self.tdtype = {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(dtype, torch.float32)
@@ -46,7 +47,10 @@ class MoELayer:
         self.slice_lo = self.slice_hi = None
         self.side = None
         self.x_perm = e(A, d_model, dtype=td, device=dev)
-        self.saved = torch.empty(B.moe_saved_bytes(self.cfg), dtype=torch.uint8, device=dev)
+        n = B.moe_saved_bytes(self.cfg)
+        if saved is not None and (saved.dtype != torch.uint8 or saved.device != self.x.device or not saved.is_contiguous() or saved.numel() < n):
+            raise ValueError(f"saved must be {n} contiguous bytes on {dev}")
+        self.saved = torch.empty(n, dtype=torch.uint8, device=dev) if saved is None else saved
         self.y_perm = e(A, d_model, dtype=td, device=dev)
         self.out = e(T, d_model, dtype=td, device=dev)
         need = B.moe_layer_bwd_inputs_ws_bytes if defer_dw else B.moe_workspace_bytes

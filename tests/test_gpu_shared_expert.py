@@ -96,3 +96,29 @@ def test_balance_update_evens_out_the_load():
         spread.append(int(blk.moe.counts.max() - blk.moe.counts.min()))
         blk.update_balance(0.01)
     assert min(spread[-10:]) < spread[0] // 2
+
+
+@pytest.mark.parametrize("fmt", [B.PACK_I8, B.PACK_E4M3])
+def test_blocks_that_share_their_planes(fmt):
+    """Two blocks one after the other, backward in reverse, in one set of planes: the bits of blocks with planes of their own."""
+    from paper_2504_03871_amd.block import SharedExpertMoE
+    args = (200, 128, 192, 320, 16, 4, B.DTYPE_BF16, B.ACT_SWIGLU, fmt)
+    alone = [make(*args, seed=s) for s in (1, 2)]
+    shared = [make(*args, seed=1), make(*args, seed=2)]
+    again = SharedExpertMoE(200, 128, 192, 320, 16, 4, shared[1].score, act=B.ACT_SWIGLU, fmt=fmt, saved=shared[0].moe.saved, pre=shared[0].pre)
+    for name in ("x", "Wr", "W1", "W1b", "W2", "d_out"):
+        getattr(again.moe, name).copy_(getattr(shared[1].moe, name))
+    for name in ("Wg", "Wu", "Wd", "balance"):
+        getattr(again, name).copy_(getattr(shared[1], name))
+    shared[1] = again
+    for blk in alone:
+        blk.step()
+    for blk in shared:
+        blk.forward()
+    for blk in reversed(shared):
+        blk.backward()
+    for a, b in zip(alone, shared):
+        for name in ("out", "dx", "dW1", "dW1b", "dW2", "dWr"):
+            assert torch.equal(getattr(a.moe, name), getattr(b.moe, name)), name
+        for name in ("dWg", "dWu", "dWd"):
+            assert torch.equal(getattr(a, name), getattr(b, name)), name
