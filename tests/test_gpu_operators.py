@@ -860,3 +860,27 @@ def test_linear_forward_in_its_own_workspace(dtype, T, d, n, act):
     y = torch.full_like(whole, 77.0)
     B.moe_linear_fwd(lin, c["x"], *two(c["W"]), *two(c["b"]), c["r"], None, None, y, ws, ws_bytes=need)
     assert torch.equal(y, whole) and (ws[need:] == 0xAB).all()
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("dtype,T,d,n,with_dw", [
+    ("bf16", 300, 256, 2048, True), ("f16", 64, 128, 1024, True),       # both gradients in one launch, K parts
+    ("bf16", 300, 512, 4096, False), ("f16", 33, 256, 8192, False),     # dx alone, K parts
+    ("bf16", 4100, 1024, 512, True), ("f16", 2300, 2048, 1088, True),   # large tiles, whole and in parts
+    ("f32", 70, 132, 1024, True), ("f32", 300, 64, 2048, False), ("f32", 900, 516, 100, True)])
+def test_linear_input_gradient_in_place(dtype, T, d, n, with_dw, act):
+    """dx_add may be dx itself: the bits of a sum with dx_add apart."""
+    c = linear_case(T, d, n, dtype, act)
+    lin = B.make_linear(T, d, n, DT[dtype], ACTS[act])
+    ws = torch.empty(B.moe_linear_workspace_bytes(lin), dtype=torch.uint8, device=DEV)
+    pre = two(c["pre"] if act != "none" else [])
+    dW = [torch.empty(d, n, device=DEV) for _ in range(c["mats"])] if with_dw else []
+
+    def dx_of(add, dx):
+        B.moe_linear_bwd(lin, c["dy"], c["x"], *two(c["W"]), *pre, None, None, add, dx, *two(dW), None, None, 0, ws)
+        return dx
+    apart = dx_of(c["add"], torch.full_like(c["x"], 77.0))
+    without = dx_of(None, torch.full_like(c["x"], 77.0))
+    assert not torch.equal(apart, without)
+    mine = c["add"].clone()
+    assert torch.equal(dx_of(mine, mine), apart)
