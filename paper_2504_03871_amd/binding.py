@@ -357,24 +357,29 @@ def moe_pack8_bytes(rows, width):
     return _two_sizes("moe_pack8_bytes", lambda a, b: lib().moe_pack8_bytes(int(rows), int(width), a, b))
 
 
-def _rows_ptr(t, width, pitch):
-    """A matrix whose rows are dense and `pitch` elements apart: a view of such a tensor, not only a contiguous one."""
-    if t is None or isinstance(t, int) or t.is_contiguous():
-        return _ptr(t)
-    if t.dim() != 2 or t.shape[1] != width or t.stride() != (pitch, 1):
-        raise ValueError("tensor must be contiguous, or rows of `width` elements `pitch` apart")
-    return ctypes.c_void_p(t.data_ptr())
+def _rows_ptr(t, dtype, rows, width, pitch):
+    """A matrix of `rows` dense rows that are `pitch` elements apart: a view of such a tensor, not only a contiguous one."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.element_size() != (4 if dtype == DTYPE_F32 else 2):
+        raise ValueError("tensor's elements must be of `dtype`")
+    if t.is_contiguous():
+        if rows > 0 and t.numel() < (rows - 1) * pitch + width:
+            raise ValueError("tensor must have `rows` rows of `width` elements `pitch` apart")
+    elif t.dim() != 2 or t.shape[0] < rows or t.shape[1] != width or t.stride() != (pitch, 1):
+        raise ValueError("tensor must be contiguous, or `rows` rows of `width` elements `pitch` apart")
+    return t.data_ptr()
 
 
 def moe_pack8(dtype, fmt, rows, width, pitch, src, codes, scales, stream=None):
     """A matrix to 8 bits in blocks of 32 with a shared power of two."""
-    _check("moe_pack8", lib().moe_pack8(int(dtype), int(fmt), int(rows), int(width), int(pitch), _rows_ptr(src, width, pitch), _ptr(codes),
+    _check("moe_pack8", lib().moe_pack8(int(dtype), int(fmt), int(rows), int(width), int(pitch), _rows_ptr(src, dtype, rows, width, pitch), _ptr(codes),
                                         _ptr(scales), _stream() if stream is None else stream))
 
 
 def moe_unpack8(dtype, fmt, rows, width, pitch, codes, scales, dst, stream=None):
     _check("moe_unpack8", lib().moe_unpack8(int(dtype), int(fmt), int(rows), int(width), int(pitch), _ptr(codes), _ptr(scales),
-                                            _rows_ptr(dst, width, pitch), _stream() if stream is None else stream))
+                                            _rows_ptr(dst, dtype, rows, width, pitch), _stream() if stream is None else stream))
 
 
 def moe_saved_pack8_bytes(cfg):

@@ -152,3 +152,17 @@ def test_linear_forward_needs_its_own_workspace_only():
                 Wb = P if act == B.ACT_SWIGLU else None
                 refused(-7, B.moe_linear_fwd, lin, P, P, Wb, None, None, None, None, None, P, P, stream=S, ws_bytes=need - 1)
                 refused(-7, B.moe_linear_bwd, lin, P, P, P, Wb, P, Wb, None, None, None, P, P, Wb, P, Wb, 0, P, stream=S, ws_bytes=both - 1)
+
+
+def test_packed_matrices_are_as_large_as_the_call_says():
+    """A tensor with fewer rows, narrower ones or smaller elements than `rows`, `pitch` and `dtype` say would be read past its end."""
+    torch = pytest.importorskip("torch")
+    whole = torch.zeros(8, 64, dtype=torch.bfloat16)
+    for t, rows, width, pitch, dt in ((whole[:, :40].contiguous(), 8, 40, 64, B.DTYPE_BF16), (whole, 9, 64, 64, B.DTYPE_BF16), (whole[:, :40], 9, 40, 64, B.DTYPE_BF16),
+                                      (whole, 8, 64, 64, B.DTYPE_F32), (whole.view(-1)[:500], 8, 60, 64, B.DTYPE_BF16), (whole[:, :40], 8, 40, 64, B.DTYPE_F32)):
+        with pytest.raises(ValueError):
+            B.moe_pack8(dt, B.PACK_I8, rows, width, pitch, t, P, P, stream=S)
+        with pytest.raises(ValueError):
+            B.moe_unpack8(dt, B.PACK_I8, rows, width, pitch, P, P, t, stream=S)
+    for t, rows, width, pitch in ((whole, 8, 64, 64), (whole[:, :40], 8, 40, 64), (whole[:, :40], 3, 40, 64), (whole, 8, 40, 64), (whole.view(-1)[:488], 8, 40, 64)):
+        assert B._rows_ptr(t, B.DTYPE_BF16, rows, width, pitch) == whole.data_ptr()
