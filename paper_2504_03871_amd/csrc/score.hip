@@ -433,7 +433,7 @@ __device__ __forceinline__ float softmax_sum(const float (&l)[V], float top) {
 }
 
 // The choice.  Bound by its instructions (vector ALUs busy 95 % of the cycles), not by the one pass over the logits: 32768 tokens, 8 of 256 experts, four of eight groups,
-// 23.6 us for 36 MB; 8191 tokens, 6 of 64, 4.9 us, and a call of four tokens 5.5, both the length of one wave's work.
+// 23.8 us for 36 MB; 8191 tokens, 6 of 64, 4.3 us, and a call of four tokens 5.3, both the length of one wave's work.
 template <int V, bool BY_LOGIT>
 __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a) {
   __shared__ float keys[SC_ROWS][SC_LANES * V];
