@@ -67,7 +67,8 @@ enum {
   MOE_ERR_BAD_SLICE = -4, /* exactly one of slice_lo / slice_hi is NULL */
   MOE_ERR_ALIGN = -5,     /* a device pointer is not 16-byte aligned */
   MOE_ERR_HIP = -6,       /* a launch failed; see moe_last_hip_error() */
-  MOE_ERR_WORKSPACE = -7  /* ws_bytes is smaller than moe_workspace_bytes(cfg) */
+  MOE_ERR_WORKSPACE = -7, /* ws_bytes is smaller than moe_workspace_bytes(cfg) */
+  MOE_ERR_OVERLAP = -8    /* two results of one call at the same address */
 };
 
 /*
@@ -451,6 +452,103 @@ MOE_API int moe_linear_fwd(const moe_linear* lin, const void* x, const void* W, 
 MOE_API int moe_linear_bwd(const moe_linear* lin, const void* dy, const void* x, const void* W, const void* Wb, const void* pre,
                    const void* pre_b, const void* pre_scales, const void* pre_b_scales, const void* dx_add, void* dx,
                    void* dW, void* dWb, void* dbias, void* dbias_b, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Dropout with a mask that is never stored.  Element (row r, column c) of a matrix is dropped where 16 bits of a counter generator are
+ * below cut = min(65535, floor(65536 p + 1/2)), and else multiplied by 65536 / (65536 - cut); what is dropped becomes 0 whatever it was.  The
+ * bits: Philox 4x32 with ten rounds, key = seed (low word first), counter = (c / 8, r, low, high word of offset); output word
+ * (c % 8) / 2, its low half for even c, the high half for odd c.  The mask depends on seed, offset, row and column alone: the backward
+ * pass gives the same ones, and another layer, step or call another offset (or seed).
+ * `step`: DEVICE pointer (8-byte aligned) or NULL; *step is added to offset when the kernel runs, so that a captured graph gives
+ * another mask on each replay.  Its forward and backward must see the same value.
+ */
+typedef struct moe_drop {
+  uint64_t seed;
+  uint64_t offset;
+  const uint64_t* step;
+  float p;             /* 0 <= p < 1 */
+} moe_drop;
+
+/*
+ * y = residual + dropout(x) (residual NULL: dropout(x)), any dense matrix of storage type `dtype`; y may be x or residual.  The gradient
+ * of x is moe_dropout of y's gradient with the same `drop` and no residual; the residual's is y's itself.
+ * rows < 2^31, width <= 2^20, rows * width <= 2^35.
+ */
+MOE_API int moe_dropout(int32_t dtype, int64_t rows, int32_t width, const moe_drop* drop, const void* x, const void* residual, void* y, void* stream);
+
+/*
+ * The norm in front of a block: root mean square, of a residual stream that takes in a branch.
+ *   h = residual + dropout(x), rounded to the stream's type; rstd = 1 / sqrt(mean of h^2 + eps); y = gamma h rstd.
+ * x, gamma, y, dy, dx: storage type `dtype` [T][d] ([d]: gamma; NULL: ones).  residual, h, dh_add, dh: type `stream`, dtype or
+ * MOE_DTYPE_F32.  rstd [T] fp32.  residual, drop NULL: none.  h NULL: not kept (h may be residual; and x, where the types are one).  rstd
+ * NULL: not kept (inference).  y or codes and scales may be NULL, not all of them: codes [T][d] and scales [T] are y in 8 bits, quantised
+ * as by moe_quant_rows below before y is rounded to its type.  y may be x (h and y must differ: MOE_ERR_OVERLAP).
+ * The norm is that of h as it is stored, kept or not.  Sums are fp32 (of squares: up to 3.4e38).
+ * Any T >= 0 up to 2^24, 1 <= d <= MOE_MAX_NORM; rows that start at multiples of 16 bytes are fastest.
+ *
+ * Backward: a = gamma dy, u = h rstd; dh = rstd (a - u mean(a u)) + dh_add (NULL: nothing; the gradient that reaches h by other ways), which
+ * is the gradient of residual too; dx = dropout's gradient of dh; dgamma = sum over the rows of dy u.  dh, dx, dgamma may be NULL: skipped;
+ * dh may be dh_add, and dx may be dy (not dh: MOE_ERR_OVERLAP).  dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or
+ * dtype (accumulate must be 0).  ws holds moe_norm_bwd_workspace_bytes and is needed for dgamma only.  No atomics: the same bits every time.
+ */
+#define MOE_MAX_NORM 16384
+typedef struct moe_norm {
+  int32_t T, d;
+  int32_t dtype;    /* MOE_DTYPE_* */
+  int32_t stream;   /* dtype or MOE_DTYPE_F32 */
+  int32_t grad;     /* dtype or MOE_DTYPE_F32 */
+  float eps;        /* > 0 */
+} moe_norm;
+MOE_API int moe_norm_fwd(const moe_norm* norm, const moe_drop* drop, const void* x, const void* residual, const void* gamma, void* h, float* rstd,
+                 void* y, void* codes, float* scales, void* stream);
+MOE_API int moe_norm_bwd_workspace_bytes(const moe_norm* norm, size_t* bytes);
+MOE_API int moe_norm_bwd(const moe_norm* norm, const moe_drop* drop, const void* dy, const void* h, const void* gamma, const float* rstd,
+                 const void* dh_add, void* dh, void* dx, void* dgamma, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * 8-bit integers with one fp32 scale for each token (row) or channel (column): m = max(largest magnitude, 2^-100), codes
+ * round(v * (127 / m)) in fp32, ties to even, from -127 to 127, scale m * (1 / 127).  A row or column with an infinity or NaN has codes of
+ * zero and the scale NaN: its products are NaN.
+ * moe_quant_rows: a matrix of `rows` rows and `width` <= MOE_MAX_ROW columns, `pitch` (>= width) elements from row to row; codes
+ * [rows][width] without gaps, scales [rows].  rows * pitch <= 2^40.
+ * moe_quant_weight: n matrices [d_in][d_out], d_in and d_out multiples of 64, each below 2^31 values; scales [n][d_out]; codes [n], the
+ * d_in * d_out bytes of a matrix in the order in which the products read them: column c and row r lie at byte
+ *   ((c / 16) * (d_in / 64) + r / 64) * 1024 + (r % 64 / 16) * 256 + (c % 16) * 16 + r % 16.
+ */
+#define MOE_MAX_ROW 65536
+MOE_API int moe_quant_rows(int32_t dtype, int64_t rows, int32_t width, int64_t pitch, const void* src, void* codes, float* scales, void* stream);
+MOE_API int moe_quant_weight(int32_t dtype, int32_t n, int32_t d_in, int32_t d_out, const void* W, void* codes, float* scales, void* stream);
+
+/*
+ * moe_linear's forward with both operands in 8 bits, for inference: y = act(z) + residual, z = x_scales w_scales (x W) + bias.
+ *   x codes [T][d_in] and x_scales [T] as moe_quant_rows writes them, W, Wb and w_scales, wb_scales [d_out] as moe_quant_weight does (codes of
+ *   other origin may be -128); bias, bias_b, residual, y in the storage type `dtype`, as in moe_linear_fwd, act too.
+ * Sums are 32-bit integers, exact; z, the activation and the residual's addition are fp32 and rounded once.
+ * Shapes: 0 <= T <= 2^24, d_in and d_out multiples of 64, d_in <= MOE_MAX_ROW, d_out <= 2^20, d_in * d_out < 2^31, T * d_in < 2^32.
+ * `ws` holds moe_linear8_workspace_bytes and is free again when the call is done.
+ */
+typedef struct moe_linear8 {
+  int32_t T, d_in, d_out;
+  int32_t dtype;      /* MOE_DTYPE_* of bias, residual, y */
+  int32_t act;        /* MOE_ACT_* */
+} moe_linear8;
+MOE_API int moe_linear8_workspace_bytes(const moe_linear8* lin, size_t* bytes);
+MOE_API int moe_linear8_fwd(const moe_linear8* lin, const void* x, const float* x_scales, const void* W, const float* w_scales, const void* Wb,
+                    const float* wb_scales, const void* bias, const void* bias_b, const void* residual, void* y, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The expert FFN of inference with both operands of both products in 8 bits, on the in-share rows:
+ *   H = act of the products of the tokens' codes with W1[e] (and W1b[e]) and their scales, rounded to the storage type; H quantised by rows;
+ *   y_perm = the products of those codes with W2[e] and their scales.
+ * x codes [T][d_model], x_scales [T] (moe_quant_rows): the rows are fetched by src_of (moe_dispatch with x_perm NULL), no permuted copy is
+ * needed.  W1, W1b, W2 and their scales [E][d_ff], [E][d_ff], [E][d_model] as moe_quant_weight writes them for n = E.  y_perm as in
+ * moe_expert_ffn_fwd, for moe_combine.  16-bit storage types only (MOE_ERR_BAD_DTYPE); d_model, d_ff <= MOE_MAX_ROW.
+ * `ws` holds moe_expert_ffn8_workspace_bytes (H and its codes in it).
+ */
+MOE_API int moe_expert_ffn8_workspace_bytes(const moe_cfg* cfg, size_t* bytes);
+MOE_API int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales, const void* W1, const float* w1_scales, const void* W1b,
+                        const float* w1b_scales, const void* W2, const float* w2_scales, const int32_t* src_of, const int32_t* offsets,
+                        const int32_t* kept, const int32_t* slice_lo, const int32_t* slice_hi, void* y_perm, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Planner of the asymmetric expert assignment (Section 4.2 of the paper, Algorithm 1 and the paragraph

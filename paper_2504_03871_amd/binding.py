@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libmoe_hip.so")
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 ACT_GELU, ACT_SWIGLU, ACT_NONE = 0, 1, 2   # ACT_NONE: moe_linear only
 MAX_E, MAX_K, MAX_GROUPS = 256, 8, 16
+MAX_NORM, MAX_ROW = 16384, 65536
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 PACK_NONE, PACK_E4M3, PACK_I8 = 0, 1, 2
 
@@ -24,7 +25,9 @@ SYMBOLS = ("moe_error_string", "moe_last_hip_error", "moe_workspace_bytes", "moe
            "moe_route_bwd", "moe_layer_fwd", "moe_layer_bwd", "moe_layer_bwd_inputs_ws_bytes", "moe_layer_bwd_inputs",
            "moe_layer_bwd_inputs_room_bytes", "moe_layer_bwd_inputs_in",
            "moe_layer_expert_dw", "moe_route_scored", "moe_route_scored_bwd", "moe_pack8_bytes", "moe_pack8", "moe_unpack8",
-           "moe_saved_pack8_bytes", "moe_saved_pack8", "moe_saved_restore8", "moe_linear_workspace_bytes", "moe_linear_fwd_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
+           "moe_saved_pack8_bytes", "moe_saved_pack8", "moe_saved_restore8", "moe_linear_workspace_bytes", "moe_linear_fwd_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd",
+           "moe_dropout", "moe_norm_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd", "moe_quant_rows", "moe_quant_weight",
+           "moe_linear8_workspace_bytes", "moe_linear8_fwd", "moe_expert_ffn8_workspace_bytes", "moe_expert_ffn_fwd8", "moe_asymea_plan", "moe_asymea_shares", "moe_bench_stream", "moe_bench_clock_probe", "moe_bench_mfma_loop", "moe_gemm_block_tile")
 
 PROF = {"gemm1_fwd": 0, "gemm2_fwd": 1, "dh_bwd": 2, "dw2_bwd": 3, "dw1_bwd": 4, "dx_bwd": 5, "gather": 6,
         "combine": 7, "combine_bwd": 8, "route": 9}
@@ -56,6 +59,18 @@ class MoeScore(ctypes.Structure):
 
 class MoeLinear(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "d_in", "d_out", "dtype", "act", "pre_pack", "grad")]
+
+
+class MoeDrop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p), ("p", ctypes.c_float)]
+
+
+class MoeNorm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "dtype", "stream", "grad")] + [("eps", ctypes.c_float)]
+
+
+class MoeLinear8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d_in", "d_out", "dtype", "act")]
 
 
 class MoeError(RuntimeError):
@@ -112,6 +127,16 @@ def lib():
             "moe_linear_fwd_workspace_bytes": [ctypes.POINTER(MoeLinear), ctypes.POINTER(sz)],
             "moe_linear_fwd": [ctypes.POINTER(MoeLinear)] + [p] * 10 + [sz, p],
             "moe_linear_bwd": [ctypes.POINTER(MoeLinear)] + [p] * 14 + [i32, p, sz, p],
+            "moe_dropout": [i32, i64, i32, ctypes.POINTER(MoeDrop)] + [p] * 4,
+            "moe_norm_fwd": [ctypes.POINTER(MoeNorm), ctypes.POINTER(MoeDrop)] + [p] * 9,
+            "moe_norm_bwd_workspace_bytes": [ctypes.POINTER(MoeNorm), ctypes.POINTER(sz)],
+            "moe_norm_bwd": [ctypes.POINTER(MoeNorm), ctypes.POINTER(MoeDrop)] + [p] * 8 + [i32, p, sz, p],
+            "moe_quant_rows": [i32, i64, i32, i64] + [p] * 4,
+            "moe_quant_weight": [i32] * 4 + [p] * 4,
+            "moe_linear8_workspace_bytes": [ctypes.POINTER(MoeLinear8), ctypes.POINTER(sz)],
+            "moe_linear8_fwd": [ctypes.POINTER(MoeLinear8)] + [p] * 11 + [sz, p],
+            "moe_expert_ffn8_workspace_bytes": [cfgp, ctypes.POINTER(sz)],
+            "moe_expert_ffn_fwd8": [cfgp] + [p] * 15 + [sz, p],
             "moe_asymea_plan": [i32] * 4 + [ctypes.c_double] * 3 + [i32, i32, ctypes.POINTER(i32)],
             "moe_asymea_shares": [i32] * 6 + [ctypes.POINTER(i32), ctypes.POINTER(i32)],
             "moe_bench_stream": [p, p, sz, i32, p],
@@ -428,6 +453,93 @@ def moe_linear_bwd(lin, dy, x, W, Wb, pre, pre_b, pre_scales, pre_b_scales, dx_a
     _check("moe_linear_bwd", lib().moe_linear_bwd(
         ctypes.byref(lin), _ptr(dy), _ptr(x), _ptr(W), _ptr(Wb), _ptr(pre), _ptr(pre_b), _ptr(pre_scales), _ptr(pre_b_scales), _ptr(dx_add),
         _ptr(dx), _ptr(dW), _ptr(dWb), _ptr(dbias), _ptr(dbias_b), int(accumulate), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
+        _stream() if stream is None else stream))
+
+
+def make_drop(p, seed, offset=0, step=None) -> MoeDrop:
+    """Dropout of probability p; `seed` and `offset` name the mask.  `step`: a tensor of one int64 on the GPU, added to offset when the
+    kernel runs; the caller keeps it alive."""
+    if step is not None and not isinstance(step, int):
+        if step.element_size() != 8 or step.numel() < 1 or not step.is_cuda:
+            raise ValueError("step must be a 64-bit integer on the GPU")
+        step = step.data_ptr()
+    return MoeDrop(int(seed) % (1 << 64), int(offset) % (1 << 64), step, float(p))
+
+
+def _drop(drop):
+    return None if drop is None else ctypes.byref(drop)
+
+
+def moe_dropout(dtype, rows, width, drop, x, residual, y, stream=None):
+    """y = residual + dropout(x)."""
+    _check("moe_dropout", lib().moe_dropout(int(dtype), int(rows), int(width), _drop(drop), _ptr(x), _ptr(residual), _ptr(y),
+                                            _stream() if stream is None else stream))
+
+
+def make_norm(T, d, dtype=DTYPE_BF16, stream=None, grad=DTYPE_F32, eps=1e-6) -> MoeNorm:
+    """`stream`: type of the residual stream (None: dtype); `grad`: of gamma's gradient."""
+    return MoeNorm(int(T), int(d), int(dtype), int(dtype if stream is None else stream), int(grad), float(eps))
+
+
+def moe_norm_fwd(norm, drop, x, residual, gamma, h, rstd, y, codes, scales, stream=None):
+    """h = residual + dropout(x), y = gamma h / rms(h); y also, or only, in 8 bits."""
+    _check("moe_norm_fwd", lib().moe_norm_fwd(ctypes.byref(norm), _drop(drop), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(h), _ptr(rstd), _ptr(y),
+                                              _ptr(codes), _ptr(scales), _stream() if stream is None else stream))
+
+
+def moe_norm_bwd_workspace_bytes(norm) -> int:
+    n = ctypes.c_size_t(0)
+    _check("moe_norm_bwd_workspace_bytes", lib().moe_norm_bwd_workspace_bytes(ctypes.byref(norm), ctypes.byref(n)))
+    return n.value
+
+
+def moe_norm_bwd(norm, drop, dy, h, gamma, rstd, dh_add, dh, dx, dgamma, accumulate, ws, stream=None, ws_bytes=None):
+    _check("moe_norm_bwd", lib().moe_norm_bwd(
+        ctypes.byref(norm), _drop(drop), _ptr(dy), _ptr(h), _ptr(gamma), _ptr(rstd), _ptr(dh_add), _ptr(dh), _ptr(dx), _ptr(dgamma), int(accumulate),
+        _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream() if stream is None else stream))
+
+
+def moe_quant_rows(dtype, rows, width, pitch, src, codes, scales, stream=None):
+    """Rows to 8-bit integers with a scale each."""
+    _check("moe_quant_rows", lib().moe_quant_rows(int(dtype), int(rows), int(width), int(pitch), _rows_ptr(src, dtype, rows, width, pitch), _ptr(codes),
+                                                  _ptr(scales), _stream() if stream is None else stream))
+
+
+def moe_quant_weight(dtype, n, d_in, d_out, W, codes, scales, stream=None):
+    """n matrices [d_in, d_out] to 8-bit integers with a scale for each column, in the order that the products read."""
+    _check("moe_quant_weight", lib().moe_quant_weight(int(dtype), int(n), int(d_in), int(d_out), _ptr(W), _ptr(codes), _ptr(scales),
+                                                      _stream() if stream is None else stream))
+
+
+def make_linear8(T, d_in, d_out, dtype=DTYPE_BF16, act=ACT_NONE) -> MoeLinear8:
+    return MoeLinear8(int(T), int(d_in), int(d_out), int(dtype), int(act))
+
+
+def moe_linear8_workspace_bytes(lin) -> int:
+    n = ctypes.c_size_t(0)
+    _check("moe_linear8_workspace_bytes", lib().moe_linear8_workspace_bytes(ctypes.byref(lin), ctypes.byref(n)))
+    return n.value
+
+
+def moe_linear8_fwd(lin, x, x_scales, W, w_scales, Wb, wb_scales, bias, bias_b, residual, y, ws, stream=None, ws_bytes=None):
+    """y = act(x_scales w_scales (x W) + bias) + residual of 8-bit x and W."""
+    _check("moe_linear8_fwd", lib().moe_linear8_fwd(
+        ctypes.byref(lin), _ptr(x), _ptr(x_scales), _ptr(W), _ptr(w_scales), _ptr(Wb), _ptr(wb_scales), _ptr(bias), _ptr(bias_b), _ptr(residual),
+        _ptr(y), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes, _stream() if stream is None else stream))
+
+
+def moe_expert_ffn8_workspace_bytes(cfg) -> int:
+    n = ctypes.c_size_t(0)
+    _check("moe_expert_ffn8_workspace_bytes", lib().moe_expert_ffn8_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def moe_expert_ffn_fwd8(cfg, x, x_scales, W1, w1_scales, W1b, w1b_scales, W2, w2_scales, src_of, offsets, kept, slice_lo, slice_hi, y_perm, ws,
+                        stream=None, ws_bytes=None):
+    """The expert FFN with both products in 8 bits; x are the tokens' codes, unpermuted."""
+    _check("moe_expert_ffn_fwd8", lib().moe_expert_ffn_fwd8(
+        ctypes.byref(cfg), _ptr(x), _ptr(x_scales), _ptr(W1), _ptr(w1_scales), _ptr(W1b), _ptr(w1b_scales), _ptr(W2), _ptr(w2_scales), _ptr(src_of),
+        _ptr(offsets), _ptr(kept), _ptr(slice_lo), _ptr(slice_hi), _ptr(y_perm), _ptr(ws), _nbytes(ws) if ws_bytes is None else ws_bytes,
         _stream() if stream is None else stream))
 
 

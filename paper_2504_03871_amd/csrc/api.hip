@@ -1,7 +1,9 @@
 // C ABI of the MoE library: argument validation, workspace layout, kernel sequencing.
 #include "common.h"
 #include "gemm.h"
+#include "gemm_i8.h"
 #include "linear.h"
+#include "norm.h"
 #include "pack8.h"
 #include "prof.h"
 #include "tile_map.h"
@@ -218,6 +220,7 @@ const char* moe_error_string(int code) {
     case MOE_ERR_ALIGN: return "device pointer not 16-byte aligned";
     case MOE_ERR_HIP: return "HIP launch failed (see moe_last_hip_error)";
     case MOE_ERR_WORKSPACE: return "workspace smaller than moe_workspace_bytes(cfg), or problem too large for the static scratch";
+    case MOE_ERR_OVERLAP: return "two results at the same address";
     default: return "unknown error code";
   }
 }
@@ -1026,6 +1029,197 @@ int moe_layer_expert_dw(const moe_cfg* cfg, const moe_layer_bufs* const* calls, 
     CHECK(launch_gemm_half_dw_segs(cfg->dtype, gw2, s2, gw1, s1, s));
   }
   return MOE_OK;
+}
+
+// ---- the norm, dropout, products in 8 bits ------------------------------------------------------------------------
+static bool known_dtype(int32_t t) { return t == MOE_DTYPE_F32 || t == MOE_DTYPE_BF16 || t == MOE_DTYPE_F16; }
+static int check_drop(const moe_drop* d) {
+  if (d == nullptr) return MOE_OK;
+  if (!(d->p >= 0.f && d->p < 1.f)) return MOE_ERR_BAD_SHAPE;
+  return (reinterpret_cast<uintptr_t>(d->step) & 7u) != 0 ? MOE_ERR_ALIGN : MOE_OK;
+}
+
+int moe_dropout(int32_t dtype, int64_t rows, int32_t width, const moe_drop* drop, const void* x, const void* residual, void* y, void* stream) {
+  if (!known_dtype(dtype)) return MOE_ERR_BAD_DTYPE;
+  REQUIRE(drop);
+  CHECK(check_drop(drop));
+  if (rows < 0 || rows >= (1ll << 31) || width < 1 || width > (1 << 20) || rows * width > (1ll << 35)) return MOE_ERR_BAD_SHAPE;
+  if (rows == 0) return MOE_OK;
+  REQUIRE(x); REQUIRE(y);
+  ALIGNED(x); ALIGNED(residual); ALIGNED(y);
+  return launch_dropout(dtype, rows, width, drop_args(drop), x, residual, y, (hipStream_t)stream);
+}
+
+static int check_norm(const moe_norm* n) {
+  REQUIRE(n);
+  if (!known_dtype(n->dtype) || (n->stream != n->dtype && n->stream != MOE_DTYPE_F32) || (n->grad != n->dtype && n->grad != MOE_DTYPE_F32)) return MOE_ERR_BAD_DTYPE;
+  if (n->T < 0 || n->T > (1 << 24) || n->d < 1 || n->d > MOE_MAX_NORM || !(n->eps > 0.f && n->eps < __builtin_inff())) return MOE_ERR_BAD_SHAPE;
+  return MOE_OK;
+}
+
+int moe_norm_fwd(const moe_norm* norm, const moe_drop* drop, const void* x, const void* residual, const void* gamma, void* h, float* rstd, void* y,
+                 void* codes, float* scales, void* stream) {
+  CHECK(check_norm(norm));
+  CHECK(check_drop(drop));
+  if (norm->T == 0) return MOE_OK;
+  REQUIRE(x);
+  if (y == nullptr) REQUIRE(codes);
+  if ((codes == nullptr) != (scales == nullptr)) return MOE_ERR_NULL;
+  if (h != nullptr && h == y) return MOE_ERR_OVERLAP;
+  ALIGNED(x); ALIGNED(residual); ALIGNED(gamma); ALIGNED(h); ALIGNED(rstd); ALIGNED(y); ALIGNED(codes); ALIGNED(scales);
+  NormFwdArgs a = {x, residual, gamma, h, rstd, y, (int8_t*)codes, scales, drop_args(drop), norm->T, norm->d, norm->eps};
+  return launch_norm_fwd(norm, a, (hipStream_t)stream);
+}
+
+int moe_norm_bwd_workspace_bytes(const moe_norm* norm, size_t* bytes) {
+  CHECK(check_norm(norm));
+  REQUIRE(bytes);
+  *bytes = norm_bwd_ws_bytes(norm);
+  return MOE_OK;
+}
+
+int moe_norm_bwd(const moe_norm* norm, const moe_drop* drop, const void* dy, const void* h, const void* gamma, const float* rstd, const void* dh_add,
+                 void* dh, void* dx, void* dgamma, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_norm(norm));
+  CHECK(check_drop(drop));
+  if (accumulate && norm->grad != MOE_DTYPE_F32) return MOE_ERR_BAD_DTYPE;
+  if (dh != nullptr && dh == dx) return MOE_ERR_OVERLAP;
+  ALIGNED(dy); ALIGNED(h); ALIGNED(gamma); ALIGNED(rstd); ALIGNED(dh_add); ALIGNED(dh); ALIGNED(dx); ALIGNED(dgamma); ALIGNED(ws);
+  if (norm->T > 0) {
+    REQUIRE(dy); REQUIRE(h); REQUIRE(rstd);
+    if (dgamma != nullptr) {
+      REQUIRE(ws);
+      if (ws_bytes < norm_bwd_ws_bytes(norm)) return MOE_ERR_WORKSPACE;
+    } else if (dh == nullptr && dx == nullptr) {
+      return MOE_OK;
+    }
+  }
+  NormBwdArgs a = {dy, h, gamma, rstd, dh_add, dh, dx, dgamma != nullptr ? (float*)ws : nullptr, drop_args(drop), norm->T, norm->d};
+  return launch_norm_bwd(norm, a, dgamma, accumulate, (hipStream_t)stream);
+}
+
+int moe_quant_rows(int32_t dtype, int64_t rows, int32_t width, int64_t pitch, const void* src, void* codes, float* scales, void* stream) {
+  if (!known_dtype(dtype)) return MOE_ERR_BAD_DTYPE;
+  if (rows < 0 || width < 1 || width > MOE_MAX_ROW || pitch < width || pitch > (1ll << 40) || (rows > 0 && rows > (1ll << 40) / pitch)) return MOE_ERR_BAD_SHAPE;
+  if (rows == 0) return MOE_OK;
+  REQUIRE(src); REQUIRE(codes); REQUIRE(scales);
+  ALIGNED(src); ALIGNED(codes); ALIGNED(scales);
+  return launch_quant_rows(dtype, rows, width, pitch, src, RowRange{}, (int8_t*)codes, scales, (hipStream_t)stream);
+}
+
+int moe_quant_weight(int32_t dtype, int32_t n, int32_t d_in, int32_t d_out, const void* W, void* codes, float* scales, void* stream) {
+  if (!known_dtype(dtype)) return MOE_ERR_BAD_DTYPE;
+  if (n < 0 || n > 65535 || d_in < 1 || d_out < 1 || d_in % 64 != 0 || d_out % 64 != 0 || (long long)d_in * d_out >= (1ll << 31)) return MOE_ERR_BAD_SHAPE;
+  if (n == 0) return MOE_OK;
+  REQUIRE(W); REQUIRE(codes); REQUIRE(scales);
+  ALIGNED(W); ALIGNED(codes); ALIGNED(scales);
+  return launch_quant_weight(dtype, n, d_in, d_out, W, (int8_t*)codes, scales, (hipStream_t)stream);
+}
+
+static int check_linear8(const moe_linear8* c) {
+  REQUIRE(c);
+  if (!known_dtype(c->dtype) || (c->act != MOE_ACT_NONE && c->act != MOE_ACT_GELU && c->act != MOE_ACT_SWIGLU)) return MOE_ERR_BAD_DTYPE;
+  if (c->T < 0 || c->T > (1 << 24) || c->d_in < 1 || c->d_out < 1 || c->d_in % 64 != 0 || c->d_out % 64 != 0 || c->d_in > MOE_MAX_ROW ||
+      c->d_out > (1 << 20) || (long long)c->d_in * c->d_out >= (1ll << 31))
+    return MOE_ERR_BAD_SHAPE;
+  return MOE_OK;
+}
+static size_t linear8_need(const moe_linear8* c) {
+  const int mats = c->act == MOE_ACT_SWIGLU ? 2 : 1;
+  return c->T == 0 ? 0 : linear8_ws_bytes(cut_linear8(c->T, c->d_out, c->d_in, mats), c->T, c->d_out, mats);
+}
+
+int moe_linear8_workspace_bytes(const moe_linear8* lin, size_t* bytes) {
+  CHECK(check_linear8(lin));
+  REQUIRE(bytes);
+  *bytes = linear8_need(lin);
+  return MOE_OK;
+}
+
+int moe_linear8_fwd(const moe_linear8* lin, const void* x, const float* x_scales, const void* W, const float* w_scales, const void* Wb,
+                    const float* wb_scales, const void* bias, const void* bias_b, const void* residual, void* y, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_linear8(lin));
+  if (lin->T == 0) return MOE_OK;
+  REQUIRE(x); REQUIRE(x_scales); REQUIRE(W); REQUIRE(w_scales); REQUIRE(y);
+  const bool two = lin->act == MOE_ACT_SWIGLU;
+  if (two) { REQUIRE(Wb); REQUIRE(wb_scales); }
+  if (!two && (Wb != nullptr || wb_scales != nullptr || bias_b != nullptr)) return MOE_ERR_BAD_DTYPE;
+  ALIGNED(x); ALIGNED(x_scales); ALIGNED(W); ALIGNED(w_scales); ALIGNED(Wb); ALIGNED(wb_scales); ALIGNED(bias); ALIGNED(bias_b); ALIGNED(residual);
+  ALIGNED(y); ALIGNED(ws);
+  REQUIRE(ws);
+  if (ws_bytes < linear8_need(lin)) return MOE_ERR_WORKSPACE;
+  return launch_linear8(lin, x, x_scales, W, w_scales, Wb, wb_scales, bias, bias_b, residual, y, ws, (hipStream_t)stream);
+}
+
+namespace {
+// Workspace of the experts' products in 8 bits
+struct Ffn8Layout { size_t map, hidden, codes, scales, total; };
+Ffn8Layout ffn8_layout(const moe_cfg* c) {
+  const size_t A = (size_t)c->T * c->k, f = c->d_ff;
+  Ffn8Layout l = {};
+  size_t off = align_up(tile_map_bytes(max_row_tiles((int)A, c->E, TILE_ROWS_MIN), c->E), 256);
+  l.hidden = off; off += align_up(A * f * 2, 256);
+  l.codes = off; off += align_up(A * f, 256);
+  l.scales = off; off += align_up(A * 4, 256);
+  l.total = off;
+  return l;
+}
+int check_ffn8(const moe_cfg* c) {
+  CHECK(check_cfg(c));
+  if (!is_half(c)) return MOE_ERR_BAD_DTYPE;
+  return c->d_model > MOE_MAX_ROW || c->d_ff > MOE_MAX_ROW ? MOE_ERR_BAD_SHAPE : MOE_OK;
+}
+}  // namespace
+
+int moe_expert_ffn8_workspace_bytes(const moe_cfg* cfg, size_t* bytes) {
+  CHECK(check_ffn8(cfg));
+  REQUIRE(bytes);
+  *bytes = ffn8_layout(cfg).total;
+  return MOE_OK;
+}
+
+int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales, const void* W1, const float* w1_scales, const void* W1b,
+                        const float* w1b_scales, const void* W2, const float* w2_scales, const int32_t* src_of, const int32_t* offsets,
+                        const int32_t* kept, const int32_t* slice_lo, const int32_t* slice_hi, void* y_perm, void* ws, size_t ws_bytes, void* stream) {
+  CHECK(check_ffn8(cfg));
+  CHECK(check_slices(slice_lo, slice_hi));
+  REQUIRE(x); REQUIRE(x_scales); REQUIRE(W1); REQUIRE(w1_scales); REQUIRE(W2); REQUIRE(w2_scales); REQUIRE(src_of); REQUIRE(offsets); REQUIRE(kept);
+  REQUIRE(y_perm); REQUIRE(ws);
+  const bool swiglu = cfg->act == MOE_ACT_SWIGLU;
+  if (swiglu) { REQUIRE(W1b); REQUIRE(w1b_scales); }
+  if (!swiglu && (W1b != nullptr || w1b_scales != nullptr)) return MOE_ERR_BAD_DTYPE;
+  ALIGNED(x); ALIGNED(x_scales); ALIGNED(W1); ALIGNED(w1_scales); ALIGNED(W1b); ALIGNED(w1b_scales); ALIGNED(W2); ALIGNED(w2_scales); ALIGNED(src_of);
+  ALIGNED(offsets); ALIGNED(kept); ALIGNED(slice_lo); ALIGNED(slice_hi); ALIGNED(y_perm); ALIGNED(ws);
+  const Ffn8Layout l = ffn8_layout(cfg);
+  if (ws_bytes < l.total) return MOE_ERR_WORKSPACE;
+  if (cfg->T == 0) return MOE_OK;
+  hipStream_t s = (hipStream_t)stream;
+  char* w = static_cast<char*>(ws);
+  const int A = cfg->T * cfg->k, d = cfg->d_model, f = cfg->d_ff, tr = expert8_tile_rows(A, cfg->E);
+  Gemm8Args g = {};
+  g.offsets = offsets; g.kept = kept; g.lo = slice_lo; g.hi = slice_hi; g.E = cfg->E;
+  if (tr > 0) {
+    TileMapArgs tm = {offsets, kept, slice_lo, slice_hi, cfg->E};
+    tm.tile_rows = tr;
+    tm.table = GELU_TAB_NONE;
+    tm.map = tile_map_at(w, max_row_tiles(A, cfg->E, TILE_ROWS_MIN), cfg->E);
+    CHECK(launch_tile_map(tm, s));
+    g.tiles = tm.map.tiles;
+    g.ntiles = tm.map.header;
+  }
+  const int max_tiles = tr > 0 ? max_row_tiles(A, cfg->E, tr) : 0;
+  int8_t* codes = reinterpret_cast<int8_t*>(w + l.codes);
+  float* scales = reinterpret_cast<float*>(w + l.scales);
+  Gemm8Args g1 = g, g2 = g;
+  g1.A = static_cast<const int8_t*>(x); g1.a_scale = x_scales; g1.src_of = src_of; g1.per_row = cfg->k; g1.src_rows = cfg->T;
+  g1.B = static_cast<const int8_t*>(W1); g1.B2 = static_cast<const int8_t*>(W1b); g1.b_scale = w1_scales; g1.b2_scale = w1b_scales;
+  g1.N = f; g1.K = d; g1.C = w + l.hidden;
+  CHECK(launch_expert8(cfg->dtype, cfg->act, g1, tr, max_tiles, A, s));
+  CHECK(launch_quant_rows(cfg->dtype, A, f, f, w + l.hidden, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, codes, scales, s));
+  g2.A = codes; g2.a_scale = scales;
+  g2.B = static_cast<const int8_t*>(W2); g2.b_scale = w2_scales;
+  g2.N = d; g2.K = f; g2.C = y_perm;
+  return launch_expert8(cfg->dtype, MOE_ACT_NONE, g2, tr, max_tiles, A, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,292 @@
+// Root-mean-square norm of a residual stream that takes in a branch, with dropout on the branch: forward and backward; and dropout
+// by itself.
+//   forward    h = residual + drop(x), rounded to the stream's type; r = 1 / sqrt(mean(h^2) + eps); y = gamma h r, written in the
+//              storage type, in 8-bit integers with a scale for the row, or both
+//   backward   u = h r, a = gamma dy; dh = r (a - u mean(a u)) + dh_add; dx = drop(dh) with the same mask; dgamma = sum over rows of dy u
+// The norm is that of h as it is stored: the backward, which reads it, differentiates exactly what the forward computed, and a
+// forward from a kept h gives the same bits.  Sums are fp32; every result is rounded once.
+//
+// One pass over memory each: a row stays in the registers of one or several waves (rows.h) between its sums and its results.
+#include "norm.h"
+
+namespace moe {
+
+template <typename T, typename S, bool ODD, int WPR, int NCH>
+__global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs a) {
+  constexpr int TPR = WPR * WAVE, R = rows_per_block(WPR);
+  __shared__ float s_sum[2][WPR];
+  __shared__ unsigned s_top[2][WPR];
+  const int tid = threadIdx.x % TPR, d = a.d;
+  const T* gamma = reinterpret_cast<const T*>(a.gamma);
+  const uint64_t offset = a.drop.cut != 0 ? drop_offset(a.drop) : 0;
+  int turn = 0;
+  for (int row = blockIdx.x * R + threadIdx.x / TPR; row < a.T; row += gridDim.x * R, turn ^= 1) {
+    const size_t at = (size_t)row * d;
+    const T* x = reinterpret_cast<const T*>(a.x) + at;
+    Raw8<T> xr[NCH];
+    Raw8<S> rr[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) xr[i] = load_row8<T, ODD>(x, (i * TPR + tid) * 8, d);
+    if (a.residual != nullptr) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) rr[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.residual) + at, (i * TPR + tid) * 8, d);
+    }
+    float v[NCH][8], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      unpack8<T>(xr[i], v[i]);
+      if (a.drop.cut != 0) drop8(a.drop, offset, (uint32_t)row, (uint32_t)(i * TPR + tid), v[i]);
+      if (a.residual != nullptr) {
+        float q[8];
+        unpack8<S>(rr[i], q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] += q[j];
+      }
+      const Raw8<S> h = pack_row8<S>(v[i]);
+      if (a.h != nullptr) store_row8<S, ODD>(reinterpret_cast<S*>(a.h) + at, (i * TPR + tid) * 8, d, h);
+      unpack8<S>(h, v[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum = fmaf(v[i][j], v[i][j], sum);
+    }
+    sum = row_reduce<WPR>(sum, s_sum[turn], add_f);
+    const float r = 1.f / sqrtf(sum / (float)d + a.eps);
+    if (a.rstd != nullptr && tid == 0) a.rstd[row] = r;
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = (i * TPR + tid) * 8;
+      float g[8];
+      if (gamma != nullptr) unpack8<T>(load_row8<T, ODD, false>(gamma, c, d), g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] *= r;
+        if (gamma != nullptr) v[i][j] *= g[j];
+      }
+      if (a.y != nullptr) store_row8<T, ODD>(reinterpret_cast<T*>(a.y) + at, c, d, pack_row8<T>(v[i]));
+      top = top_of(top, v[i]);
+    }
+    if (a.codes != nullptr) {
+      const RowScale q = row_scale(row_reduce<WPR>(top, s_top[turn], max_u));
+      if (tid == 0) a.scales[row] = q.scale;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) store_codes8<ODD>(a.codes + at, (i * TPR + tid) * 8, d, codes8(v[i], q.up));
+    }
+  }
+}
+
+template <typename T, typename S, bool ODD, int WPR, int NCH>
+__global__ __launch_bounds__(row_threads(WPR)) void norm_bwd_kernel(NormBwdArgs a) {
+  constexpr int TPR = WPR * WAVE, R = rows_per_block(WPR);
+  __shared__ float s_sum[2][WPR];
+  const int tid = threadIdx.x % TPR, d = a.d;
+  const T* gamma = reinterpret_cast<const T*>(a.gamma);
+  const uint64_t offset = a.drop.cut != 0 ? drop_offset(a.drop) : 0;
+  float dg[NCH][8] = {};
+  int turn = 0;
+  for (int row = blockIdx.x * R + threadIdx.x / TPR; row < a.T; row += gridDim.x * R, turn ^= 1) {
+    const size_t at = (size_t)row * d;
+    Raw8<T> yr[NCH];
+    Raw8<S> hr[NCH], ar[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      yr[i] = load_row8<T, ODD>(reinterpret_cast<const T*>(a.dy) + at, (i * TPR + tid) * 8, d);
+      hr[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.h) + at, (i * TPR + tid) * 8, d);
+    }
+    if (a.dh_add != nullptr) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) ar[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.dh_add) + at, (i * TPR + tid) * 8, d);
+    }
+    const float r = a.rstd[row];
+    float w[NCH][8], u[NCH][8], dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      unpack8<T>(yr[i], w[i]);
+      unpack8<S>(hr[i], u[i]);
+      float g[8];
+      if (gamma != nullptr) unpack8<T>(load_row8<T, ODD, false>(gamma, (i * TPR + tid) * 8, d), g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        u[i][j] *= r;
+        dg[i][j] = fmaf(w[i][j], u[i][j], dg[i][j]);
+        if (gamma != nullptr) w[i][j] *= g[j];
+        dot = fmaf(w[i][j], u[i][j], dot);
+      }
+    }
+    dot = row_reduce<WPR>(dot, s_sum[turn], add_f) / (float)d;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = (i * TPR + tid) * 8;
+      float q[8];
+      if (a.dh_add != nullptr) unpack8<S>(ar[i], q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[i][j] = r * (w[i][j] - u[i][j] * dot);
+        if (a.dh_add != nullptr) w[i][j] += q[j];
+      }
+      if (a.dh != nullptr) store_row8<S, ODD>(reinterpret_cast<S*>(a.dh) + at, c, d, pack_row8<S>(w[i]));
+      if (a.dx != nullptr) {
+        if (a.drop.cut != 0) drop8(a.drop, offset, (uint32_t)row, (uint32_t)(i * TPR + tid), w[i]);
+        store_row8<T, ODD>(reinterpret_cast<T*>(a.dx) + at, c, d, pack_row8<T>(w[i]));
+      }
+    }
+  }
+  if (a.partials == nullptr) return;
+  float* out = a.partials + (size_t)blockIdx.x * d;
+  if constexpr (R > 1) {   // the block's waves one after the other: the same order every time
+    __shared__ float s_dg[NCH * TPR * 8];
+    for (int w = 1; w < R; ++w) {
+      if ((int)threadIdx.x / TPR == w) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s_dg[(i * 8 + j) * TPR + tid] = dg[i][j];
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < TPR) {
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dg[i][j] += s_dg[(i * 8 + j) * TPR + tid];
+      }
+      __syncthreads();
+    }
+    if ((int)threadIdx.x >= TPR) return;
+  }
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int c = (i * TPR + tid) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < d) out[c + j] = dg[i][j];
+  }
+}
+
+// Column sums of the partial sums: 16 columns by 16 rows at a time, whose sums are added in order.
+template <typename OT>
+__global__ __launch_bounds__(256) void norm_dgamma_kernel(const float* partials, int rows, int d, OT* out, int accumulate) {
+  __shared__ float part[16][17];
+  const int cl = threadIdx.x & 15, rl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+  float sum = 0.f;
+  if (c < d) {
+#pragma unroll 8
+    for (int r = rl; r < rows; r += 16) sum += partials[(size_t)r * d + c];
+  }
+  part[rl][cl] = sum;
+  __syncthreads();
+  if (rl != 0 || c >= d) return;
+#pragma unroll
+  for (int r = 1; r < 16; ++r) sum += part[r][cl];
+  out[c] = from_f32<OT>(sum + (accumulate ? to_f32(out[c]) : 0.f));
+}
+
+// A thread takes U groups of eight adjacent values, 256 apart, and requests them all before it uses the first.  Rows are found by a
+// division of a block's own 32-bit numbers.
+template <typename T, int U>
+__global__ __launch_bounds__(256) void dropout_kernel(DropArgs drop, const T* x, const T* residual, T* y, long long rows, int width, unsigned groups) {
+  const uint64_t offset = drop_offset(drop);
+  const long long first = (long long)blockIdx.x * (256 * U), row0 = first / groups;
+  const unsigned in0 = (unsigned)(first - row0 * groups);
+  Raw8<T> xr[U], rr[U];
+  long long row[U];
+  unsigned g[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const unsigned i = in0 + u * 256 + threadIdx.x, q = i / groups;
+    row[u] = row0 + q;
+    g[u] = i - q * groups;
+    if (row[u] >= rows) continue;
+    xr[u] = load_row8<T, true>(x + row[u] * width, (int)g[u] * 8, width);
+    if (residual != nullptr) rr[u] = load_row8<T, true>(residual + row[u] * width, (int)g[u] * 8, width);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (row[u] >= rows) break;
+    float v[8];
+    unpack8<T>(xr[u], v);
+    if (drop.cut != 0) drop8(drop, offset, (uint32_t)row[u], g[u], v);
+    if (residual != nullptr) {
+      float q[8];
+      unpack8<T>(rr[u], q);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += q[j];
+    }
+    store_row8<T, true>(y + row[u] * width, (int)g[u] * 8, width, pack_row8<T>(v));
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+constexpr int NORM_MOST_BLOCKS = 1 << 16;   // further rows in further turns
+
+// F(odd, waves per row, groups per thread) for rows of d values; rows of no whole groups have fewer variants (norm_geom).
+#define MOE_NORM_GEOM(D_, F_)                                                                              \
+  do {                                                                                                     \
+    const RowGeom g_ = norm_geom(D_);                                                                      \
+    if ((D_) % 8 != 0) { if (g_.wpr == 1) F_(true, 1, 2); else if (g_.wpr == 4) F_(true, 4, 2); else F_(true, 8, 4); } \
+    else if (g_.wpr == 8) F_(false, 8, 4);                                                                 \
+    else if (g_.wpr == 4) { if (g_.nch == 2) F_(false, 4, 2); else F_(false, 4, 4); }                      \
+    else if (g_.nch == 1) F_(false, 1, 1);                                                                 \
+    else if (g_.nch == 2) F_(false, 1, 2);                                                                 \
+    else F_(false, 1, 4);                                                                                  \
+  } while (0)
+
+template <typename T, typename S>
+static int norm_fwd_for(const NormFwdArgs& a, hipStream_t s) {
+  const int rows = rows_per_block(norm_geom(a.d).wpr);
+  const long long want = ((long long)a.T + rows - 1) / rows;
+  const unsigned grid = (unsigned)(want < NORM_MOST_BLOCKS ? want : NORM_MOST_BLOCKS);
+#define MOE_NORM_FWD(O_, W_, C_) norm_fwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(W_), 0, s>>>(a)
+  MOE_NORM_GEOM(a.d, MOE_NORM_FWD);
+#undef MOE_NORM_FWD
+  return launch_status();
+}
+int launch_norm_fwd(const moe_norm* n, const NormFwdArgs& a, hipStream_t s) {
+  if (n->dtype == MOE_DTYPE_F32) return norm_fwd_for<float, float>(a, s);
+  if (n->dtype == MOE_DTYPE_BF16) return n->stream == MOE_DTYPE_F32 ? norm_fwd_for<bf16, float>(a, s) : norm_fwd_for<bf16, bf16>(a, s);
+  return n->stream == MOE_DTYPE_F32 ? norm_fwd_for<f16, float>(a, s) : norm_fwd_for<f16, f16>(a, s);
+}
+
+template <typename T, typename S>
+static int norm_bwd_for(const NormBwdArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)norm_bwd_blocks(a.T, a.d);
+#define MOE_NORM_BWD(O_, W_, C_) norm_bwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(W_), 0, s>>>(a)
+  MOE_NORM_GEOM(a.d, MOE_NORM_BWD);
+#undef MOE_NORM_BWD
+  return launch_status();
+}
+template <typename OT>
+static int dgamma_for(const float* partials, int rows, int d, void* out, int accumulate, hipStream_t s) {
+  norm_dgamma_kernel<OT><<<(d + 15) / 16, 256, 0, s>>>(partials, rows, d, (OT*)out, accumulate);
+  return launch_status();
+}
+int launch_norm_bwd(const moe_norm* n, const NormBwdArgs& a, void* dgamma, int accumulate, hipStream_t s) {
+  int rc = MOE_OK, rows = 0;
+  if (n->T > 0) {
+    rows = norm_bwd_blocks(n->T, n->d);
+    if (n->dtype == MOE_DTYPE_F32) rc = norm_bwd_for<float, float>(a, s);
+    else if (n->dtype == MOE_DTYPE_BF16) rc = n->stream == MOE_DTYPE_F32 ? norm_bwd_for<bf16, float>(a, s) : norm_bwd_for<bf16, bf16>(a, s);
+    else rc = n->stream == MOE_DTYPE_F32 ? norm_bwd_for<f16, float>(a, s) : norm_bwd_for<f16, f16>(a, s);
+  }
+  if (rc != MOE_OK || dgamma == nullptr || (rows == 0 && accumulate)) return rc;
+  return n->grad == MOE_DTYPE_F32    ? dgamma_for<float>(a.partials, rows, n->d, dgamma, accumulate, s)
+         : n->grad == MOE_DTYPE_BF16 ? dgamma_for<bf16>(a.partials, rows, n->d, dgamma, accumulate, s)
+                                     : dgamma_for<f16>(a.partials, rows, n->d, dgamma, accumulate, s);
+}
+
+template <typename T>
+static int dropout_for(long long rows, int width, const DropArgs& drop, const void* x, const void* residual, void* y, hipStream_t s) {
+  const unsigned groups = (unsigned)((width + 7) / 8);
+  const long long items = rows * groups;
+  if (items >= 256 * 2048) {
+    dropout_kernel<T, 2><<<(unsigned)((items + 511) / 512), 256, 0, s>>>(drop, (const T*)x, (const T*)residual, (T*)y, rows, width, groups);
+  } else {
+    dropout_kernel<T, 1><<<(unsigned)((items + 255) / 256), 256, 0, s>>>(drop, (const T*)x, (const T*)residual, (T*)y, rows, width, groups);
+  }
+  return launch_status();
+}
+int launch_dropout(int dtype, long long rows, int width, const DropArgs& drop, const void* x, const void* residual, void* y, hipStream_t s) {
+  if (dtype == MOE_DTYPE_F32) return dropout_for<float>(rows, width, drop, x, residual, y, s);
+  if (dtype == MOE_DTYPE_BF16) return dropout_for<bf16>(rows, width, drop, x, residual, y, s);
+  return dropout_for<f16>(rows, width, drop, x, residual, y, s);
+}
+
+}  // namespace moe
