@@ -11,16 +11,18 @@
 
 namespace moe {
 
-template <typename T, typename S, bool ODD, int WPR, int NCH>
-__global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs a) {
-  constexpr int TPR = WPR * WAVE, R = rows_per_block(WPR);
-  __shared__ float s_sum[2][WPR];
-  __shared__ unsigned s_top[2][WPR];
-  const int tid = threadIdx.x % TPR, d = a.d;
+template <typename T, typename S, bool ODD, int MAXW, int NCH>
+__global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_fwd_kernel(NormFwdArgs a) {
+  constexpr int R = MAXW == 1 ? 4 : 1;
+  __shared__ __align__(16) float s_sum[2][MAXW];
+  __shared__ __align__(16) unsigned s_top[2][MAXW];
+  const int TPR = MAXW == 1 ? WAVE : (int)blockDim.x, tid = MAXW == 1 ? threadIdx.x % WAVE : threadIdx.x, d = a.d;
+  row_reduce_init<MAXW>(s_sum[0]);
+  row_reduce_init<MAXW>(s_top[0]);
   const T* gamma = reinterpret_cast<const T*>(a.gamma);
   const uint64_t offset = a.drop.cut != 0 ? drop_offset(a.drop) : 0;
   int turn = 0;
-  for (int row = blockIdx.x * R + threadIdx.x / TPR; row < a.T; row += gridDim.x * R, turn ^= 1) {
+  for (int row = blockIdx.x * R + (MAXW == 1 ? threadIdx.x / WAVE : 0); row < a.T; row += gridDim.x * R, turn ^= 1) {
     const size_t at = (size_t)row * d;
     const T* x = reinterpret_cast<const T*>(a.x) + at;
     Raw8<T> xr[NCH];
@@ -34,11 +36,11 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs 
     float v[NCH][8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      unpack8<T>(xr[i], v[i]);
+      unpack_row8<T, ODD>(xr[i], (i * TPR + tid) * 8, d, v[i]);
       if (a.drop.cut != 0) drop8(a.drop, offset, (uint32_t)row, (uint32_t)(i * TPR + tid), v[i]);
       if (a.residual != nullptr) {
         float q[8];
-        unpack8<S>(rr[i], q);
+        unpack_row8<S, ODD>(rr[i], (i * TPR + tid) * 8, d, q);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] += q[j];
       }
@@ -48,7 +50,7 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs 
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum = fmaf(v[i][j], v[i][j], sum);
     }
-    sum = row_reduce<WPR>(sum, s_sum[turn], add_f);
+    sum = row_reduce<MAXW>(sum, s_sum[turn], add_f);
     const float r = 1.f / sqrtf(sum / (float)d + a.eps);
     if (a.rstd != nullptr && tid == 0) a.rstd[row] = r;
     unsigned top = 0;
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs 
     for (int i = 0; i < NCH; ++i) {
       const int c = (i * TPR + tid) * 8;
       float g[8];
-      if (gamma != nullptr) unpack8<T>(load_row8<T, ODD, false>(gamma, c, d), g);
+      if (gamma != nullptr) unpack_row8<T, ODD>(load_row8<T, ODD, false>(gamma, c, d), c, d, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         v[i][j] *= r;
@@ -66,7 +68,7 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs 
       top = top_of(top, v[i]);
     }
     if (a.codes != nullptr) {
-      const RowScale q = row_scale(row_reduce<WPR>(top, s_top[turn], max_u));
+      const RowScale q = row_scale(row_reduce<MAXW>(top, s_top[turn], max_u));
       if (tid == 0) a.scales[row] = q.scale;
 #pragma unroll
       for (int i = 0; i < NCH; ++i) store_codes8<ODD>(a.codes + at, (i * TPR + tid) * 8, d, codes8(v[i], q.up));
@@ -74,36 +76,45 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_fwd_kernel(NormFwdArgs 
   }
 }
 
-template <typename T, typename S, bool ODD, int WPR, int NCH>
-__global__ __launch_bounds__(row_threads(WPR)) void norm_bwd_kernel(NormBwdArgs a) {
-  constexpr int TPR = WPR * WAVE, R = rows_per_block(WPR);
-  __shared__ float s_sum[2][WPR];
-  const int tid = threadIdx.x % TPR, d = a.d;
+template <typename T, typename S, bool ODD, int MAXW, int NCH>
+__global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_bwd_kernel(NormBwdArgs a) {
+  constexpr int R = MAXW == 1 ? 4 : 1;
+  __shared__ __align__(16) float s_sum[2][MAXW];
+  const int TPR = MAXW == 1 ? WAVE : (int)blockDim.x, tid = MAXW == 1 ? threadIdx.x % WAVE : threadIdx.x, d = a.d;
+  row_reduce_init<MAXW>(s_sum[0]);
   const T* gamma = reinterpret_cast<const T*>(a.gamma);
   const uint64_t offset = a.drop.cut != 0 ? drop_offset(a.drop) : 0;
   float dg[NCH][8] = {};
   int turn = 0;
-  for (int row = blockIdx.x * R + threadIdx.x / TPR; row < a.T; row += gridDim.x * R, turn ^= 1) {
+  // The next row is requested before this one is used, where registers hold both.
+  constexpr bool AHEAD = NCH < 4, ADD_EARLY = AHEAD || (sizeof(S) == 2 && !ODD);
+  struct Row { Raw8<T> dy[NCH]; Raw8<S> h[NCH], add[NCH]; float r; };
+  auto fetch = [&](int row, Row& f) {
+    if (row >= a.T) return;
     const size_t at = (size_t)row * d;
-    Raw8<T> yr[NCH];
-    Raw8<S> hr[NCH], ar[NCH];
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      yr[i] = load_row8<T, ODD>(reinterpret_cast<const T*>(a.dy) + at, (i * TPR + tid) * 8, d);
-      hr[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.h) + at, (i * TPR + tid) * 8, d);
+      f.dy[i] = load_row8<T, ODD>(reinterpret_cast<const T*>(a.dy) + at, (i * TPR + tid) * 8, d);
+      f.h[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.h) + at, (i * TPR + tid) * 8, d);
+      if (ADD_EARLY && a.dh_add != nullptr) f.add[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.dh_add) + at, (i * TPR + tid) * 8, d);
     }
-    if (a.dh_add != nullptr) {
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) ar[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.dh_add) + at, (i * TPR + tid) * 8, d);
-    }
-    const float r = a.rstd[row];
+    f.r = a.rstd[row];
+  };
+  Row now = {}, next = {};
+  const int first = blockIdx.x * R + (MAXW == 1 ? threadIdx.x / WAVE : 0), stride = gridDim.x * R;
+  if constexpr (AHEAD) fetch(first, now);
+  for (int row = first; row < a.T; row += stride, turn ^= 1) {
+    if constexpr (AHEAD) fetch(row + stride, next);
+    else fetch(row, now);
+    const size_t at = (size_t)row * d;
+    const float r = now.r;
     float w[NCH][8], u[NCH][8], dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      unpack8<T>(yr[i], w[i]);
-      unpack8<S>(hr[i], u[i]);
+      unpack_row8<T, ODD>(now.dy[i], (i * TPR + tid) * 8, d, w[i]);
+      unpack_row8<S, ODD>(now.h[i], (i * TPR + tid) * 8, d, u[i]);
       float g[8];
-      if (gamma != nullptr) unpack8<T>(load_row8<T, ODD, false>(gamma, (i * TPR + tid) * 8, d), g);
+      if (gamma != nullptr) unpack_row8<T, ODD>(load_row8<T, ODD, false>(gamma, (i * TPR + tid) * 8, d), (i * TPR + tid) * 8, d, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         u[i][j] *= r;
@@ -112,12 +123,15 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_bwd_kernel(NormBwdArgs 
         dot = fmaf(w[i][j], u[i][j], dot);
       }
     }
-    dot = row_reduce<WPR>(dot, s_sum[turn], add_f) / (float)d;
+    dot = row_reduce<MAXW>(dot, s_sum[turn], add_f) / (float)d;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
       const int c = (i * TPR + tid) * 8;
       float q[8];
-      if (a.dh_add != nullptr) unpack8<S>(ar[i], q);
+      if (a.dh_add != nullptr) {
+        if constexpr (!ADD_EARLY) now.add[i] = load_row8<S, ODD>(reinterpret_cast<const S*>(a.dh_add) + at, c, d);
+        unpack_row8<S, ODD>(now.add[i], c, d, q);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         w[i][j] = r * (w[i][j] - u[i][j] * dot);
@@ -129,28 +143,29 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_bwd_kernel(NormBwdArgs 
         store_row8<T, ODD>(reinterpret_cast<T*>(a.dx) + at, c, d, pack_row8<T>(w[i]));
       }
     }
+    if constexpr (AHEAD) now = next;
   }
   if (a.partials == nullptr) return;
   float* out = a.partials + (size_t)blockIdx.x * d;
   if constexpr (R > 1) {   // the block's waves one after the other: the same order every time
-    __shared__ float s_dg[NCH * TPR * 8];
+    __shared__ float s_dg[NCH * WAVE * 8];
     for (int w = 1; w < R; ++w) {
-      if ((int)threadIdx.x / TPR == w) {
+      if ((int)threadIdx.x / WAVE == w) {
 #pragma unroll
         for (int i = 0; i < NCH; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) s_dg[(i * 8 + j) * TPR + tid] = dg[i][j];
+          for (int j = 0; j < 8; ++j) s_dg[(i * 8 + j) * WAVE + tid] = dg[i][j];
       }
       __syncthreads();
-      if ((int)threadIdx.x < TPR) {
+      if (threadIdx.x < WAVE) {
 #pragma unroll
         for (int i = 0; i < NCH; ++i)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dg[i][j] += s_dg[(i * 8 + j) * TPR + tid];
+          for (int j = 0; j < 8; ++j) dg[i][j] += s_dg[(i * 8 + j) * WAVE + tid];
       }
       __syncthreads();
     }
-    if ((int)threadIdx.x >= TPR) return;
+    if (threadIdx.x >= WAVE) return;
   }
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
@@ -161,22 +176,26 @@ __global__ __launch_bounds__(row_threads(WPR)) void norm_bwd_kernel(NormBwdArgs 
   }
 }
 
-// Column sums of the partial sums: 16 columns by 16 rows at a time, whose sums are added in order.
+// Column sums of the partial sums: 16 columns by 64 rows at a time, whose sums are added in order.  (16 rows at a time: 6.6 us for 1024
+// rows of 4096, every thread 64 loads long.)
+constexpr int DGAMMA_ROWS = 64;
 template <typename OT>
-__global__ __launch_bounds__(256) void norm_dgamma_kernel(const float* partials, int rows, int d, OT* out, int accumulate) {
-  __shared__ float part[16][17];
+__global__ __launch_bounds__(16 * DGAMMA_ROWS) void norm_dgamma_kernel(const float* partials, int rows, int d, OT* out, int accumulate) {
+  __shared__ float part[DGAMMA_ROWS][17];
   const int cl = threadIdx.x & 15, rl = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
   float sum = 0.f;
   if (c < d) {
 #pragma unroll 8
-    for (int r = rl; r < rows; r += 16) sum += partials[(size_t)r * d + c];
+    for (int r = rl; r < rows; r += DGAMMA_ROWS) sum += partials[(size_t)r * d + c];
   }
   part[rl][cl] = sum;
   __syncthreads();
-  if (rl != 0 || c >= d) return;
+  if (rl >= 4) return;
 #pragma unroll
-  for (int r = 1; r < 16; ++r) sum += part[r][cl];
-  out[c] = from_f32<OT>(sum + (accumulate ? to_f32(out[c]) : 0.f));
+  for (int r = 4; r < DGAMMA_ROWS; r += 4) sum += part[rl + r][cl];
+  sum += __shfl_down(sum, 32, WAVE);   // rows 0 and 2, 1 and 3; then those two
+  sum += __shfl_down(sum, 16, WAVE);
+  if (rl == 0 && c < d) out[c] = from_f32<OT>(sum + (accumulate ? to_f32(out[c]) : 0.f));
 }
 
 // A thread takes U groups of eight adjacent values, 256 apart, and requests them all before it uses the first.  Rows are found by a
@@ -202,11 +221,11 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs drop, const T* x,
   for (int u = 0; u < U; ++u) {
     if (row[u] >= rows) break;
     float v[8];
-    unpack8<T>(xr[u], v);
+    unpack_row8<T, true>(xr[u], (int)g[u] * 8, width, v);
     if (drop.cut != 0) drop8(drop, offset, (uint32_t)row[u], g[u], v);
     if (residual != nullptr) {
       float q[8];
-      unpack8<T>(rr[u], q);
+      unpack_row8<T, true>(rr[u], (int)g[u] * 8, width, q);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += q[j];
     }
@@ -217,25 +236,24 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs drop, const T* x,
 // ---- launches ------------------------------------------------------------------------------------------------------
 constexpr int NORM_MOST_BLOCKS = 1 << 16;   // further rows in further turns
 
-// F(odd, waves per row, groups per thread) for rows of d values; rows of no whole groups have fewer variants (norm_geom).
-#define MOE_NORM_GEOM(D_, F_)                                                                              \
-  do {                                                                                                     \
-    const RowGeom g_ = norm_geom(D_);                                                                      \
-    if ((D_) % 8 != 0) { if (g_.wpr == 1) F_(true, 1, 2); else if (g_.wpr == 4) F_(true, 4, 2); else F_(true, 8, 4); } \
-    else if (g_.wpr == 8) F_(false, 8, 4);                                                                 \
-    else if (g_.wpr == 4) { if (g_.nch == 2) F_(false, 4, 2); else F_(false, 4, 4); }                      \
-    else if (g_.nch == 1) F_(false, 1, 1);                                                                 \
-    else if (g_.nch == 2) F_(false, 1, 2);                                                                 \
-    else F_(false, 1, 4);                                                                                  \
+// F(odd, most waves of a row, groups per thread) by the geometry of a row.
+#define MOE_NORM_GEOM_(O_, G_, F_)                                          \
+  do {                                                                      \
+    if (G_.waves == 1) { if (G_.nch == 1) F_(O_, 1, 1); else F_(O_, 1, 2); } \
+    else if (G_.nch == 1) F_(O_, 8, 1);                                     \
+    else if (G_.nch == 2) F_(O_, 8, 2);                                     \
+    else F_(O_, 8, 4);                                                      \
   } while (0)
+#define MOE_NORM_GEOM(D_, G_, F_) do { if ((D_) % 8 != 0) MOE_NORM_GEOM_(true, G_, F_); else MOE_NORM_GEOM_(false, G_, F_); } while (0)
 
 template <typename T, typename S>
 static int norm_fwd_for(const NormFwdArgs& a, hipStream_t s) {
-  const int rows = rows_per_block(norm_geom(a.d).wpr);
+  const RowGeom geom = norm_geom(a.T, a.d);
+  const int rows = rows_per_block(geom);
   const long long want = ((long long)a.T + rows - 1) / rows;
   const unsigned grid = (unsigned)(want < NORM_MOST_BLOCKS ? want : NORM_MOST_BLOCKS);
-#define MOE_NORM_FWD(O_, W_, C_) norm_fwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(W_), 0, s>>>(a)
-  MOE_NORM_GEOM(a.d, MOE_NORM_FWD);
+#define MOE_NORM_FWD(O_, W_, C_) norm_fwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(geom), 0, s>>>(a)
+  MOE_NORM_GEOM(a.d, geom, MOE_NORM_FWD);
 #undef MOE_NORM_FWD
   return launch_status();
 }
@@ -247,15 +265,16 @@ int launch_norm_fwd(const moe_norm* n, const NormFwdArgs& a, hipStream_t s) {
 
 template <typename T, typename S>
 static int norm_bwd_for(const NormBwdArgs& a, hipStream_t s) {
+  const RowGeom geom = norm_geom(a.T, a.d);
   const unsigned grid = (unsigned)norm_bwd_blocks(a.T, a.d);
-#define MOE_NORM_BWD(O_, W_, C_) norm_bwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(W_), 0, s>>>(a)
-  MOE_NORM_GEOM(a.d, MOE_NORM_BWD);
+#define MOE_NORM_BWD(O_, W_, C_) norm_bwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(geom), 0, s>>>(a)
+  MOE_NORM_GEOM(a.d, geom, MOE_NORM_BWD);
 #undef MOE_NORM_BWD
   return launch_status();
 }
 template <typename OT>
 static int dgamma_for(const float* partials, int rows, int d, void* out, int accumulate, hipStream_t s) {
-  norm_dgamma_kernel<OT><<<(d + 15) / 16, 256, 0, s>>>(partials, rows, d, (OT*)out, accumulate);
+  norm_dgamma_kernel<OT><<<(d + 15) / 16, 16 * DGAMMA_ROWS, 0, s>>>(partials, rows, d, (OT*)out, accumulate);
   return launch_status();
 }
 int launch_norm_bwd(const moe_norm* n, const NormBwdArgs& a, void* dgamma, int accumulate, hipStream_t s) {

@@ -5,26 +5,27 @@
 namespace moe {
 
 // One pass: a row stays in registers between its maximum and its codes.
-template <typename T, bool ODD, int WPR, int NCH>
-__global__ __launch_bounds__(row_threads(WPR)) void quant_rows_kernel(const T* src, long long rows, int width, long long pitch, RowRange range,
+template <typename T, bool ODD, int MAXW, int NCH>
+__global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void quant_rows_kernel(const T* src, long long rows, int width, long long pitch, RowRange range,
                                                                              int8_t* codes, float* scales) {
-  constexpr int TPR = WPR * WAVE, R = rows_per_block(WPR);
+  constexpr int R = MAXW == 1 ? 4 : 1;
   __shared__ int32_t s_range[2 * MOE_MAX_E];
-  __shared__ unsigned s_top[2][WPR];
+  __shared__ unsigned s_top[2][MAXW];
   const RangeTable rt = load_range(range, s_range);
   const long long end = rt.limit(rows);
-  const int tid = threadIdx.x % TPR;
+  const int TPR = MAXW == 1 ? WAVE : (int)blockDim.x, tid = MAXW == 1 ? threadIdx.x % WAVE : threadIdx.x;
+  row_reduce_init<MAXW>(s_top[0]);
   int turn = 0;
-  for (long long row = (long long)blockIdx.x * R + threadIdx.x / TPR; row < end; row += (long long)gridDim.x * R) {
+  for (long long row = (long long)blockIdx.x * R + (MAXW == 1 ? threadIdx.x / WAVE : 0); row < end; row += (long long)gridDim.x * R) {
     if (!rt.live(row)) continue;   // (the same for every thread of a row, and of a block where several waves share one)
     float v[NCH][8];
     unsigned top = 0;
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      unpack8<T>(load_row8<T, ODD>(src + row * pitch, (i * TPR + tid) * 8, width), v[i]);
+      unpack_row8<T, ODD>(load_row8<T, ODD>(src + row * pitch, (i * TPR + tid) * 8, width), (i * TPR + tid) * 8, width, v[i]);
       top = top_of(top, v[i]);
     }
-    const RowScale q = row_scale(row_reduce<WPR>(top, s_top[turn], max_u));
+    const RowScale q = row_scale(row_reduce<MAXW>(top, s_top[turn], max_u));
     turn ^= 1;
     if (tid == 0) scales[row] = q.scale;
 #pragma unroll
@@ -82,27 +83,33 @@ __global__ __launch_bounds__(256) void quant_weight_kernel(const T* W, int d_in,
 }
 
 constexpr int QUANT_MOST_BLOCKS = 1 << 16;   // further rows in further turns
+// Two to four groups of eight per thread: a row is short work, and threads with several requests in flight make more of it than more
+// threads.  (32768 rows of 4096 bf16, us: one group in eight waves 81, two in four waves 63; 16384 of 2048: 22.7, 19.1, four in one
+// wave 18.4; 3001 of 2880 8.2, 6.4.)
 static RowGeom quant_geom(int width) {
   const int g = (width + 7) / 8;
-  if (width % 8 != 0) return g <= 256 ? RowGeom{1, 4} : g <= 1024 ? RowGeom{4, 4} : RowGeom{16, 8};
-  return g <= 128 ? RowGeom{1, 2} : g <= 256 ? RowGeom{1, 4} : g <= 512 ? RowGeom{4, 2} : g <= 1024 ? RowGeom{4, 4} : g <= 2048 ? RowGeom{4, 8} : g <= 4096 ? RowGeom{16, 4} : RowGeom{16, 8};
+  if (g <= 128) return {1, 2};
+  if (g <= 256) return {1, 4};
+  const int nch = g <= 512 ? 2 : g <= 4096 ? 4 : 8;
+  return {row_waves(g, nch), nch};
 }
-static_assert(MOE_MAX_ROW == 16 * WAVE * 8 * 8, "the widest variant");
+static_assert(MOE_MAX_ROW == 16 * WAVE * 8 * 8, "sixteen waves hold the widest row");
 template <typename T>
 static int quant_rows_for(long long rows, int width, long long pitch, const void* src, const RowRange& range, int8_t* codes, float* scales, hipStream_t s) {
   const RowGeom g = quant_geom(width);
-  const long long per = rows_per_block(g.wpr), want = (rows + per - 1) / per;
+  const long long per = rows_per_block(g), want = (rows + per - 1) / per;
   const unsigned grid = (unsigned)(want < QUANT_MOST_BLOCKS ? want : QUANT_MOST_BLOCKS);
-#define MOE_QUANT_ROWS(O_, W_, C_) quant_rows_kernel<T, O_, W_, C_><<<grid, row_threads(W_), 0, s>>>((const T*)src, rows, width, pitch, range, codes, scales)
-  if (width % 8 != 0) {
-    if (g.wpr == 1) MOE_QUANT_ROWS(true, 1, 4); else if (g.wpr == 4) MOE_QUANT_ROWS(true, 4, 4); else MOE_QUANT_ROWS(true, 16, 8);
-  } else if (g.wpr == 1) {
-    if (g.nch == 2) MOE_QUANT_ROWS(false, 1, 2); else MOE_QUANT_ROWS(false, 1, 4);
-  } else if (g.wpr == 4) {
-    if (g.nch == 2) MOE_QUANT_ROWS(false, 4, 2); else if (g.nch == 4) MOE_QUANT_ROWS(false, 4, 4); else MOE_QUANT_ROWS(false, 4, 8);
-  } else {
-    if (g.nch == 4) MOE_QUANT_ROWS(false, 16, 4); else MOE_QUANT_ROWS(false, 16, 8);
-  }
+#define MOE_QUANT_ROWS(O_, W_, C_) quant_rows_kernel<T, O_, W_, C_><<<grid, row_threads(g), 0, s>>>((const T*)src, rows, width, pitch, range, codes, scales)
+#define MOE_QUANT_GEOM(O_)                        \
+  do {                                            \
+    if (g.waves == 1) { if (g.nch == 2) MOE_QUANT_ROWS(O_, 1, 2); else MOE_QUANT_ROWS(O_, 1, 4); } \
+    else if (g.nch == 2) MOE_QUANT_ROWS(O_, 4, 2); \
+    else if (g.nch == 4 && g.waves <= 8) MOE_QUANT_ROWS(O_, 8, 4); \
+    else if (g.nch == 4) MOE_QUANT_ROWS(O_, 16, 4); \
+    else MOE_QUANT_ROWS(O_, 16, 8);               \
+  } while (0)
+  if (width % 8 != 0) MOE_QUANT_GEOM(true);
+  else MOE_QUANT_GEOM(false);
 #undef MOE_QUANT_ROWS
   return launch_status();
 }

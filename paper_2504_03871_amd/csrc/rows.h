@@ -5,11 +5,12 @@
 
 namespace moe {
 
-// A row is dealt out in groups of eight values to the threads of WPR waves, NCH groups each, neighbours to neighbours.  One wave per
-// row (four rows to a block of 256 threads) needs no barrier; more waves per row where one could not hold it.
-struct RowGeom { int wpr, nch; };
-constexpr int row_threads(int wpr) { return wpr * WAVE < 256 ? 256 : wpr * WAVE; }
-constexpr int rows_per_block(int wpr) { return row_threads(wpr) / (wpr * WAVE); }
+// A row is dealt out in groups of eight values, neighbours to neighbours, `nch` to a thread: to one wave, four rows to a block of 256
+// threads and no barrier, or to `waves` waves of a block of their own, as few as hold the row so that no thread is idle.
+struct RowGeom { int waves, nch; };
+inline int row_threads(const RowGeom& g) { return g.waves == 1 ? 256 : g.waves * WAVE; }
+inline int rows_per_block(const RowGeom& g) { return g.waves == 1 ? 4 : 1; }
+inline int row_waves(int groups, int nch) { return (groups + WAVE * nch - 1) / (WAVE * nch); }
 
 #ifdef __HIPCC__
 // Vectors that may start at any element: rows of any width are read and written 16 bytes at a time.
@@ -48,26 +49,44 @@ __device__ __forceinline__ Raw8<T> pack_row8(const float (&v)[8]) {
   }
   return r;
 }
-// Values c .. c + 7 of a row of `width`; those past its end are zero, and are not written.
-// ODD: whether a row may end inside a group of eight.
+// Values c .. c + 7 of a row of `width`; those past its end are zero, and are not written.  ODD: a row may end inside a group of eight.
+// Its last group is then read as the row's last eight values, so that every lane makes the same vector load, and moved into place
+// behind it (place8).  (Value by value, which makes a wave wait for up to seven loads in turn: rows of 516 fp32, 300 of them, 5.2
+// instead of 4.2 us, 3001 of 1091 fp16 18 instead of 9.)
 template <typename T, bool ODD, bool NT = true>
 __device__ __forceinline__ Raw8<T> load_row8(const T* row, int c, int width) {
-  Raw8<T> r;
-  if (c + 8 <= width) {
+  Raw8<T> r = {};
+  if (ODD && width < 8) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < width ? to_f32(row[c + i]) : 0.f;
+    return pack_row8<T>(v);   // exact: they come from this type
+  }
+  if (ODD ? c < width : c + 8 <= width) {
+    const int at = ODD ? min(c, width - 8) : c;
 #pragma unroll
     for (int i = 0; i < Raw8<T>::N; ++i) {
-      const any_u32x4* p = reinterpret_cast<const any_u32x4*>(row + c) + i;
+      const any_u32x4* p = reinterpret_cast<const any_u32x4*>(row + at) + i;
       r.q[i] = NT ? __builtin_nontemporal_load(p) : *p;
     }
-  } else {
-    float v[8] = {};
-    if (ODD && c < width) {
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] = c + i < width ? to_f32(row[c + i]) : 0.f;
-    }
-    r = pack_row8<T>(v);   // exact: they come from this type
   }
   return r;
+}
+template <bool ODD>
+__device__ __forceinline__ void place8(float (&v)[8], int c, int width) {
+  if (!ODD || c >= width || c + 8 <= width || width < 8) return;
+  const int by = 8 - width % 8;   // the same for every row
+#pragma unroll
+  for (int s = 4; s > 0; s >>= 1)
+    if ((by & s) != 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i + s < 8 ? v[i + s] : 0.f;
+    }
+}
+template <typename T, bool ODD>
+__device__ __forceinline__ void unpack_row8(const Raw8<T>& r, int c, int width, float (&v)[8]) {
+  unpack8<T>(r, v);
+  place8<ODD>(v, c, width);
 }
 template <typename T, bool ODD>
 __device__ __forceinline__ void store_row8(T* row, int c, int width, const Raw8<T>& r) {
@@ -89,18 +108,25 @@ __device__ __forceinline__ V wave_reduce(V v, F f) {
   for (int s = 32; s > 0; s >>= 1) v = f(v, __shfl_xor(v, s, WAVE));
   return v;
 }
-// Over the WPR waves of a row; every thread gets the result.  `lds`: WPR values that no reduction since the last barrier but one
-// has used (rows alternate between two sets).
-template <int WPR, typename V, typename F>
+// Over the waves of a row, at most MAXW (1: a wave has a row); every thread gets the result.  `lds`: MAXW values, zeros for waves that the
+// block does not have (row_reduce_init), and none that a reduction since the last barrier but one has used: rows alternate
+// between two sets.
+template <int MAXW, typename V>
+__device__ __forceinline__ void row_reduce_init(V* lds) {   // both sets
+  if constexpr (MAXW > 1) {
+    if (threadIdx.x < 2 * MAXW) lds[threadIdx.x] = V(0);
+    __syncthreads();
+  }
+}
+template <int MAXW, typename V, typename F>
 __device__ __forceinline__ V row_reduce(V v, V* lds, F f) {
   v = wave_reduce(v, f);
-  if constexpr (WPR > 1) {
-    const int w = threadIdx.x / WAVE;
-    if (threadIdx.x % WAVE == 0) lds[w] = v;
+  if constexpr (MAXW > 1) {
+    if (threadIdx.x % WAVE == 0) lds[threadIdx.x / WAVE] = v;
     __syncthreads();
     v = lds[0];
 #pragma unroll
-    for (int i = 1; i < WPR; ++i) v = f(v, lds[i]);
+    for (int i = 1; i < MAXW; ++i) v = f(v, lds[i]);
   }
   return v;
 }
