@@ -489,7 +489,7 @@ MOE_API int moe_dropout(int32_t dtype, int64_t rows, int32_t width, const moe_dr
  * Backward: a = gamma dy, u = h rstd; dh = rstd (a - u mean(a u)) + dh_add (NULL: nothing; the gradient that reaches h by other ways), which
  * is the gradient of residual too; dx = dropout's gradient of dh; dgamma = sum over the rows of dy u.  dh, dx, dgamma may be NULL: skipped;
  * dh may be dh_add, and dx may be dy (not dh: MOE_ERR_OVERLAP).  dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or
- * dtype (accumulate must be 0).  ws holds moe_norm_bwd_workspace_bytes and is needed for dgamma only.  No atomics: the same bits every time.
+ * dtype (accumulate must be 0).  ws holds moe_norm_bwd_workspace_bytes (enough for any smaller T too) and is needed for dgamma only.  No atomics: the same bits every time.
  */
 #define MOE_MAX_NORM 16384
 typedef struct moe_norm {
@@ -524,8 +524,9 @@ MOE_API int moe_quant_weight(int32_t dtype, int32_t n, int32_t d_in, int32_t d_o
  *   x codes [T][d_in] and x_scales [T] as moe_quant_rows writes them, W, Wb and w_scales, wb_scales [d_out] as moe_quant_weight does (codes of
  *   other origin may be -128); bias, bias_b, residual, y in the storage type `dtype`, as in moe_linear_fwd, act too.
  * Sums are 32-bit integers, exact; z, the activation and the residual's addition are fp32 and rounded once.
- * Shapes: 0 <= T <= 2^24, d_in and d_out multiples of 64, d_in <= MOE_MAX_ROW, d_out <= 2^20, d_in * d_out < 2^31, T * d_in < 2^32.
- * `ws` holds moe_linear8_workspace_bytes and is free again when the call is done.
+ * Shapes: 0 <= T <= 2^24, d_in and d_out multiples of 64, d_in <= MOE_MAX_ROW, d_out <= 2^20, d_in * d_out < 2^31.
+ * `ws` holds moe_linear8_workspace_bytes, which is enough for any smaller T too and 0 up to 32 (ws may be NULL then), and is free again when
+ * the call is done.  A row's result is the same bits whatever T is and whatever stands in the other rows.
  */
 typedef struct moe_linear8 {
   int32_t T, d_in, d_out;

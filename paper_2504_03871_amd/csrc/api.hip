@@ -1124,10 +1124,7 @@ static int check_linear8(const moe_linear8* c) {
     return MOE_ERR_BAD_SHAPE;
   return MOE_OK;
 }
-static size_t linear8_need(const moe_linear8* c) {
-  const int mats = c->act == MOE_ACT_SWIGLU ? 2 : 1;
-  return c->T == 0 ? 0 : linear8_ws_bytes(cut_linear8(c->T, c->d_out, c->d_in, mats), c->T, c->d_out, mats);
-}
+static size_t linear8_need(const moe_linear8* c) { return linear8_ws_bytes(c->T, c->d_out, c->act == MOE_ACT_SWIGLU ? 2 : 1); }
 
 int moe_linear8_workspace_bytes(const moe_linear8* lin, size_t* bytes) {
   CHECK(check_linear8(lin));
@@ -1146,8 +1143,9 @@ int moe_linear8_fwd(const moe_linear8* lin, const void* x, const float* x_scales
   if (!two && (Wb != nullptr || wb_scales != nullptr || bias_b != nullptr)) return MOE_ERR_BAD_DTYPE;
   ALIGNED(x); ALIGNED(x_scales); ALIGNED(W); ALIGNED(w_scales); ALIGNED(Wb); ALIGNED(wb_scales); ALIGNED(bias); ALIGNED(bias_b); ALIGNED(residual);
   ALIGNED(y); ALIGNED(ws);
-  REQUIRE(ws);
-  if (ws_bytes < linear8_need(lin)) return MOE_ERR_WORKSPACE;
+  const size_t need = linear8_need(lin);
+  if (need > 0) REQUIRE(ws);
+  if (ws_bytes < need) return MOE_ERR_WORKSPACE;
   return launch_linear8(lin, x, x_scales, W, w_scales, Wb, wb_scales, bias, bias_b, residual, y, ws, (hipStream_t)stream);
 }
 
@@ -1211,7 +1209,7 @@ int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales
   int8_t* codes = reinterpret_cast<int8_t*>(w + l.codes);
   float* scales = reinterpret_cast<float*>(w + l.scales);
   Gemm8Args g1 = g, g2 = g;
-  g1.A = static_cast<const int8_t*>(x); g1.a_scale = x_scales; g1.src_of = src_of; g1.per_row = cfg->k; g1.src_rows = cfg->T;
+  g1.A = static_cast<const int8_t*>(x); g1.a_scale = x_scales; g1.src_of = src_of; g1.per_row = quotient_factor(cfg->k); g1.src_rows = cfg->T;
   g1.B = static_cast<const int8_t*>(W1); g1.B2 = static_cast<const int8_t*>(W1b); g1.b_scale = w1_scales; g1.b2_scale = w1b_scales;
   g1.N = f; g1.K = d; g1.C = w + l.hidden;
   CHECK(launch_expert8(cfg->dtype, cfg->act, g1, tr, max_tiles, A, s));

@@ -9,7 +9,8 @@ struct Gemm8Args {
   const int8_t* A;          // [rows][K]
   const float* a_scale;     // [rows]
   const int32_t* src_of;    // experts' first product: row r of the permuted order is row src_of[r] / per_row of A; NULL: r itself
-  int per_row, src_rows;    // assignments per row of A, and how many rows it has
+  int src_rows;             // rows of A
+  uint64_t per_row;         // assignments per row of A, as a factor (quotient_factor)
   const int8_t *B, *B2;     // tiles of quant8.h, a matrix (or two) or one for each expert
   const float *b_scale, *b2_scale;
   const void *bias, *bias2, *residual;   // storage type, may be NULL
@@ -21,15 +22,24 @@ struct Gemm8Args {
   const int32_t *offsets, *kept, *lo, *hi;
   int E;
   int chunked;              // order of the tiles (block_to_tile)
-  int32_t* parts;           // few rows, dense: sums of K parts, [part][matrix][row][N]
+  int few_nk;               // few rows: waves that share a strip's K range (1, 2, 4 or 8)
+  int32_t* parts;           // dense tiles: sums of K parts, [part][matrix][row][N]
   int n_parts;
 };
 
-// How a product is cut: few rows (row groups of `rows` = 16, 32 or 64, strips of 16 columns, K parts), or tiles of rows x cols.
+// a / k for 0 <= a < 2^30 and 1 <= k <= 8 as a * factor >> 33: the factor is above 2^33 / k by at most one, so the quotient by at most
+// 2^30 / 2^33 = 1 / 8, which carries no fraction (r / k, r < k) up to the next whole number.  (k = 8: a < 2^30, so by less than 1 / 8.)
+inline uint64_t quotient_factor(int k) { return (1ull << 33) / k + 1; }
+static_assert(MOE_MAX_K <= 8, "quotient_factor");
+
+// How a product is cut: up to 32 rows (rows = 16 or 32) in strips of 16 columns, else tiles of rows x cols, their K range in `parts`.
+constexpr int FEW_ROWS8 = 32, MAX_PARTS8 = 8;
 struct Cut8 { bool few; int rows, cols, parts; };
 Cut8 cut_linear8(long long T, int N, int K, int mats);
-inline size_t linear8_ws_bytes(const Cut8& c, long long T, int N, int mats) {
-  return c.few && c.parts > 1 ? align_up((size_t)c.parts * mats * T * N * 4, 256) : 256;   // (a call without one is a mistake still)
+// Room for the parts' sums: enough for any smaller T too.  Tiles that are cut make one round of blocks, 512 of 128 x 128 sums at most.
+inline size_t linear8_ws_bytes(long long T, int N, int mats) {
+  const size_t all = (size_t)MAX_PARTS8 * mats * T * N * 4, most = (size_t)512 * 128 * 128 * 4;
+  return T <= FEW_ROWS8 ? 0 : align_up(all < most ? all : most, 256);
 }
 // Row tiles of the experts' products: 0 for the few-row kernel
 int expert8_tile_rows(long long rows, int E);

@@ -52,7 +52,9 @@ __device__ __forceinline__ i32x4 mfma8(const i32x4& a, const i32x4& b, const i32
 
 // Row of A behind row r of the product: the token of an assignment (held inside A whatever the index says), or the row itself.
 __device__ __forceinline__ int row_of_a(const Gemm8Args& g, int r) {
-  return g.src_of == nullptr ? r : min(max(g.src_of[r] / g.per_row, 0), g.src_rows - 1);
+  if (g.src_of == nullptr) return r;
+  const int a = max(g.src_of[r], 0);
+  return min((int)((uint64_t)(unsigned)a * g.per_row >> 33), g.src_rows - 1);
 }
 
 template <int BM, int BN, bool DUAL>
@@ -72,8 +74,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WGN, wn = wave % WGN;
   const int ntn = (g.N + BN - 1) / BN, n_rt = GROUPED ? g.ntiles[0] : (g.M + BM - 1) / BM, n_full = GROUPED ? g.ntiles[1] : g.M / BM;
+  const int n_parts = GROUPED ? 1 : g.n_parts, part = n_parts > 1 ? blockIdx.x % n_parts : 0;
   int rt, nt;
-  if (!block_to_tile(blockIdx.x, n_rt, n_full, ntn, g.chunked != 0, rt, nt)) return;
+  if (!block_to_tile(n_parts > 1 ? blockIdx.x / n_parts : blockIdx.x, n_rt, n_full, ntn, g.chunked != 0, rt, nt)) return;
   rt = __builtin_amdgcn_readfirstlane(rt);
   nt = __builtin_amdgcn_readfirstlane(nt);
   RowTile t;
@@ -83,6 +86,15 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
   const int n0 = nt * BN, K = g.K;
   const int ni = min(max(((mvalid + 31) / 32 - wm + WGM - 1) / WGM, 0), WTM);   // this wave's 32-row bands with valid rows
 
+  // The tile's scales, one per thread: BM of rows, BN (twice) of columns.  Requested here and passed round in LDS when that is free, so that
+  // no wave waits for memory between the last product and the first result.
+  static_assert(BM + BN * (DUAL ? 2 : 1) <= NT * 2 && BM <= NT, "two values per thread at most");
+  const float* b_scale = g.b_scale + (size_t)e * g.N;
+  const float* b2_scale = DUAL ? g.b2_scale + (size_t)e * g.N : b_scale;
+  const float my_row = tid < BM ? g.a_scale[row_of_a(g, row0 + min(tid, mvalid - 1))] : 0.f;
+  const float my_col = tid < BN ? b_scale[min(n0 + tid, g.N - 1)] : 0.f;
+  const float my_col2 = DUAL && tid < BN ? b2_scale[min(n0 + tid, g.N - 1)] : 0.f;
+
   i32x4 acc[TM][TNN] = {}, acc2[DUAL ? TM : 1][DUAL ? TNN : 1] = {};
 
   // operands: of A the rows of this tile (by token: all of it), of B this expert's matrix
@@ -90,7 +102,8 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
   const rsrc_t ra = gather ? make_rsrc(g.A, (size_t)g.src_rows * K) : make_rsrc(g.A + (size_t)row0 * K, (size_t)mvalid * K);
   const size_t mat = (size_t)g.N * K;
   const rsrc_t rb = make_rsrc(g.B + e * mat, mat), rb2 = make_rsrc((DUAL ? g.B2 : g.B) + e * mat, mat);
-  const int KT = K / TILE8_K, KS = (KT + 1) / 2;   // tiles of 64 K values, stages
+  const int KT = K / TILE8_K, stages = (KT + 1) / 2;   // tiles of 64 K values, stages
+  const int S0 = part * stages / n_parts, KS = (part + 1) * stages / n_parts;   // this block's
   unsigned a_vo[LA], b_vo[LB1];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
@@ -166,9 +179,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 #pragma unroll
     for (int q = 0; q < LA; ++q) load_a(q, stage, abuf);
   };
-  prologue(0, a0, b0);
-  if (KS > 1) {
-    prologue(1, a1, b1);
+  prologue(S0, a0, b0);
+  if (KS - S0 > 1) {
+    prologue(S0 + 1, a1, b1);
     __builtin_amdgcn_s_waitcnt(WAIT_P);
   } else {
     __builtin_amdgcn_s_waitcnt(0x70 | (15 << 8));
@@ -207,7 +220,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
       const int a = a0; a0 = a1; a1 = a2; a2 = a;
       const int b = b0; b0 = b1; b1 = b;
     };
-    int S = 0;
+    int S = S0;
 #pragma unroll 1
     for (; S + 2 < KS; ++S) iteration(S, true, Const<1>{});
 #pragma unroll 1
@@ -216,50 +229,125 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
   if (ni == WTM) mainloop(WTM);
   else mainloop(ni);
 
-  // Epilogue.  act(z) in the accumulators' layout, then exchanges between lanes to whole lines (gemm_bf16_kernel.h), the residual there.
+  if (!GROUPED && n_parts > 1) {   // 32-bit sums of this K part, whole lines
+    constexpr int CW = TNN * 16;
+    if (n0 + wn * CW >= g.N) return;
+    auto put = [&](i32x4 (&s)[TM][TNN], int matrix) {
+      int32_t* out = g.parts + ((size_t)(part * (DUAL ? 2 : 1) + matrix) * g.M + row0) * g.N + n0 + wn * CW;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TNN; j += 2) {
+          u32x4 v[2] = {__builtin_bit_cast(u32x4, s[i][j]), __builtin_bit_cast(u32x4, s[i][j + 1])};
+          swap8(v[0], v[1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int m = ((i >> 1) * WGM + wm) * 32 + (i & 1) * 16 + h * 8 + (lane & 7);
+            if (m < mvalid) *reinterpret_cast<u32x4*>(out + (size_t)m * g.N + j * 16 + ((lane >> 3) & 1) * 16 + (lane >> 4) * 4) = v[h];
+          }
+        }
+    };
+    put(acc, 0);
+    if constexpr (DUAL) put(acc2, 1);
+    return;
+  }
+
+  // Epilogue.  The scales round LDS, act(z) in the accumulators' layout, then exchanges between lanes to whole lines (gemm_bf16_kernel.h).
+  float* s_row = reinterpret_cast<float*>(smem);
+  float* s_col = s_row + BM;
+  barrier();   // every wave has read its last fragments
+  if (tid < BM) s_row[tid] = my_row;
+  if (tid < BN) {
+    s_col[tid] = my_col;
+    if constexpr (DUAL) s_col[BN + tid] = my_col2;
+  }
+  __syncthreads();
   constexpr int C = TNN * 16;
   const int col_w = n0 + wn * C;
   if (col_w >= g.N) return;
   const int grp = lane >> 4, r8 = lane & 7, right = (lane >> 3) & 1;
-  const float* bs = g.b_scale + (size_t)e * g.N;
-  const float* bs2 = DUAL ? g.b2_scale + (size_t)e * g.N : bs;
   const size_t first = (size_t)row0 * g.N + n0, bytes = ((size_t)mvalid * g.N - n0) * sizeof(ST);
   const __amdgpu_buffer_rsrc_t oy = out_rsrc(reinterpret_cast<ST*>(g.C) + first, bytes);
-  const __amdgpu_buffer_rsrc_t res = out_rsrc(reinterpret_cast<const ST*>(g.residual) + (g.residual != nullptr ? first : 0), g.residual != nullptr ? bytes : 0);
   const unsigned pitch = (unsigned)g.N * sizeof(ST);
   auto band_row = [&](int i) { return ((i >> 1) * WGM + wm) * 32 + (i & 1) * 16; };
   f32x4 sw[TNN], sw2[DUAL ? TNN : 1], bias[TNN], bias2[DUAL ? TNN : 1];
 #pragma unroll
   for (int j = 0; j < TNN; ++j) {
-    const int c = col_w + j * 16 + grp * 4;
-    sw[j] = *reinterpret_cast<const f32x4*>(bs + c);
-    bias[j] = load4<ST>(g.bias, c);
-    if constexpr (DUAL) { sw2[j] = *reinterpret_cast<const f32x4*>(bs2 + c); bias2[j] = load4<ST>(g.bias2, c); }
+    const int c = wn * C + j * 16 + grp * 4;
+    sw[j] = *reinterpret_cast<const f32x4*>(s_col + c);
+    bias[j] = load4<ST>(g.bias, n0 + c);
+    if constexpr (DUAL) { sw2[j] = *reinterpret_cast<const f32x4*>(s_col + BN + c); bias2[j] = load4<ST>(g.bias2, n0 + c); }
   }
-  float sx[TM];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int m = min(band_row(i) + (lane & 15), mvalid - 1);
-    sx[i] = g.a_scale[row_of_a(g, row0 + m)];
-  }
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    if (band_row(i) >= mvalid) continue;
-    f32x4 y[TNN];
+  auto finish = [&](int i, f32x4 (&y)[TNN]) {
+    const float sx = s_row[band_row(i) + (lane & 15)];
 #pragma unroll
     for (int j = 0; j < TNN; ++j)
-      y[j] = finish8<ST, ACT>(acc[i][j], acc2[DUAL ? i : 0][DUAL ? j : 0], sx[i], sw[j], sw2[DUAL ? j : 0], bias[j], bias2[DUAL ? j : 0]);
+      y[j] = finish8<ST, ACT>(acc[i][j], acc2[DUAL ? i : 0][DUAL ? j : 0], sx, sw[j], sw2[DUAL ? j : 0], bias[j], bias2[DUAL ? j : 0]);
+  };
+  // where the lane's piece h of row tile i lies: eight columns (16 bits) or four (fp32) of a row
+  constexpr int PIECES = __is_same(ST, float) ? TNN : TNN / 2;
+  auto at = [&](int i, int h) {
+    int m, c;
+    if constexpr (__is_same(ST, float)) { m = (h & 1) * 8 + r8; c = (h >> 1) * 32 + right * 16 + grp * 4; }
+    else if constexpr (TNN == 4) { m = h * 8 + r8; c = right * 32 + lane_col8(grp); }
+    else { m = lane & 15; c = h * 32 + lane_col8(grp); }
+    m += band_row(i);
+    return m < mvalid ? (unsigned)m * pitch + (unsigned)(wn * C + c) * (unsigned)sizeof(ST) : OUT_OF_RANGE;
+  };
+  // half lines are written through: the neighbouring wave has the other half
+  constexpr int AUX = !__is_same(ST, float) && TNN == 2 ? AUX_WT : AUX_NT;
+  if (g.residual == nullptr) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      if (band_row(i) >= mvalid) continue;
+      f32x4 y[TNN];
+      finish(i, y);
+      if constexpr (__is_same(ST, float)) {
+#pragma unroll
+        for (int j = 0; j < TNN; j += 2) {
+          swap8(y[j], y[j + 1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) buf_store16<AUX>(oy, at(i, j + h), __builtin_bit_cast(u32x4, y[j + h]));
+        }
+      } else {
+        typedef Half16<ST> H;
+        u32x4 v[TNN / 2];
+#pragma unroll
+        for (int h = 0; h < TNN / 2; ++h) {
+          u32x2 c[2];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) c[q] = u32x2{H::pack2(y[2 * h + q][0], y[2 * h + q][1]), H::pack2(y[2 * h + q][2], y[2 * h + q][3])};
+          v[h] = join_tiles(c[0], c[1]);
+        }
+        if constexpr (TNN == 4) swap8(v[0], v[1]);
+#pragma unroll
+        for (int h = 0; h < TNN / 2; ++h) buf_store16<AUX>(oy, at(i, h), v[h]);
+      }
+    }
+    return;
+  }
+  // With a residual the exchanges are made in fp32, and it is requested AHEAD row tiles ahead.
+  constexpr int AHEAD = TM < 3 ? TM : 3;
+  const __amdgpu_buffer_rsrc_t res = out_rsrc(reinterpret_cast<const ST*>(g.residual) + first, bytes);
+  u32x4 rv[AHEAD][PIECES];
+  auto load_res = [&](int i) {
+#pragma unroll
+    for (int h = 0; h < PIECES; ++h) rv[i % AHEAD][h] = buf_load16_nt(res, at(i, h));
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD - 1; ++i) load_res(i);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    if (i + AHEAD - 1 < TM) load_res(i + AHEAD - 1);
+    if (band_row(i) >= mvalid) continue;
+    f32x4 y[TNN];
+    finish(i, y);
     if constexpr (__is_same(ST, float)) {
 #pragma unroll
       for (int j = 0; j < TNN; j += 2) {
         swap8(y[j], y[j + 1]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int m = band_row(i) + h * 8 + r8;
-          const unsigned off = m < mvalid ? (unsigned)m * pitch + (unsigned)(wn * C + j * 16 + right * 16 + grp * 4) * 4u : OUT_OF_RANGE;
-          const f32x4 r = __builtin_bit_cast(f32x4, buf_load16_nt(res, off));
-          buf_store16<AUX_NT>(oy, off, __builtin_bit_cast(u32x4, y[j + h] + r));
-        }
+        for (int h = 0; h < 2; ++h) buf_store16<AUX>(oy, at(i, j + h), __builtin_bit_cast(u32x4, y[j + h] + __builtin_bit_cast(f32x4, rv[i % AHEAD][j + h])));
       }
     } else {
       typedef Half16<ST> H;
@@ -267,24 +355,23 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
       for (int j = 0; j < TNN; j += 2) join_tiles(y[j], y[j + 1]);   // a lane: eight adjacent columns of 32
       if constexpr (TNN == 4) { swap8(y[0], y[2]); swap8(y[1], y[3]); }
 #pragma unroll
-      for (int h = 0; h < TNN / 2; ++h) {
-        const int m = band_row(i) + (TNN == 4 ? h * 8 + r8 : (lane & 15));
-        const unsigned off = m < mvalid ? (unsigned)m * pitch + (unsigned)(wn * C + (TNN == 4 ? right * 32 : h * 32) + lane_col8(grp)) * 2u : OUT_OF_RANGE;
-        const u32x4 r = buf_load16_nt(res, off);
+      for (int h = 0; h < PIECES; ++h) {
+        const u32x4 r = rv[i % AHEAD][h];
         u32x4 o;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           o[q] = H::pack2(y[2 * h + q / 2][q % 2 * 2] + H::lo(r[q]), y[2 * h + q / 2][q % 2 * 2 + 1] + H::hi(r[q]));
-        buf_store16<AUX_NT>(oy, off, o);
+        buf_store16<AUX>(oy, at(i, h), o);
       }
     }
   }
 }
 
 // ---- few rows ----
-// A block takes a strip of 16 columns and a group of 16 MT rows; its waves share out the K range, 64 values at a time in turn, and add their
-// sums in LDS, in any order the same: they are integers.  An operand of B is one contiguous 1 KB load of a wave, of A 16 rows x 64
-// bytes that all strips read from the caches.  Bound by the read of the weights.
+// A block of eight waves takes strips of 16 columns and a group of 16 MT rows: 8 / nk strips, the K range of each shared out among nk
+// waves, 64 values at a time in turn, whose sums are added in LDS, in any order the same: they are integers.  An operand of B is one
+// contiguous 1 KB load of a wave, of A 16 rows x 64 bytes that all strips read from the caches; the next U of either are requested before the
+// last are used.  Bound by the read of the weights.
 // Experts: blockIdx.y is the n-th group of 16 MT rows of some expert, which every block finds for itself from the experts' row counts.
 constexpr int FEW_WAVES = 8;
 
@@ -298,8 +385,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   int e = 0, row0 = blockIdx.y * ROWS, rows = min(ROWS, g.M - row0);
   if constexpr (GROUPED) {
     static_assert(MOE_MAX_E <= FEW_WAVES * 64, "a thread per expert");
-    int l = 0, h = 0;
-    if (tid < g.E) share_of(g.lo, g.hi, g.kept[tid], tid, l, h);
+    int l = 0, h = 0, at = 0;
+    if (tid < g.E) {
+      at = g.offsets[tid];
+      share_of(g.lo, g.hi, g.kept[tid], tid, l, h);
+    }
     const int mine = (h - l + ROWS - 1) / ROWS;
     if (tid == 0) s_tile[0] = -1;
     const int scan = wave_scan_i(mine);
@@ -310,7 +400,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     const int q = (int)blockIdx.y - before;
     if (q >= 0 && q < mine) {
       s_tile[0] = tid;
-      s_tile[1] = g.offsets[tid] + l + q * ROWS;
+      s_tile[1] = at + l + q * ROWS;
       s_tile[2] = min(ROWS, h - l - q * ROWS);
     }
     __syncthreads();
@@ -319,82 +409,98 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     row0 = __builtin_amdgcn_readfirstlane(s_tile[1]);
     rows = __builtin_amdgcn_readfirstlane(s_tile[2]);
   }
-  const int K = g.K, KT = K / TILE8_K, n0 = blockIdx.x * TILE8_N;
-  const int k0 = GROUPED ? 0 : (int)((long long)blockIdx.z * KT / g.n_parts), k1 = GROUPED ? KT : (int)((long long)(blockIdx.z + 1) * KT / g.n_parts);
-  const size_t strip = (size_t)e * g.N * K + (size_t)n0 * K + lane * 16;
+  const int nk = g.few_nk, strips = FEW_WAVES / nk, kw = wave % nk;   // this wave's part of K
+  const int K = g.K, KT = K / TILE8_K, n0 = (blockIdx.x * strips + wave / nk) * TILE8_N;
+  const bool has = n0 < g.N;   // (the last block may have fewer strips)
+  const int k1 = has ? KT : 0;
+  const size_t strip = ((size_t)e * g.N + n0) * K + lane * 16;
   const int8_t *pb = g.B + strip, *pb2 = DUAL ? g.B2 + strip : pb;
   const int8_t* pa[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
     pa[i] = g.A + (size_t)row_of_a(g, row0 + min(i * 16 + (lane & 15), rows - 1)) * K + (lane >> 4) * 16;   // (rows past the group repeat its last)
   i32x4 acc[MATS][MT] = {};
-  auto run = [&](int k, auto n_) {
-    constexpr int N_ = decltype(n_)::value;
-    i32x4 b[N_][MATS], a[N_][MT];
+  struct Operands { i32x4 b[U][MATS], a[U][MT]; };
+  // tiles k, k + nk, ... of this wave, U of them; past the end the last one again, which is then not used
+  auto fetch = [&](int k, Operands& o) {
 #pragma unroll
-    for (int u = 0; u < N_; ++u) {
-      const size_t at = (size_t)(k + u * FEW_WAVES);
-      b[u][0] = *reinterpret_cast<const i32x4*>(pb + at * TILE8_BYTES);
-      if constexpr (DUAL) b[u][1] = *reinterpret_cast<const i32x4*>(pb2 + at * TILE8_BYTES);
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (size_t)min(k + u * nk, k1 - 1);
+      o.b[u][0] = *reinterpret_cast<const i32x4*>(pb + at * TILE8_BYTES);
+      if constexpr (DUAL) o.b[u][1] = *reinterpret_cast<const i32x4*>(pb2 + at * TILE8_BYTES);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
+      for (int i = 0; i < MT; ++i) o.a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
     }
+  };
+  auto use = [&](int k, const Operands& o) {
 #pragma unroll
-    for (int u = 0; u < N_; ++u)
+    for (int u = 0; u < U; ++u) {
+      if (k + u * nk >= k1) break;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int q = 0; q < MATS; ++q) acc[q][i] = mfma8(b[u][q], a[u][i], acc[q][i]);
+        for (int q = 0; q < MATS; ++q) acc[q][i] = mfma8(o.b[u][q], o.a[u][i], acc[q][i]);
+    }
   };
-  int k = k0 + wave;
-  for (; k + (U - 1) * FEW_WAVES < k1; k += U * FEW_WAVES) run(k, Const<U>{});
-  for (; k < k1; k += FEW_WAVES) run(k, Const<1>{});
+  int k = kw;
+  if (k < k1) {
+    Operands x, y;
+    fetch(k, x);
+    for (;;) {
+      const int k2 = k + U * nk;
+      if (k2 < k1) fetch(k2, y);
+      use(k, x);
+      if (k2 >= k1) break;
+      k = k2 + U * nk;
+      if (k < k1) fetch(k, x);
+      use(k2, y);
+      if (k >= k1) break;
+    }
+  }
 #pragma unroll
   for (int q = 0; q < MATS; ++q)
 #pragma unroll
     for (int i = 0; i < MT; ++i) s_sum[wave][q * MT + i][lane] = acc[q][i];
   __syncthreads();
-  if (wave >= MT) return;
-  const int m = wave * 16 + (lane & 15), c = n0 + (lane >> 4) * 4;
-  if (m >= rows) return;
-  i32x4 sum[MATS];
+  // the strips' MT row tiles of 16 go round the waves
+  for (int j = wave; j < strips * MT; j += FEW_WAVES) {
+    const int st = j / MT, i = j % MT, m = i * 16 + (lane & 15), c = (blockIdx.x * strips + st) * TILE8_N + (lane >> 4) * 4;
+    if (m >= rows || c >= g.N) continue;
+    i32x4 sum[MATS];
 #pragma unroll
-  for (int q = 0; q < MATS; ++q) {
-    sum[q] = s_sum[0][q * MT + wave][lane];
-#pragma unroll
-    for (int w = 1; w < FEW_WAVES; ++w) sum[q] += s_sum[w][q * MT + wave][lane];
+    for (int q = 0; q < MATS; ++q) {
+      sum[q] = s_sum[st * nk][q * MT + i][lane];
+      for (int w = 1; w < nk; ++w) sum[q] += s_sum[st * nk + w][q * MT + i][lane];
+    }
+    const size_t row = row0 + m;
+    const size_t cs = (size_t)e * g.N + c;
+    const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
+    f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
+    y += load4<ST>(g.residual, row * g.N + c);
+    ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
+    if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
+    else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
   }
-  const size_t row = row0 + m;
-  if (!GROUPED && g.n_parts > 1) {
-#pragma unroll
-    for (int q = 0; q < MATS; ++q)
-      *reinterpret_cast<i32x4*>(g.parts + ((size_t)(blockIdx.z * MATS + q) * g.M + row) * g.N + c) = sum[q];
-    return;
-  }
-  const size_t cs = (size_t)e * g.N + c;
-  const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
-  f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
-  y += load4<ST>(g.residual, row * g.N + c);
-  ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
-  if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
-  else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
 }
 
-// Adds the K parts; a thread has four adjacent columns of a row.
+// Adds the K parts of a product cut so; a thread has four adjacent columns of a row.
 template <typename ST, int ACT>
-__global__ __launch_bounds__(256) void few8_join_kernel(Gemm8Args g) {
+__global__ __launch_bounds__(256) void join8_kernel(Gemm8Args g) {
   constexpr int MATS = ACT == MOE_ACT_SWIGLU ? 2 : 1;
-  const size_t per_row = g.N / 4, i = (size_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+  const unsigned per_row = g.N / 4, i = blockIdx.x * 256 + threadIdx.x, row = i / per_row;
   const int c = (int)(i - row * per_row) * 4;
-  if (row >= (size_t)g.M) return;
+  if (row >= (unsigned)g.M) return;
   i32x4 sum[MATS] = {};
-  for (int p = 0; p < g.n_parts; ++p)
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) sum[q] += *reinterpret_cast<const i32x4*>(g.parts + ((size_t)(p * MATS + q) * g.M + row) * g.N + c);
+  for (int p = 0; p < MAX_PARTS8; ++p)
+    if (p < g.n_parts)
+#pragma unroll
+      for (int q = 0; q < MATS; ++q) sum[q] += *reinterpret_cast<const i32x4*>(g.parts + ((size_t)(p * MATS + q) * g.M + row) * g.N + c);
   const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + c), sw2 = MATS > 1 ? *reinterpret_cast<const f32x4*>(g.b2_scale + c) : sw;
   f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], g.a_scale[row], sw, sw2, load4<ST>(g.bias, c), load4<ST>(MATS > 1 ? g.bias2 : nullptr, c));
-  y += load4<ST>(g.residual, row * g.N + c);
-  ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
+  const size_t at = (size_t)row * g.N + c;
+  y += load4<ST>(g.residual, at);
+  ST* out = reinterpret_cast<ST*>(g.C) + at;
   if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
   else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
 }
@@ -409,25 +515,29 @@ static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) 
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return set_hip_error(e);
   }
-  const long long grid = row_tiles * ((g.N + BN - 1) / BN);
+  const long long grid = row_tiles * ((g.N + BN - 1) / BN) * (GROUPED ? 1 : g.n_parts);
   gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, GROUPED><<<(unsigned)grid, WGM * WGN * 64, LDS, s>>>(g);
+  if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
 }
-template <typename ST, int ACT, bool GROUPED>
-static int few8_launch(const Gemm8Args& g, int rows, int groups, hipStream_t s) {
-  const dim3 grid(g.N / TILE8_N, groups, GROUPED ? 1 : g.n_parts);
-  if (rows == 16) few8_kernel<ST, ACT, 1, GROUPED><<<grid, FEW_WAVES * 64, 0, s>>>(g);
-  else if (rows == 32) few8_kernel<ST, ACT, 2, GROUPED><<<grid, FEW_WAVES * 64, 0, s>>>(g);
-  else few8_kernel<ST, ACT, 4, GROUPED><<<grid, FEW_WAVES * 64, 0, s>>>(g);
-  if (!GROUPED && g.n_parts > 1) few8_join_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
+template <typename ST, int ACT, int MT, bool GROUPED>
+static int few8_launch(const Gemm8Args& g, int groups, hipStream_t s) {
+  const int strips = FEW_WAVES / g.few_nk;
+  few8_kernel<ST, ACT, MT, GROUPED><<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, 0, s>>>(g);
   return launch_status();
 }
 template <typename ST, int ACT, bool GROUPED>
 static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
   constexpr int D = ACT == MOE_ACT_SWIGLU ? 2 : 1;   // columns are of both matrices together
-  if (c.few) return few8_launch<ST, ACT, GROUPED>(g, c.rows, GROUPED ? max_tiles : (g.M + c.rows - 1) / c.rows, s);
+  if (c.few) {
+    if constexpr (GROUPED) return few8_launch<ST, ACT, 1, true>(g, max_tiles, s);
+    else return c.rows == 16 ? few8_launch<ST, ACT, 1, false>(g, 1, s) : few8_launch<ST, ACT, 2, false>(g, 1, s);
+  }
   const long long rt = GROUPED ? max_tiles : (g.M + c.rows - 1) / c.rows;
-  if (c.rows == 256) return gemm8_launch<ST, ACT, 256, 256 / D, 2, 4, 1, GROUPED>(g, rt, s);
+  if (c.rows == 256) {   // two matrices: four waves down, so that a wave has 64 columns of either and writes whole lines (fp32 has them with 32)
+    constexpr int DOWN = __is_same(ST, float) ? 2 : 2 * D;
+    return gemm8_launch<ST, ACT, 256, 256 / D, DOWN, 8 / DOWN, 1, GROUPED>(g, rt, s);
+  }
   if (c.rows == 128) return gemm8_launch<ST, ACT, 128, 128 / D, 2, 2, 2, GROUPED>(g, rt, s);
   return gemm8_launch<ST, ACT, 64, 128 / D, 2, 2, 2, GROUPED>(g, rt, s);
 }

@@ -5,7 +5,12 @@
 namespace moe {
 
 // A tile shape, rows and columns (two matrices: of both together), how many run at a time, and what a round of them takes, us: `fixed` in
-// front of and behind the K loop, and per 128 K values `alone` where few tiles run and `full` where all do.
+// front of and behind the K loop, and per 128 K values `alone` where few tiles run and `full` where all do.  Fitted to T x d x n, us in the
+// order below: 1024 x 1024 x 1024 15.2 | 7.2 | 6.0; 128 x 4096 x 4096 27.2 | 16.0 | 12.1; 8192 x 4096 x 1024 43.3 | 34.5 | 43.5; 8192 x 1024 x
+// 4096 41.8 | 43.9 | 57.0; 8192 x 2048 x 8192 122 | 137 | 186; 8192 x 8192 x 8192 432 | 492; two matrices 512 x 2048 x 2048 24 | 10.3 | 8.2,
+// 4096 x 2048 x 4096 63 | 77 | 101.  Parts, 64 rows x 14336 x 4096, one | four | eight of tiles of 64: 52 | 21 | 17.5 (strips: 29); 100 x 8192
+// x 1024 19.7 | 11.1 | 10.7; 128 x 4096 x 4096 11.6 | 13.3 | 18.4.  Strips against tiles: 32 x 4096 x 4096 6.8 | 9.0 (two parts), 32 x 14336 x
+// 4096 17.0 | 16.1 (eight), 64 x 4096 x 4096 10.7 | 10.6 (four), 64 x 4096 x 14336 of two matrices 21.4 in tiles.
 struct Shape8 {
   int rows, cols, slots;
   double fixed, alone, full;
@@ -16,28 +21,44 @@ struct Shape8 {
     return t;
   }
 };
-constexpr Shape8 SHAPES8[] = {{256, 256, 256, 6.5, 1.05, 1.37}, {128, 128, 512, 4.0, 0.5, 0.8}, {64, 128, 512, 3.0, 0.35, 0.54}};
-constexpr int FEW_ROWS = 64;       // up to here the weights are streamed
-constexpr int FEW_STRIPS = 256;    // strips of 16 columns that fill the chip; fewer are cut along K
-constexpr int FEW_PART = 16;       // tiles of 64 K values that a part has at least
-static int few_rows(long long rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+constexpr Shape8 SHAPES8[] = {{256, 256, 256, 7.0, 1.0, 1.55}, {128, 128, 512, 3.8, 0.37, 0.9}, {64, 128, 512, 2.5, 0.28, 0.57}};
+constexpr double JOIN8_US = 2.5, JOIN8_US_PER_MB = 0.6;   // the adding launch; sums written and read again
+constexpr int PART8_STAGES = 4;    // stages that a part has at least
+
+// Waves that share a strip's K range of `tiles` tiles of 64 values: all eight where the strips are few, else as many as leave each
+// sixteen tiles, so that a wave has requests enough in flight and a block enough to do.  (us, eight | four | two waves: 4 x 2048 x 2048, two
+// matrices, 3.7 | 4.6 | 6.1; 16 x 4096 x 14336, two, 20.3 | 19.4 | 19.8; 4 tokens x 8 of 256 experts, d 2048, f 1024, both products
+// 46.7 | 38.7 | 36.5.  Sixteen waves: 16 x 14336 x 4096 12.9 instead of 12.1.)
+static int few_nk(long long strips, int tiles) {
+  if (strips <= 512) return 8;
+  return tiles >= 128 ? 8 : tiles >= 64 ? 4 : tiles >= 32 ? 2 : 1;
+}
 
 Cut8 cut_linear8(long long T, int N, int K, int mats) {
-  if (T <= FEW_ROWS) {
-    const int strips = N / TILE8_N, parts = std::min({(FEW_STRIPS + strips - 1) / strips, K / TILE8_K / FEW_PART, 16});
-    return Cut8{true, few_rows(T), TILE8_N, std::max(parts, 1)};
-  }
+  if (T <= FEW_ROWS8) return Cut8{true, T <= 16 ? 16 : 32, TILE8_N, 1};
   Cut8 best = {};
   double least = 1e30;
+  const int stages = (K + 127) / 128;
   for (const Shape8& s : SHAPES8) {
     const int cols = s.cols / mats;
-    const double us = s.us((T + s.rows - 1) / s.rows * ((N + cols - 1) / cols), (K + 127) / 128);
-    if (us < least) { least = us; best = Cut8{false, s.rows, cols, 1}; }
+    const long long tiles = (T + s.rows - 1) / s.rows * ((N + cols - 1) / cols);
+    for (int p = 1; p <= MAX_PARTS8; ++p) {
+      if (p > 1 && (s.rows == 256 || p * tiles > s.slots || stages < p * PART8_STAGES)) break;
+      double us = s.us(tiles * p, (stages + p - 1) / p);
+      if (p > 1) us += JOIN8_US + JOIN8_US_PER_MB * (double)p * T * N * mats * 4 / 1e6;
+      if (us < least) { least = us; best = Cut8{false, s.rows, cols, p}; }
+    }
   }
   return best;
 }
 
-int expert8_tile_rows(long long rows, int E) { return rows <= (long long)FEW_ROWS * E ? 0 : rows <= 256ll * E ? 128 : 256; }
+// Few rows per expert: strips of 16 columns and groups of 16 rows, for each of which the expert's weights are read again.  (Both products
+// with their map, us, strips | tiles of 64 | 128 | 256 rows: d 2048, f 1024, 64 experts, 4 rows per expert 68 | 72 | 75; 8 79 | 81 | 83; 16
+// 98 | 90 | 91; 32 135 | 101 | 98; 128 398 | 157 | 136 | 159; 1024 - | 744 | 575 | 525; 128 experts, 512 rows - | 828 | 653 | 565; d 4096, f
+// 14336, 8 experts, 4 rows 240 | 265 | 269; 16 333 | 271 | 275.)
+int expert8_tile_rows(long long rows, int E) {
+  return rows <= 8ll * E ? 0 : rows <= 24ll * E ? 64 : rows <= 256ll * E ? 128 : 256;
+}
 
 static int gemm8(int dtype, int act, const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
   if (dtype == MOE_DTYPE_F32) return gemm8_f32(act, g, c, max_tiles, s);
@@ -54,6 +75,7 @@ int launch_linear8(const moe_linear8* c, const void* x, const float* xs, const v
   g.bias = bias; g.bias2 = bias_b; g.residual = residual; g.C = y;
   g.M = c->T; g.N = c->d_out; g.K = c->d_in;
   g.chunked = row_tiles_chunked(c->T, c->d_in, c->d_out, 1, mats, 1);
+  g.few_nk = few_nk(c->d_out / TILE8_N, c->d_in / TILE8_K);
   g.parts = (int32_t*)ws;
   g.n_parts = cut.parts;
   return gemm8(c->dtype, c->act, g, cut, 0, s);
@@ -62,12 +84,12 @@ int launch_linear8(const moe_linear8* c, const void* x, const float* xs, const v
 int launch_expert8(int dtype, int act, const Gemm8Args& args, int tile_rows, int max_tiles, int rows, hipStream_t s) {
   Gemm8Args g = args;
   const int mats = act == MOE_ACT_SWIGLU ? 2 : 1;
-  g.n_parts = 1;
   g.chunked = row_tiles_chunked(rows, g.K, g.N, g.E, mats, 1);
-  Cut8 cut = {tile_rows == 0, tile_rows, 0, 1};
+  g.n_parts = 1;
+  const Cut8 cut = {tile_rows == 0, tile_rows, 0, 1};
   if (cut.few) {
-    cut.rows = few_rows((rows + g.E - 1) / g.E);
-    max_tiles = std::min(g.E, rows) + rows / cut.rows;   // every expert's last group may be a part of one
+    max_tiles = std::min(g.E, rows) + rows / 16;   // every expert's last group may be a part of one
+    g.few_nk = few_nk((long long)(g.N / TILE8_N) * std::min(g.E, rows), g.K / TILE8_K);
   }
   return gemm8(dtype, act, g, cut, max_tiles, s);
 }
