@@ -3,7 +3,7 @@
 //
 // Tiles.  v_mfma_i32_16x16x64_i8 has the operand registers of the 16-bit 16 x 16 x 32 instruction and twice its products, so a stage of
 // 128 K values is as many bytes as one of 64 there, and the pipeline is the one of gemm_bf16_kernel.h: LDS stages filled by loads that
-// write LDS directly, three of A and two of B, two K steps to an iteration with one block barrier, in regions of one row tile's
+// write LDS directly, three of A and two of B (the smallest tiles: three of both), two K steps to an iteration with one block barrier, in regions of one row tile's
 // instructions each, behind which the reads of the next step's fragments and this step's share of the loads are issued.  A comes in rows and
 // is swizzled in LDS (kc_off); B comes in the order of the instruction (quant8.h) and is read lane by lane.  Sums of 64 K values past
 // the end (an odd number of them) are those of a B of zeros, which the descriptor's byte count gives.
@@ -57,16 +57,17 @@ __device__ __forceinline__ int row_of_a(const Gemm8Args& g, int r) {
   return min((int)((uint64_t)(unsigned)a * g.per_row >> 33), g.src_rows - 1);
 }
 
-template <int BM, int BN, bool DUAL>
-constexpr int gemm8_lds_bytes() { return 3 * BM * BK8 + 2 * BN * BK8 * (DUAL ? 2 : 1); }
+// DEPTH 2: two stages of B and three of A; 3: three of both.
+template <int BM, int BN, bool DUAL, int DEPTH>
+constexpr int gemm8_lds_bytes() { return DEPTH == 2 ? 3 * BM * BK8 + 2 * BN * BK8 * (DUAL ? 2 : 1) : DEPTH * BK8 * (BM + BN * (DUAL ? 2 : 1)); }
 
-template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, bool GROUPED>
+template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool GROUPED>
 __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_kernel(Gemm8Args g) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
   constexpr int NT = WGM * WGN * 64;
   constexpr int WTM = BM / 32 / WGM, TM = 2 * WTM, TNN = BN / WGN / 16;   // row tiles, column tiles (of either matrix) of a wave
-  constexpr int A_BYTES = BM * BK8, B_BYTES = BN * BK8, B_STAGE = B_BYTES * (DUAL ? 2 : 1), B_AT = 3 * A_BYTES;
+  constexpr int A_BYTES = BM * BK8, B_BYTES = BN * BK8, B_STAGE = B_BYTES * (DUAL ? 2 : 1), B_AT = (DEPTH == 2 ? 3 : DEPTH) * A_BYTES;
   constexpr int LA = BM * 8 / NT, LB1 = BN * 8 / NT, LB = LB1 * (DUAL ? 2 : 1);   // 16-byte loads per thread and stage
   static_assert(BM * 8 % NT == 0 && BN * 8 % NT == 0 && WTM * 32 * WGM == BM && TNN % 2 == 0, "whole loads, whole waves");
   static_assert((WGM * WGN) % 2 == 0, "a wave's loads of B are all of the same half of a stage");
@@ -140,9 +141,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     bf[set][j] = *reinterpret_cast<const i32x4*>(p);
     if constexpr (DUAL) bf2[set][j] = *reinterpret_cast<const i32x4*>(p + B_BYTES);
   };
-  constexpr int WAIT_P = ((LA + LB) & 15) | (((LA + LB) >> 4) << 14) | 0x70 | (15 << 8);   // s_waitcnt vmcnt(LA + LB) only
-  constexpr int WAIT_A = LA | 0x70;                                                        // s_waitcnt vmcnt(LA) lgkmcnt(0)
-  static_assert(LA + LB < 64 && LA < 16, "the wait counter");
+  static_assert(LA + LB < 64, "the wait counter");
   auto barrier = [&]() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -172,22 +171,26 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     }
   };
 
-  int a0 = 0, a1 = A_BYTES, a2 = 2 * A_BYTES, b0 = 0, b1 = B_STAGE;
-  auto prologue = [&](int stage, int abuf, int bbuf) {
+  auto request = [&](int stage, int abuf, int bbuf) {
 #pragma unroll
     for (int q = 0; q < LB; ++q) load_b(q, stage, bbuf);
 #pragma unroll
     for (int q = 0; q < LA; ++q) load_a(q, stage, abuf);
   };
-  prologue(S0, a0, b0);
-  if (KS - S0 > 1) {
-    prologue(S0 + 1, a1, b1);
-    __builtin_amdgcn_s_waitcnt(WAIT_P);
-  } else {
-    __builtin_amdgcn_s_waitcnt(0x70 | (15 << 8));
-  }
-  barrier();
+  constexpr int L = LA + LB;
+  // s_waitcnt vmcnt(n) lgkmcnt(0): the n newest loads may be in flight, every read of LDS is done
+#define MOE_WAIT8(n_) __builtin_amdgcn_s_waitcnt(((n_) & 15) | (((n_) >> 4) << 14) | 0x70)
   auto mainloop = [&](int bands) {
+    if constexpr (DEPTH == 2) {
+    int a0 = 0, a1 = A_BYTES, a2 = 2 * A_BYTES, b0 = 0, b1 = B_STAGE;
+    request(S0, a0, b0);
+    if (KS - S0 > 1) {
+      request(S0 + 1, a1, b1);
+      MOE_WAIT8(L);
+    } else {
+      MOE_WAIT8(0);
+    }
+    barrier();
 #pragma unroll
     for (int i = 0; i < TM; ++i) frag_a(i, a0, 0);
 #pragma unroll
@@ -206,8 +209,8 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
         }
       }, bands);
       if (more) {
-        if constexpr (LOAD) __builtin_amdgcn_s_waitcnt(WAIT_A);
-        else __builtin_amdgcn_s_waitcnt(0);
+        if constexpr (LOAD) MOE_WAIT8(LA);
+        else MOE_WAIT8(0);
         barrier();
       }
       step(Const<1>{}, more, a1, b1, 0, [&](int r) {
@@ -225,7 +228,58 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     for (; S + 2 < KS; ++S) iteration(S, true, Const<1>{});
 #pragma unroll 1
     for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
+    } else {
+    // Three stages of both, all requested ahead: where a compute unit has one or two small blocks, a stage's products are over long before
+    // a load requested an iteration ago has landed.  Stage S + 3 goes where stage S was, in K step 1 of iteration S.  (Tiles of 64 x 128,
+    // us, the pipeline above -> this one: 300 x 4096 x 4096 17.8 -> 13.1, 64 x 14336 x 4096 52 -> 33, 8192 x 2048 x 8192 188 -> 179.  Four and six
+    // stages leave room for one block: 300 x 4096 x 4096 15.1 and 15.7, 8192 x 2048 x 8192 266 and 293.  128 x 128, three stages and
+    // one block per compute unit: 300 x 4096 x 4096 19.1 -> 17.2, but 8192 x 2048 x 8192 146 -> 177.)
+    static_assert(DEPTH == 3 && 2 * L < 64, "the wait counter");
+#pragma unroll
+    for (int q = 0; q < DEPTH; ++q)
+      if (S0 + q < KS) request(S0 + q, q * A_BYTES, q * B_STAGE);
+    auto wait_for = [&](int left) {   // all but `left` stages
+      if (left >= 2) MOE_WAIT8(2 * L);
+      else if (left == 1) MOE_WAIT8(L);
+      else MOE_WAIT8(0);
+    };
+    wait_for(min(KS - S0, DEPTH) - 1);
+    barrier();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) frag_a(i, 0, 0);
+#pragma unroll
+    for (int j = 0; j < TNN; ++j) frag_b(0, j, 0, 0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    int at = 0;   // which stage of LDS is multiplied
+    auto iteration = [&](int S, bool more, auto load) {
+      constexpr bool LOAD = decltype(load)::value != 0;
+      const int next = at + 1 == DEPTH ? 0 : at + 1;
+      step(Const<0>{}, true, at * A_BYTES, at * B_STAGE, 1, [&](int) {}, bands);
+      if (more) {
+        if constexpr (LOAD) MOE_WAIT8((DEPTH - 2) * L);
+        else wait_for(KS - 2 - S);
+        barrier();
+      }
+      step(Const<1>{}, more, next * A_BYTES, next * B_STAGE, 0, [&](int r) {
+        if constexpr (LOAD) {
+#pragma unroll
+          for (int q = 0; q < L; ++q)
+            if (q * TM / L == r) {
+              if (q < LB) load_b(q, S + DEPTH, at * B_STAGE);
+              else load_a(q - LB, S + DEPTH, at * A_BYTES);
+            }
+        }
+      }, bands);
+      at = next;
+    };
+    int S = S0;
+#pragma unroll 1
+    for (; S + DEPTH < KS; ++S) iteration(S, true, Const<1>{});
+#pragma unroll 1
+    for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
+   }
   };
+#undef MOE_WAIT8
   if (ni == WTM) mainloop(WTM);
   else mainloop(ni);
 
@@ -506,17 +560,17 @@ __global__ __launch_bounds__(256) void join8_kernel(Gemm8Args g) {
 }
 
 // ---- launches ----
-template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, bool GROUPED>
+template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool GROUPED>
 static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) {
-  constexpr int LDS = gemm8_lds_bytes<BM, BN, ACT == MOE_ACT_SWIGLU>();
+  constexpr int LDS = gemm8_lds_bytes<BM, BN, ACT == MOE_ACT_SWIGLU, DEPTH>();
   static_assert(LDS * PER_CU <= LDS_BYTES, "blocks that a compute unit holds");
-  const void* fn = reinterpret_cast<const void*>(gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, GROUPED>);
+  const void* fn = reinterpret_cast<const void*>(gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, GROUPED>);
   if (LDS > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return set_hip_error(e);
   }
   const long long grid = row_tiles * ((g.N + BN - 1) / BN) * (GROUPED ? 1 : g.n_parts);
-  gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, GROUPED><<<(unsigned)grid, WGM * WGN * 64, LDS, s>>>(g);
+  gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, GROUPED><<<(unsigned)grid, WGM * WGN * 64, LDS, s>>>(g);
   if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
 }
@@ -536,10 +590,10 @@ static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream
   const long long rt = GROUPED ? max_tiles : (g.M + c.rows - 1) / c.rows;
   if (c.rows == 256) {   // two matrices: four waves down, so that a wave has 64 columns of either and writes whole lines (fp32 has them with 32)
     constexpr int DOWN = __is_same(ST, float) ? 2 : 2 * D;
-    return gemm8_launch<ST, ACT, 256, 256 / D, DOWN, 8 / DOWN, 1, GROUPED>(g, rt, s);
+    return gemm8_launch<ST, ACT, 256, 256 / D, DOWN, 8 / DOWN, 1, 2, GROUPED>(g, rt, s);
   }
-  if (c.rows == 128) return gemm8_launch<ST, ACT, 128, 128 / D, 2, 2, 2, GROUPED>(g, rt, s);
-  return gemm8_launch<ST, ACT, 64, 128 / D, 2, 2, 2, GROUPED>(g, rt, s);
+  if (c.rows == 128) return gemm8_launch<ST, ACT, 128, 128 / D, 2, 2, 2, 2, GROUPED>(g, rt, s);
+  return gemm8_launch<ST, ACT, 64, 128 / D, 2, 2, 2, 3, GROUPED>(g, rt, s);
 }
 template <typename ST>
 static int gemm8_for(int act, const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {

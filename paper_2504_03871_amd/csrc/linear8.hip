@@ -6,11 +6,12 @@ namespace moe {
 
 // A tile shape, rows and columns (two matrices: of both together), how many run at a time, and what a round of them takes, us: `fixed` in
 // front of and behind the K loop, and per 128 K values `alone` where few tiles run and `full` where all do.  Fitted to T x d x n, us in the
-// order below: 1024 x 1024 x 1024 15.2 | 7.2 | 6.0; 128 x 4096 x 4096 27.2 | 16.0 | 12.1; 8192 x 4096 x 1024 43.3 | 34.5 | 43.5; 8192 x 1024 x
-// 4096 41.8 | 43.9 | 57.0; 8192 x 2048 x 8192 122 | 137 | 186; 8192 x 8192 x 8192 432 | 492; two matrices 512 x 2048 x 2048 24 | 10.3 | 8.2,
-// 4096 x 2048 x 4096 63 | 77 | 101.  Parts, 64 rows x 14336 x 4096, one | four | eight of tiles of 64: 52 | 21 | 17.5 (strips: 29); 100 x 8192
-// x 1024 19.7 | 11.1 | 10.7; 128 x 4096 x 4096 11.6 | 13.3 | 18.4.  Strips against tiles: 32 x 4096 x 4096 6.8 | 9.0 (two parts), 32 x 14336 x
-// 4096 17.0 | 16.1 (eight), 64 x 4096 x 4096 10.7 | 10.6 (four), 64 x 4096 x 14336 of two matrices 21.4 in tiles.
+// order below: 1024 x 1024 x 1024 15.2 | 7.4 | 6.1; 128 x 4096 x 4096 27.2 | 15.9 | 11.8; 300 x 4096 x 4096 39 | 19 | 13.1; 8192 x 4096 x 1024
+// 43 | 34 | 43; 8192 x 1024 x 4096 42 | 46 | 58; 8192 x 2048 x 8192 122 | 138 | 179; 8192 x 8192 x 8192 432 | 492 | -; two matrices 512 x 2048
+// x 2048 24 | 10.5 | 8.1, 4096 x 2048 x 4096 63 | 72 | 87.  Tiles of 64 in one | two | four | eight parts: 64 x 14336 x 4096 32.5 | 22.4 | 16.7 |
+// 17.2 (strips: 29), 100 x 8192 x 1024 19.1 | 14.0 | 11.2 | 10.9, 128 x 4096 x 4096 11.8 | 12.5 | 13.4 | 19.0.  Strips against the best tiles: 16 x
+// 14336 x 4096 12.1 | 14.9, 32 x 4096 x 4096 7.0 | 9.2, 32 x 14336 x 4096 17.2 | 15.3, 64 x 4096 x 4096 10.7 | 10.8, 24 x 4096 x 14336 of two
+// matrices 20.7 | 22.2, 64 of them - | 20.7 (5.8 TB/s).
 struct Shape8 {
   int rows, cols, slots;
   double fixed, alone, full;
@@ -21,7 +22,7 @@ struct Shape8 {
     return t;
   }
 };
-constexpr Shape8 SHAPES8[] = {{256, 256, 256, 7.0, 1.0, 1.55}, {128, 128, 512, 3.8, 0.37, 0.9}, {64, 128, 512, 2.5, 0.28, 0.57}};
+constexpr Shape8 SHAPES8[] = {{256, 256, 256, 7.0, 1.0, 1.55}, {128, 128, 512, 3.8, 0.37, 0.9}, {64, 128, 512, 2.5, 0.26, 0.55}};
 constexpr double JOIN8_US = 2.5, JOIN8_US_PER_MB = 0.6;   // the adding launch; sums written and read again
 constexpr int PART8_STAGES = 4;    // stages that a part has at least
 
@@ -35,6 +36,7 @@ static int few_nk(long long strips, int tiles) {
 }
 
 Cut8 cut_linear8(long long T, int N, int K, int mats) {
+
   if (T <= FEW_ROWS8) return Cut8{true, T <= 16 ? 16 : 32, TILE8_N, 1};
   Cut8 best = {};
   double least = 1e30;
@@ -52,13 +54,13 @@ Cut8 cut_linear8(long long T, int N, int K, int mats) {
   return best;
 }
 
-// Few rows per expert: strips of 16 columns and groups of 16 rows, for each of which the expert's weights are read again.  (Both products
-// with their map, us, strips | tiles of 64 | 128 | 256 rows: d 2048, f 1024, 64 experts, 4 rows per expert 68 | 72 | 75; 8 79 | 81 | 83; 16
-// 98 | 90 | 91; 32 135 | 101 | 98; 128 398 | 157 | 136 | 159; 1024 - | 744 | 575 | 525; 128 experts, 512 rows - | 828 | 653 | 565; d 4096, f
-// 14336, 8 experts, 4 rows 240 | 265 | 269; 16 333 | 271 | 275.)
-int expert8_tile_rows(long long rows, int E) {
-  return rows <= 8ll * E ? 0 : rows <= 24ll * E ? 64 : rows <= 256ll * E ? 128 : 256;
-}
+// Few rows per expert: strips of 16 columns and groups of 16 rows, for each of which the expert's weights are read again.  Both products
+// with their map, us, strips | tiles of 64 | 128 | 256 rows: d 2048, f 1024, SwiGLU, 64 experts, rows per expert (uneven loads)
+//   4: 68 | 71 | 75 | 85     8: 79 | 80 | 84 | 94     16: 99 | 90 | 91 | 98     32: 135 | 92 | 98 | 103     64: 214 | 104 | 112 | 133
+//   128: 398 | 157 | 136 | 159     1024: - | 744 | 575 | 525;     128 experts, 512: - | 828 | 653 | 565
+// d 4096, f 14336, 8 experts
+//   2: 213 | 223 | 258 | 321     4: 239 | 251 | 271 | 335     16: 337 | 253 | 275 | 340     64: 930 | 384 | 299 | 350     256: - | 784 | 633 | 498
+int expert8_tile_rows(long long rows, int E) { return rows <= 8ll * E ? 0 : rows <= 40ll * E ? 64 : rows <= 200ll * E ? 128 : 256; }
 
 static int gemm8(int dtype, int act, const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
   if (dtype == MOE_DTYPE_F32) return gemm8_f32(act, g, c, max_tiles, s);
