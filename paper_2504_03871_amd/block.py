@@ -1,4 +1,4 @@
-"""An MoE block with a shared expert: scored routing, routed experts, a dense expert for every token, 8-bit checkpoints.
+"""MoE blocks with a shared expert, in training alone and behind their norm, and in 8 bits for inference: scored routing, routed experts, a dense expert for every token, 8-bit checkpoints.
 
     h      = silu(x Wg) * (x Wu)                                   the shared expert, moe_linear_fwd
     out    = sum_j w_j expert_{e_j}(x) + h Wd                      routed output as the down-projection's residual
@@ -84,3 +84,89 @@ class SharedExpertMoE:
         """Moves the balance bias towards an even load: up for experts below the mean, down for those above."""
         load = self.moe.counts.float()
         self.balance += rate * torch.sign(load.mean() - load)
+
+
+class NormedBlock:
+    """A SharedExpertMoE with what a network has in front of it, in training: the residual stream takes in the last block's output, with
+    dropout, and the block sees its norm.
+
+        h = residual + dropout(branch)      out = block(gamma h / rms(h))      the next block's branch is out, its residual h
+
+    `stream`: type of the residual stream (None: the block's).  Dropout's mask follows from `seed`, `layer` and the number in `step`, a
+    64-bit integer on the GPU that the caller advances once per training step, by a kernel, so that captured steps have masks of
+    their own."""
+
+    def __init__(self, block, stream=None, p=0.0, seed=0, layer=0, eps=1e-6):
+        self.block, m = block, block.moe
+        T, d, dtype = m.T, m.d, m.cfg.dtype
+        self.norm = B.make_norm(T, d, dtype, stream, eps=eps)
+        st = {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(self.norm.stream, torch.float32)
+        e = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=m.device)  # noqa: E731
+        self.step = torch.zeros(1, dtype=torch.int64, device=m.device)
+        self.drop = B.make_drop(p, seed, layer << 32, self.step) if p > 0 else None
+        self.gamma, self.dgamma = e(d, dtype=m.tdtype), e(d)      # gamma: filled by the caller
+        self.h, self.rstd, self.dh = e(T, d, dtype=st), e(T), e(T, d, dtype=st)
+        # without dropout and in one type the branch's gradient is the stream's
+        self.d_branch = e(T, d, dtype=m.tdtype) if p > 0 or st != m.tdtype else self.dh
+        self.ws = e(max(256, B.moe_norm_bwd_workspace_bytes(self.norm)), dtype=torch.uint8)
+
+    def forward(self, branch, residual=None):
+        """(out, h)."""
+        B.moe_norm_fwd(self.norm, self.drop, branch, residual, self.gamma, self.h, self.rstd, self.block.moe.x, None, None)
+        self.block.forward()
+        return self.block.moe.out, self.h
+
+    def backward(self, d_h=None, accumulate=0):
+        """(gradient of branch, gradient of residual) from block.moe.d_out and `d_h`, what reaches h past this block."""
+        self.block.backward(accumulate)
+        B.moe_norm_bwd(self.norm, self.drop, self.block.moe.dx, self.h, self.gamma, self.rstd, d_h, self.dh,
+                       None if self.d_branch is self.dh else self.d_branch, self.dgamma, accumulate, self.ws)
+        return self.d_branch, self.dh
+
+
+class ServedBlock:
+    """The same block as it answers requests, T tokens at a time: every product with weights and activations in 8 bits, a scale for each
+    column and each token.  `source`: a SharedExpertMoE whose weights are quantised here, once; its router is used as it is."""
+
+    def __init__(self, source, gamma, T, eps=1e-6):
+        m, self.T, self.score = source.moe, T, source.score
+        dtype, d, f, fs, td = m.cfg.dtype, m.d, m.f, source.Wg.shape[1], m.tdtype
+        if dtype == B.DTYPE_F32:
+            raise ValueError("8-bit products of experts have results of 16 bits")
+        e = lambda *s, dtype=td: torch.empty(*s, dtype=dtype, device=m.device)  # noqa: E731
+        i32 = lambda *s: e(*s, dtype=torch.int32)  # noqa: E731
+        f32 = lambda *s: e(*s, dtype=torch.float32)  # noqa: E731
+        i8 = lambda *s: e(*s, dtype=torch.int8)  # noqa: E731
+
+        def quantised(W):
+            n, (d_in, d_out) = (W.shape[0], W.shape[1:]) if W.dim() == 3 else (1, W.shape)
+            codes, scales = i8(n * d_in * d_out), f32(n, d_out)
+            B.moe_quant_weight(dtype, n, d_in, d_out, W, codes, scales)
+            return codes, scales
+
+        self.W1, self.W1b, self.W2 = quantised(m.W1), (None, None) if m.W1b is None else quantised(m.W1b), quantised(m.W2)
+        self.Wg, self.Wu, self.Wd = (quantised(w) for w in (source.Wg, source.Wu, source.Wd))
+        self.Wr, self.bias, self.balance, self.gamma = m.Wr, m.bias, source.balance, gamma
+        self.cfg = B.make_cfg(T, d, f, m.E, m.k, dtype, m.act, m.cfg.capacity)
+        self.norm = B.make_norm(T, d, dtype, eps=eps)
+        self.up, self.down = B.make_linear8(T, d, fs, dtype, B.ACT_SWIGLU), B.make_linear8(T, fs, d, dtype)
+        A = T * m.k
+        self.h, self.y, self.codes, self.scales, self.out = e(T, d), e(T, d), i8(T, d), f32(T), e(T, d)
+        self.logits, self.topk_idx, self.topk_w = f32(T, m.E), i32(T, m.k), f32(T, m.k)
+        self.counts, self.kept, self.offsets, self.row_of, self.src_of, self.y_perm = i32(m.E), i32(m.E), i32(m.E + 1), i32(A), i32(A), e(A, d)
+        self.hidden, self.hidden_codes, self.hidden_scales = e(T, fs), i8(T, fs), f32(T)
+        self.ws = e(max(256, B.moe_workspace_bytes(self.cfg), B.moe_expert_ffn8_workspace_bytes(self.cfg), B.moe_linear8_workspace_bytes(self.up),
+                        B.moe_linear8_workspace_bytes(self.down)), dtype=torch.uint8)
+
+    def forward(self, branch, residual=None):
+        """(out, h) as NormedBlock's, without dropout."""
+        B.moe_norm_fwd(self.norm, None, branch, residual, self.gamma, self.h, None, self.y, self.codes, self.scales)
+        B.moe_route_scored(self.cfg, self.score, self.y, self.Wr, self.bias, self.balance, None, self.logits, self.topk_idx, self.topk_w, self.ws)
+        B.moe_dispatch(self.cfg, None, self.topk_idx, None, None, self.counts, self.kept, self.offsets, self.row_of, self.src_of, None, self.ws)
+        B.moe_expert_ffn_fwd8(self.cfg, self.codes, self.scales, *self.W1, *self.W1b, *self.W2, self.src_of, self.offsets, self.kept, None, None,
+                              self.y_perm, self.ws)
+        B.moe_combine(self.cfg, self.y_perm, self.topk_w, self.topk_idx, self.row_of, self.offsets, self.kept, None, None, self.out)
+        B.moe_linear8_fwd(self.up, self.codes, self.scales, *self.Wg, *self.Wu, None, None, None, self.hidden, self.ws)
+        B.moe_quant_rows(self.up.dtype, self.T, self.hidden.shape[1], self.hidden.shape[1], self.hidden, self.hidden_codes, self.hidden_scales)
+        B.moe_linear8_fwd(self.down, self.hidden_codes, self.hidden_scales, *self.Wd, None, None, None, None, self.out, self.out, self.ws)
+        return self.out, self.h
