@@ -1212,11 +1212,15 @@ int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales
   g1.A = static_cast<const int8_t*>(x); g1.a_scale = x_scales; g1.src_of = src_of; g1.per_row = quotient_factor(cfg->k); g1.src_rows = cfg->T;
   g1.B = static_cast<const int8_t*>(W1); g1.B2 = static_cast<const int8_t*>(W1b); g1.b_scale = w1_scales; g1.b2_scale = w1b_scales;
   g1.N = f; g1.K = d; g1.C = w + l.hidden;
-  CHECK(launch_expert8(cfg->dtype, cfg->act, g1, tr, max_tiles, A, s));
+  {
+    ProfScope ps(cfg, MOE_PROF_GEMM1_FWD, s);
+    CHECK(launch_expert8(cfg->dtype, cfg->act, g1, tr, max_tiles, A, s));
+  }
   CHECK(launch_quant_rows(cfg->dtype, A, f, f, w + l.hidden, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, codes, scales, s));
   g2.A = codes; g2.a_scale = scales;
   g2.B = static_cast<const int8_t*>(W2); g2.b_scale = w2_scales;
   g2.N = d; g2.K = f; g2.C = y_perm;
+  ProfScope ps(cfg, MOE_PROF_GEMM2_FWD, s);
   return launch_expert8(cfg->dtype, MOE_ACT_NONE, g2, tr, max_tiles, A, s);
 }
 

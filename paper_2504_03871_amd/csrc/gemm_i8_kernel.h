@@ -182,102 +182,102 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 #define MOE_WAIT8(n_) __builtin_amdgcn_s_waitcnt(((n_) & 15) | (((n_) >> 4) << 14) | 0x70)
   auto mainloop = [&](int bands) {
     if constexpr (DEPTH == 2) {
-    int a0 = 0, a1 = A_BYTES, a2 = 2 * A_BYTES, b0 = 0, b1 = B_STAGE;
-    request(S0, a0, b0);
-    if (KS - S0 > 1) {
-      request(S0 + 1, a1, b1);
-      MOE_WAIT8(L);
-    } else {
-      MOE_WAIT8(0);
-    }
-    barrier();
+      int a0 = 0, a1 = A_BYTES, a2 = 2 * A_BYTES, b0 = 0, b1 = B_STAGE;
+      request(S0, a0, b0);
+      if (KS - S0 > 1) {
+        request(S0 + 1, a1, b1);
+        MOE_WAIT8(L);
+      } else {
+        MOE_WAIT8(0);
+      }
+      barrier();
 #pragma unroll
-    for (int i = 0; i < TM; ++i) frag_a(i, a0, 0);
+      for (int i = 0; i < TM; ++i) frag_a(i, a0, 0);
 #pragma unroll
-    for (int j = 0; j < TNN; ++j) frag_b(0, j, b0, 0);
-    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-    // Iteration S: K step 0 reads the fragments of K step 1 and requests A of stage S + 2, whose LDS has been free since the last barrier;
-    // then every wave waits for stage S + 1 (B of it, and A, are older than those loads) and for its reads, and joins the barrier;
-    // K step 1 reads the first fragments of stage S + 1 and requests B of stage S + 2 into what stage S has left.
-    auto iteration = [&](int S, bool more, auto load) {
-      constexpr bool LOAD = decltype(load)::value != 0;
-      step(Const<0>{}, true, a0, b0, 1, [&](int r) {
-        if constexpr (LOAD) {
+      for (int j = 0; j < TNN; ++j) frag_b(0, j, b0, 0);
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+      // Iteration S: K step 0 reads the fragments of K step 1 and requests A of stage S + 2, whose LDS has been free since the last barrier;
+      // then every wave waits for stage S + 1 (B of it, and A, are older than those loads) and for its reads, and joins the barrier;
+      // K step 1 reads the first fragments of stage S + 1 and requests B of stage S + 2 into what stage S has left.
+      auto iteration = [&](int S, bool more, auto load) {
+        constexpr bool LOAD = decltype(load)::value != 0;
+        step(Const<0>{}, true, a0, b0, 1, [&](int r) {
+          if constexpr (LOAD) {
 #pragma unroll
-          for (int q = 0; q < LA; ++q)
-            if (q * TM / LA == r) load_a(q, S + 2, a2);
+            for (int q = 0; q < LA; ++q)
+              if (q * TM / LA == r) load_a(q, S + 2, a2);
+          }
+        }, bands);
+        if (more) {
+          if constexpr (LOAD) MOE_WAIT8(LA);
+          else MOE_WAIT8(0);
+          barrier();
         }
-      }, bands);
-      if (more) {
-        if constexpr (LOAD) MOE_WAIT8(LA);
+        step(Const<1>{}, more, a1, b1, 0, [&](int r) {
+          if constexpr (LOAD) {
+#pragma unroll
+            for (int q = 0; q < LB; ++q)
+              if (q * TM / LB == r) load_b(q, S + 2, b0);   // (in the first half of the regions: 0.6 % slower)
+          }
+        }, bands);
+        const int a = a0; a0 = a1; a1 = a2; a2 = a;
+        const int b = b0; b0 = b1; b1 = b;
+      };
+      int S = S0;
+#pragma unroll 1
+      for (; S + 2 < KS; ++S) iteration(S, true, Const<1>{});
+#pragma unroll 1
+      for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
+    } else {
+      // Three stages of both, all requested ahead: where a compute unit has one or two small blocks, a stage's products are over long before
+      // a load requested an iteration ago has landed.  Stage S + 3 goes where stage S was, in K step 1 of iteration S.  (Tiles of 64 x 128,
+      // us, the pipeline above -> this one: 300 x 4096 x 4096 17.8 -> 13.1, 64 x 14336 x 4096 52 -> 33, 8192 x 2048 x 8192 188 -> 179.  Four and six
+      // stages leave room for one block: 300 x 4096 x 4096 15.1 and 15.7, 8192 x 2048 x 8192 266 and 293.  128 x 128, three stages and
+      // one block per compute unit: 300 x 4096 x 4096 19.1 -> 17.2, but 8192 x 2048 x 8192 146 -> 177.)
+      static_assert(DEPTH == 3 && 2 * L < 64, "the wait counter");
+#pragma unroll
+      for (int q = 0; q < DEPTH; ++q)
+        if (S0 + q < KS) request(S0 + q, q * A_BYTES, q * B_STAGE);
+      auto wait_for = [&](int left) {   // all but `left` stages
+        if (left >= 2) MOE_WAIT8(2 * L);
+        else if (left == 1) MOE_WAIT8(L);
         else MOE_WAIT8(0);
-        barrier();
-      }
-      step(Const<1>{}, more, a1, b1, 0, [&](int r) {
-        if constexpr (LOAD) {
+      };
+      wait_for(min(KS - S0, DEPTH) - 1);
+      barrier();
 #pragma unroll
-          for (int q = 0; q < LB; ++q)
-            if (q * TM / (2 * LB) == r) load_b(q, S + 2, b0);
+      for (int i = 0; i < TM; ++i) frag_a(i, 0, 0);
+#pragma unroll
+      for (int j = 0; j < TNN; ++j) frag_b(0, j, 0, 0);
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+      int at = 0;   // which stage of LDS is multiplied
+      auto iteration = [&](int S, bool more, auto load) {
+        constexpr bool LOAD = decltype(load)::value != 0;
+        const int next = at + 1 == DEPTH ? 0 : at + 1;
+        step(Const<0>{}, true, at * A_BYTES, at * B_STAGE, 1, [&](int) {}, bands);
+        if (more) {
+          if constexpr (LOAD) MOE_WAIT8((DEPTH - 2) * L);
+          else wait_for(KS - 2 - S);
+          barrier();
         }
-      }, bands);
-      const int a = a0; a0 = a1; a1 = a2; a2 = a;
-      const int b = b0; b0 = b1; b1 = b;
-    };
-    int S = S0;
-#pragma unroll 1
-    for (; S + 2 < KS; ++S) iteration(S, true, Const<1>{});
-#pragma unroll 1
-    for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
-    } else {
-    // Three stages of both, all requested ahead: where a compute unit has one or two small blocks, a stage's products are over long before
-    // a load requested an iteration ago has landed.  Stage S + 3 goes where stage S was, in K step 1 of iteration S.  (Tiles of 64 x 128,
-    // us, the pipeline above -> this one: 300 x 4096 x 4096 17.8 -> 13.1, 64 x 14336 x 4096 52 -> 33, 8192 x 2048 x 8192 188 -> 179.  Four and six
-    // stages leave room for one block: 300 x 4096 x 4096 15.1 and 15.7, 8192 x 2048 x 8192 266 and 293.  128 x 128, three stages and
-    // one block per compute unit: 300 x 4096 x 4096 19.1 -> 17.2, but 8192 x 2048 x 8192 146 -> 177.)
-    static_assert(DEPTH == 3 && 2 * L < 64, "the wait counter");
+        step(Const<1>{}, more, next * A_BYTES, next * B_STAGE, 0, [&](int r) {
+          if constexpr (LOAD) {
 #pragma unroll
-    for (int q = 0; q < DEPTH; ++q)
-      if (S0 + q < KS) request(S0 + q, q * A_BYTES, q * B_STAGE);
-    auto wait_for = [&](int left) {   // all but `left` stages
-      if (left >= 2) MOE_WAIT8(2 * L);
-      else if (left == 1) MOE_WAIT8(L);
-      else MOE_WAIT8(0);
-    };
-    wait_for(min(KS - S0, DEPTH) - 1);
-    barrier();
-#pragma unroll
-    for (int i = 0; i < TM; ++i) frag_a(i, 0, 0);
-#pragma unroll
-    for (int j = 0; j < TNN; ++j) frag_b(0, j, 0, 0);
-    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
-    int at = 0;   // which stage of LDS is multiplied
-    auto iteration = [&](int S, bool more, auto load) {
-      constexpr bool LOAD = decltype(load)::value != 0;
-      const int next = at + 1 == DEPTH ? 0 : at + 1;
-      step(Const<0>{}, true, at * A_BYTES, at * B_STAGE, 1, [&](int) {}, bands);
-      if (more) {
-        if constexpr (LOAD) MOE_WAIT8((DEPTH - 2) * L);
-        else wait_for(KS - 2 - S);
-        barrier();
-      }
-      step(Const<1>{}, more, next * A_BYTES, next * B_STAGE, 0, [&](int r) {
-        if constexpr (LOAD) {
-#pragma unroll
-          for (int q = 0; q < L; ++q)
-            if (q * TM / L == r) {
-              if (q < LB) load_b(q, S + DEPTH, at * B_STAGE);
-              else load_a(q - LB, S + DEPTH, at * A_BYTES);
-            }
-        }
-      }, bands);
-      at = next;
-    };
-    int S = S0;
+            for (int q = 0; q < L; ++q)
+              if (q * TM / L == r) {
+                if (q < LB) load_b(q, S + DEPTH, at * B_STAGE);
+                else load_a(q - LB, S + DEPTH, at * A_BYTES);
+              }
+          }
+        }, bands);
+        at = next;
+      };
+      int S = S0;
 #pragma unroll 1
-    for (; S + DEPTH < KS; ++S) iteration(S, true, Const<1>{});
+      for (; S + DEPTH < KS; ++S) iteration(S, true, Const<1>{});
 #pragma unroll 1
-    for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
-   }
+      for (; S < KS; ++S) iteration(S, S + 1 < KS, Const<0>{});
+    }
   };
 #undef MOE_WAIT8
   if (ni == WTM) mainloop(WTM);

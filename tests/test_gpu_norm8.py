@@ -430,3 +430,57 @@ def test_experts_are_the_dense_products_of_their_rows(T, E, k, d, f, cap, sliced
         B.moe_quant_rows(DT[dtype], n, f, f, h, hc, hs)
         want[rows] = linear8(n, f, d, dtype, "none", hc, hs, [l2[e]], [s2[e].contiguous()])
     assert torch.equal(y, want)
+
+
+# ---- beyond 32 bits ------------------------------------------------------------------------------------------------
+
+def test_matrices_of_more_than_2_to_the_32_elements():
+    """The last rows of matrices past 2^32 elements are those of the same rows by themselves."""
+    rows, width = (1 << 18) + 3, 16384
+    x = torch.full((rows, width), 0.5, dtype=torch.bfloat16, device=DEV)
+    r = np.random.default_rng(0)
+    tail = dev(r.normal(size=(3, width)), "bf16")
+    x[-3:] = tail
+    norm, y = B.make_norm(rows, width, B.DTYPE_BF16), torch.empty_like(x)
+    B.moe_norm_fwd(norm, None, x, None, None, None, None, y, None, None)
+    y3 = empty(3, width, dtype="bf16")
+    B.moe_norm_fwd(B.make_norm(3, width, B.DTYPE_BF16), None, tail, None, None, None, None, y3, None, None)
+    assert torch.equal(y[-3:], y3) and bool((y[1 << 17] == 1).all())
+    B.moe_dropout(B.DTYPE_BF16, rows, width, B.make_drop(0.5, 3, 4), x, None, y)
+    m = O.drop_mask(3, width, 0.5, 3, 4, first_row=rows - 3)
+    assert np.array_equal(f64(y[-3:]), f64(tail) * m)
+    q, s, q3, s3 = torch.empty((rows, width), dtype=torch.int8, device=DEV), empty(rows), torch.empty((3, width), dtype=torch.int8, device=DEV), empty(3)
+    B.moe_quant_rows(B.DTYPE_BF16, rows, width, width, x, q, s)
+    B.moe_quant_rows(B.DTYPE_BF16, 3, width, width, tail, q3, s3)
+    assert torch.equal(q[-3:], q3) and torch.equal(s[-3:], s3)
+    del x
+    # a product with that many results, and rows of A past 2^32 bytes
+    w, ws = codes(r, width, 64), dev(r.random(64))
+    lw = [laid(w)]
+    y = linear8(rows, width, 64, "bf16", "none", q, s, lw, [ws])
+    assert torch.equal(y[-3:], linear8(3, width, 64, "bf16", "none", q3, s3, lw, [ws]))
+    del q, y
+    T, N = (1 << 18) + 5, 16384
+    xs, w = codes(r, T, 64), codes(r, 64, N)
+    dx, sx, lw, ws = torch.from_numpy(xs).to(DEV), dev(r.random(T)), [laid(w)], dev(r.random(N))
+    y = linear8(T, 64, N, "bf16", "none", dx, sx, lw, [ws])
+    assert torch.equal(y[-5:], linear8(5, 64, N, "bf16", "none", dx[-5:].contiguous(), sx[-5:].contiguous(), lw, [ws]))
+
+
+def test_calls_on_two_streams_at_once():
+    """Calls with buffers of their own do not see each other."""
+    r = np.random.default_rng(7)
+    T, K, N = 100, 8192, 256
+    x, w = codes(r, T, K), codes(r, K, N)
+    xs, ws = dev(r.random(T) / K), dev(r.random(N))
+    dx, lw = torch.from_numpy(x).to(DEV), [laid(w)]
+    want = linear8(T, K, N, "bf16", "none", dx, xs, lw, [ws])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(linear8(T, K, N, "bf16", "none", dx, xs, lw, [ws]))
+    torch.cuda.synchronize()
+    for g in got:
+        assert torch.equal(g, want)
