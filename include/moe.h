@@ -488,7 +488,7 @@ MOE_API int moe_dropout(int32_t dtype, int64_t rows, int32_t width, const moe_dr
  *
  * Backward: a = gamma dy, u = h rstd; dh = rstd (a - u mean(a u)) + dh_add (NULL: nothing; the gradient that reaches h by other ways), which
  * is the gradient of residual too; dx = dropout's gradient of dh; dgamma = sum over the rows of dy u.  dh, dx, dgamma may be NULL: skipped;
- * dh may be dh_add, and dx may be dy (not dh: MOE_ERR_OVERLAP).  dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or
+ * dh may be dh_add, and dx or dh may be dy or h (dx not dh: MOE_ERR_OVERLAP).  dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or
  * dtype (accumulate must be 0).  ws holds moe_norm_bwd_workspace_bytes (enough for any smaller T too) and is needed for dgamma only.  No atomics: the same bits every time.
  */
 #define MOE_MAX_NORM 16384

@@ -1094,7 +1094,7 @@ int moe_norm_bwd(const moe_norm* norm, const moe_drop* drop, const void* dy, con
       return MOE_OK;
     }
   }
-  NormBwdArgs a = {dy, h, gamma, rstd, dh_add, dh, dx, dgamma != nullptr ? (float*)ws : nullptr, drop_args(drop), norm->T, norm->d};
+  NormBwdArgs a = {dy, h, gamma, rstd, dh_add, dh, dx, dgamma != nullptr ? (float*)ws : nullptr, nullptr, drop_args(drop), norm->T, norm->d, 0, 0, 0, 0};
   return launch_norm_bwd(norm, a, dgamma, accumulate, (hipStream_t)stream);
 }
 

@@ -21,9 +21,12 @@ struct NormBwdArgs {
   const float* rstd;
   const void* dh_add;
   void *dh, *dx;
-  float* partials;   // [blocks][d], or NULL: no gradient of gamma
+  float* partials;   // [row_blocks][d], or NULL: no gradient of gamma
+  void* dgamma;
   DropArgs drop;
   int T, d;
+  int grad, accumulate;
+  int row_blocks, col_blocks;   // col_blocks: of few rows' gradient of gamma (NORM_FEW), else 0
 };
 // A wave holds a row of up to 1024 values by itself, or, so that few rows fill the chip, two waves share one of more than 512.  (Forward |
 // backward, us, one wave -> two: 300 rows of 516 fp32 4.8 | 8.5 -> 3.9 | 7.5; 4096 of 700 bf16 7.7 | 12.3 -> 8.3 | 16.8; 8192 of 1024
@@ -47,6 +50,13 @@ inline int norm_bwd_blocks(int T, int d) {
   const long long want = ((long long)T + rows - 1) / rows, most = 256 * per_cu;
   return (int)(want < most ? want : most);
 }
+// Few rows: gamma's gradient in blocks of the same launch, which read them again, FEW_LANES rows at a time, instead of partial sums and a
+// launch that adds them.  (Partial sums -> this, us: 300 x 516 fp32 7.7 -> 4.3; 512 x 4096 bf16 16.5 -> 5.7; 1024 x 1024 11.6 -> 4.4; 1024 x 4096
+// 20.5 -> 9.7, in blocks of no order 14; 2048 x 1024 9.8 -> 6.2; 2048 x 4096 25.6 -> 24.6; 1024 x 16384 48.6 -> 41.7; 4096 x 1024 11.9 ->
+// 14.8; 8192 x 1024 18 -> 52, and no better in segments of the rows.)
+constexpr int NORM_FEW = 2048;
+constexpr int FEW_LANES = 128;   // threads to every eight columns
+inline int few_cols(const RowGeom& g) { return row_threads(g) / FEW_LANES * 8; }
 // (enough for any smaller T too)
 inline size_t norm_bwd_ws_bytes(const moe_norm* n) { return align_up((size_t)(n->T < 1024 ? n->T : 1024) * n->d * 4, 256); }
 

@@ -7,6 +7,7 @@
 // forward from a kept h gives the same bits.  Sums are fp32; every result is rounded once.
 //
 // One pass over memory each: a row stays in the registers of one or several waves (rows.h) between its sums and its results.
+#include "gemm.h"
 #include "norm.h"
 
 namespace moe {
@@ -76,8 +77,54 @@ __global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_fwd_kernel
   }
 }
 
+// Gamma's gradient for a few columns from all rows: 128 threads for every eight columns, by rows, whose sums are added in order, in sixteen
+// runs of eight first.
+template <typename T, typename S, bool ODD, int THREADS>
+__device__ __forceinline__ void dgamma_few(const NormBwdArgs& a, int block) {
+  constexpr int LANES = FEW_LANES, MOST = THREADS / LANES * 8;   // columns of a block, at most
+  __shared__ float part[LANES][MOST + 1], run[16][MOST + 1];
+  const int groups = blockDim.x / LANES, cols = groups * 8, cg = threadIdx.x % groups, rl = threadIdx.x / groups, c0 = block * cols, c = c0 + cg * 8, d = a.d;
+  const bool live = (int)threadIdx.x < groups * LANES;   // (a block need not be whole groups of 128 threads)
+  float s[8] = {};
+#pragma unroll 4
+  for (int r = live ? rl : a.T; r < a.T; r += LANES) {
+    const size_t at = (size_t)r * d;
+    float w[8], u[8];
+    unpack_row8<T, ODD>(load_row8<T, ODD, false>(reinterpret_cast<const T*>(a.dy) + at, c, d), c, d, w);
+    unpack_row8<S, ODD>(load_row8<S, ODD, false>(reinterpret_cast<const S*>(a.h) + at, c, d), c, d, u);
+    const float q = a.rstd[r];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = fmaf(w[j], u[j] * q, s[j]);
+  }
+  if (live) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[rl][cg * 8 + j] = s[j];
+  }
+  __syncthreads();
+  const int col = threadIdx.x % cols, seg = threadIdx.x / cols;   // 16 segments of the live threads
+  float sum = 0.f;
+  if (live) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum += part[seg * 8 + r][col];
+    run[seg][col] = sum;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= cols || c0 + col >= d) return;
+#pragma unroll
+  for (int r = 1; r < 16; ++r) sum += run[r][col];
+  if (a.grad == MOE_DTYPE_F32) {
+    float* out = reinterpret_cast<float*>(a.dgamma) + c0 + col;
+    *out = sum + (a.accumulate ? *out : 0.f);
+  } else {   // T: gamma's own type
+    reinterpret_cast<T*>(a.dgamma)[c0 + col] = from_f32<T>(sum);
+  }
+}
+
 template <typename T, typename S, bool ODD, int MAXW, int NCH>
 __global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_bwd_kernel(NormBwdArgs a) {
+  // the columns' blocks first, they take longest; the blocks of an XCD next to each other, so that they share the lines that they cut
+  const int block = (int)blockIdx.x - a.col_blocks;
+  if (block < 0) return dgamma_few<T, S, ODD, MAXW == 1 ? 256 : MAXW * WAVE>(a, chunk_position(blockIdx.x, a.col_blocks, a.col_blocks / NUM_XCD + 1));
   constexpr int R = MAXW == 1 ? 4 : 1;
   __shared__ __align__(16) float s_sum[2][MAXW];
   const int TPR = MAXW == 1 ? WAVE : (int)blockDim.x, tid = MAXW == 1 ? threadIdx.x % WAVE : threadIdx.x, d = a.d;
@@ -101,7 +148,7 @@ __global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_bwd_kernel
     f.r = a.rstd[row];
   };
   Row now = {}, next = {};
-  const int first = blockIdx.x * R + (MAXW == 1 ? threadIdx.x / WAVE : 0), stride = gridDim.x * R;
+  const int first = block * R + (MAXW == 1 ? threadIdx.x / WAVE : 0), stride = a.row_blocks * R;
   if constexpr (AHEAD) fetch(first, now);
   for (int row = first; row < a.T; row += stride, turn ^= 1) {
     if constexpr (AHEAD) fetch(row + stride, next);
@@ -145,8 +192,8 @@ __global__ __launch_bounds__(MAXW == 1 ? 256 : MAXW * WAVE) void norm_bwd_kernel
     }
     if constexpr (AHEAD) now = next;
   }
-  if (a.partials == nullptr) return;
-  float* out = a.partials + (size_t)blockIdx.x * d;
+  if (a.partials == nullptr || a.col_blocks > 0) return;
+  float* out = a.partials + (size_t)block * d;
   if constexpr (R > 1) {   // the block's waves one after the other: the same order every time
     __shared__ float s_dg[NCH * WAVE * 8];
     for (int w = 1; w < R; ++w) {
@@ -266,7 +313,7 @@ int launch_norm_fwd(const moe_norm* n, const NormFwdArgs& a, hipStream_t s) {
 template <typename T, typename S>
 static int norm_bwd_for(const NormBwdArgs& a, hipStream_t s) {
   const RowGeom geom = norm_geom(a.T, a.d);
-  const unsigned grid = (unsigned)norm_bwd_blocks(a.T, a.d);
+  const unsigned grid = (unsigned)(a.row_blocks + a.col_blocks);
 #define MOE_NORM_BWD(O_, W_, C_) norm_bwd_kernel<T, S, O_, W_, C_><<<grid, row_threads(geom), 0, s>>>(a)
   MOE_NORM_GEOM(a.d, geom, MOE_NORM_BWD);
 #undef MOE_NORM_BWD
@@ -277,18 +324,27 @@ static int dgamma_for(const float* partials, int rows, int d, void* out, int acc
   norm_dgamma_kernel<OT><<<(d + 15) / 16, 16 * DGAMMA_ROWS, 0, s>>>(partials, rows, d, (OT*)out, accumulate);
   return launch_status();
 }
-int launch_norm_bwd(const moe_norm* n, const NormBwdArgs& a, void* dgamma, int accumulate, hipStream_t s) {
-  int rc = MOE_OK, rows = 0;
+int launch_norm_bwd(const moe_norm* n, const NormBwdArgs& args, void* dgamma, int accumulate, hipStream_t s) {
+  NormBwdArgs a = args;
+  a.row_blocks = n->T > 0 ? norm_bwd_blocks(n->T, n->d) : 0;
+  a.grad = n->grad;
+  a.accumulate = accumulate;
+  a.dgamma = dgamma;
+  const int cols = few_cols(norm_geom(n->T, n->d));
+  // (not where a result takes the place of what the columns' blocks read)
+  const bool in_place = a.dx == a.dy || a.dh == a.dy || a.dx == a.h || a.dh == a.h;
+  if (n->T > 0 && n->T <= NORM_FEW && dgamma != nullptr && !in_place) a.col_blocks = (n->d + cols - 1) / cols;
   if (n->T > 0) {
-    rows = norm_bwd_blocks(n->T, n->d);
+    int rc;
     if (n->dtype == MOE_DTYPE_F32) rc = norm_bwd_for<float, float>(a, s);
     else if (n->dtype == MOE_DTYPE_BF16) rc = n->stream == MOE_DTYPE_F32 ? norm_bwd_for<bf16, float>(a, s) : norm_bwd_for<bf16, bf16>(a, s);
     else rc = n->stream == MOE_DTYPE_F32 ? norm_bwd_for<f16, float>(a, s) : norm_bwd_for<f16, f16>(a, s);
+    if (rc != MOE_OK || a.col_blocks > 0) return rc;
   }
-  if (rc != MOE_OK || dgamma == nullptr || (rows == 0 && accumulate)) return rc;
-  return n->grad == MOE_DTYPE_F32    ? dgamma_for<float>(a.partials, rows, n->d, dgamma, accumulate, s)
-         : n->grad == MOE_DTYPE_BF16 ? dgamma_for<bf16>(a.partials, rows, n->d, dgamma, accumulate, s)
-                                     : dgamma_for<f16>(a.partials, rows, n->d, dgamma, accumulate, s);
+  if (dgamma == nullptr || (n->T == 0 && accumulate)) return MOE_OK;
+  return n->grad == MOE_DTYPE_F32    ? dgamma_for<float>(a.partials, a.row_blocks, n->d, dgamma, accumulate, s)
+         : n->grad == MOE_DTYPE_BF16 ? dgamma_for<bf16>(a.partials, a.row_blocks, n->d, dgamma, accumulate, s)
+                                     : dgamma_for<f16>(a.partials, a.row_blocks, n->d, dgamma, accumulate, s);
 }
 
 template <typename T>

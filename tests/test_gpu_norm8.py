@@ -104,7 +104,7 @@ def norm_tolerance(d):
 
 NORM = [  # T, d
     (1, 1), (3, 7), (5, 8), (2, 64), (4, 100), (1, 500), (3, 512), (9, 516), (2, 1000), (3, 1024), (2, 1091), (5, 2048), (3, 3000), (3, 4096), (1, 4100),
-    (2, 4099), (2, 8192), (1, 8200), (1, 16384), (2, 16383), (300, 72), (77, 24),
+    (2, 4099), (2, 8192), (1, 8200), (1, 16384), (2, 16383), (300, 72), (77, 24), (1024, 513), (1025, 1000), (1100, 100), (1500, 1091), (2048, 264), (2049, 264), (2100, 520), (2500, 1091), (2200, 63),
 ]
 KINDS = [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32"), ("f32", "f32")]
 
@@ -169,6 +169,27 @@ def test_norm_forward_and_backward(T, d, dtype, stream):
         assert torch.equal(r2, h) and torch.equal(y2, y)
 
 
+@pytest.mark.parametrize("T, d", [(3, 64), (700, 1091), (2048, 520), (3000, 256)])
+@pytest.mark.parametrize("dtype, stream", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+def test_norm_backward_in_place_with_the_gradient_of_gamma(T, d, dtype, stream):
+    """dx over dy and dh over dh_add, dh over h, and dh over dy where the types are one: the gradients of the same call with places of its own."""
+    x, h, g, dy, add = norm_case(T, d, dtype, stream, 5)
+    norm, drop = B.make_norm(T, d, DT[dtype], DT[stream]), B.make_drop(0.25, 3)
+    rstd, y = empty(T), empty(T, d, dtype=dtype)
+    B.moe_norm_fwd(norm, None, h if dtype == stream else h.to(TD[dtype]), None, g, None, rstd, y, None, None)
+    dh, dx, dg, ws = empty(T, d, dtype=stream), empty(T, d, dtype=dtype), empty(d), torch.empty(B.moe_norm_bwd_workspace_bytes(norm), dtype=torch.uint8, device=DEV)
+    B.moe_norm_bwd(norm, drop, dy, h, g, rstd, add, dh, dx, dg, 0, ws)
+    sums = (norm_tolerance(d) + (T + 40) * U) * (dy.double().abs() * (h.double() * rstd.double()[:, None]).abs()).sum(dim=0) + 1e-30
+    for places in ("dx over dy, dh over dh_add", "dh over h", "dh over dy"):
+        if places == "dh over dy" and dtype != stream:
+            continue
+        dy2, h2, add2, dg2 = dy.clone(), h.clone(), add.clone(), empty(d)
+        to_h, to_x = {"dx over dy, dh over dh_add": (add2, dy2), "dh over h": (h2, empty(T, d, dtype=dtype)), "dh over dy": (dy2, empty(T, d, dtype=dtype))}[places]
+        B.moe_norm_bwd(norm, drop, dy2, h2, g, rstd, add2, to_h, to_x, dg2, 0, ws)
+        assert torch.equal(to_h, dh) and torch.equal(to_x, dx), places
+        assert bool(((dg2.double() - dg.double()).abs() <= 2 * sums).all()), places     # another order of the sum
+
+
 def test_norm_gradient_against_differences_of_its_forward():
     T, d, eps = 6, 40, 1e-3
     x, q, g, dy, add = norm_case(T, d, "f32", "f32", 3)
@@ -212,8 +233,8 @@ def test_norm_rows_that_hold_zeros_or_no_numbers_and_what_lies_behind_the_last()
         assert (dg == 0).all()
 
 
-def test_norm_backward_of_many_rows_is_the_same_every_time_and_in_a_graph():
-    T, d = 5000, 256
+@pytest.mark.parametrize("T, d", [(5000, 256), (700, 1536)])
+def test_norm_backward_of_many_rows_is_the_same_every_time_and_in_a_graph(T, d):
     x, q, g, dy, add = norm_case(T, d, "bf16", "f32", 1)
     norm, drop = B.make_norm(T, d, B.DTYPE_BF16, B.DTYPE_F32, grad=B.DTYPE_BF16), B.make_drop(0.1, 1)
     h, rstd, y, dh, dx = empty(T, d), empty(T), empty(T, d, dtype="bf16"), empty(T, d), empty(T, d, dtype="bf16")
