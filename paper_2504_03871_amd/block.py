@@ -1,4 +1,5 @@
-"""MoE blocks with a shared expert, in training alone and behind their norm, and in 8 bits for inference: scored routing, routed experts, a dense expert for every token, 8-bit checkpoints.
+"""MoE blocks with a shared expert, alone and behind their norm, and in 8 bits for inference: scored routing, routed experts, a dense expert for
+every token, 8-bit checkpoints.
 
     h      = silu(x Wg) * (x Wu)                                   the shared expert, moe_linear_fwd
     out    = sum_j w_j expert_{e_j}(x) + h Wd                      routed output as the down-projection's residual

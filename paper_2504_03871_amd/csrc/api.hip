@@ -1196,6 +1196,7 @@ int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales
   const int A = cfg->T * cfg->k, d = cfg->d_model, f = cfg->d_ff, tr = expert8_tile_rows(A, cfg->E);
   Gemm8Args g = {};
   g.offsets = offsets; g.kept = kept; g.lo = slice_lo; g.hi = slice_hi; g.E = cfg->E;
+  g.stream = streams8((long long)std::min(cfg->E, A) * (swiglu ? 3 : 2) * d * f);
   if (tr > 0) {
     TileMapArgs tm = {offsets, kept, slice_lo, slice_hi, cfg->E};
     tm.tile_rows = tr;

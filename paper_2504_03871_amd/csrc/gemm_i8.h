@@ -22,6 +22,7 @@ struct Gemm8Args {
   const int32_t *offsets, *kept, *lo, *hi;
   int E;
   int chunked;              // order of the tiles (block_to_tile)
+  int stream;               // weights read once are requested as streaming data (streams8)
   int few_nk;               // few rows: waves that share a strip's K range (1, 2, 4 or 8)
   int32_t* parts;           // dense tiles: sums of K parts, [part][matrix][row][N]
   int n_parts;
@@ -41,6 +42,12 @@ inline size_t linear8_ws_bytes(long long T, int N, int mats) {
   const size_t all = (size_t)MAX_PARTS8 * mats * T * N * 4, most = (size_t)512 * 128 * 128 * 4;
   return T <= FEW_ROWS8 ? 0 : align_up(all < most ? all : most, 256);
 }
+// Whether weights that are read once are requested as streaming data: where they are more than the memory-side cache keeps for the next
+// time.  Strips and tiles below 256 rows, us, plain -> streaming, both products: 4 tokens x 2 of 8 experts, d 4096, f 14336, 183 -> 160, 32
+// tokens 249 -> 226, 64 tokens 247 -> 228, 256 tokens 297 -> 288; 32 x 8 of 128, d 2048, f 1024 (805 MB at most) 104 -> 95; 512 x 4 of 64 (403
+// MB) 95 -> 88.  Dense weights of 59 to 117 MB that come from memory gain 4 to 8 %, but lose up to 30 % where the cache still has them (16 x
+// 14336 x 4096 12.0 -> 15.9), so they stay plain.
+inline bool streams8(long long weights) { return weights >= MEMORY_SIDE_CACHE / 4 * 5; }
 // Row tiles of the experts' products: 0 for the few-row kernel
 int expert8_tile_rows(long long rows, int E);
 

@@ -118,6 +118,8 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     b_vo[i] = ((unsigned)(n0 / TILE8_N + id / 2) * (unsigned)KT + (unsigned)(id & 1)) * TILE8_BYTES + (unsigned)lane * 16u;
   }
   const int half = wave & 1;
+  // weights that one row tile takes, of more than the caches hold: streaming data (Gemm8Args.stream)
+  const bool once = BM < 256 && g.stream && (GROUPED ? __builtin_amdgcn_readfirstlane(t.mates) == 0 : n_rt == 1);
   const unsigned smem_base = lds_addr(smem);
   const int wbase = wave * 1024;
   int a_fr[2];
@@ -130,7 +132,9 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     const int c = DUAL ? q / 2 : q;
     const bool first = !DUAL || q % 2 == 0;
     const unsigned off = 2 * stage + half < KT ? b_vo[c] + (unsigned)stage * (2 * TILE8_BYTES) : OUT_OF_RANGE;
-    load_to_lds16(first ? rb : rb2, smem_base + B_AT + buf + (first ? 0 : B_BYTES) + wbase + NT * 16 * c, off);
+    const unsigned to = smem_base + B_AT + buf + (first ? 0 : B_BYTES) + wbase + NT * 16 * c;
+    if (BM < 256 && once) load_to_lds16_nt(first ? rb : rb2, to, off);
+    else load_to_lds16(first ? rb : rb2, to, off);
   };
   i32x4 af[TM], bf[2][TNN], bf2[2][DUAL ? TNN : 1];
   auto frag_a = [&](int i, int buf, int ks) {
@@ -425,11 +429,13 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 // A block of eight waves takes strips of 16 columns and a group of 16 MT rows: 8 / nk strips, the K range of each shared out among nk
 // waves, 64 values at a time in turn, whose sums are added in LDS, in any order the same: they are integers.  An operand of B is one
 // contiguous 1 KB load of a wave, of A 16 rows x 64 bytes that all strips read from the caches; the next U of either are requested before the
-// last are used.  Bound by the read of the weights.
+// last are used.  (16 rows, 16 x 14336 x 4096, four | two in flight: 11.9 | 10.9 us, but 1 x 14336 x 4096 from memory 12.1 | 13.1 and 32 tokens
+// x 8 of 128 experts 93 | 95; eight: worse.)  Bound by the read of the weights: 16 x 4096 x 14336 of two matrices 19.2 us, 6.1 TB/s with a
+// part in the caches, 25.8 (4.6) from memory; 4 tokens x 2 of 8 experts, d 4096, f 14336, 160 us, 6.6 TB/s of 1.06 GB.
 // Experts: blockIdx.y is the n-th group of 16 MT rows of some expert, which every block finds for itself from the experts' row counts.
 constexpr int FEW_WAVES = 8;
 
-template <typename ST, int ACT, int MT, bool GROUPED>
+template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
   constexpr int MATS = DUAL ? 2 : 1, ROWS = 16 * MT, U = MT == 1 ? 4 : 2;
@@ -475,13 +481,17 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     pa[i] = g.A + (size_t)row_of_a(g, row0 + min(i * 16 + (lane & 15), rows - 1)) * K + (lane >> 4) * 16;   // (rows past the group repeat its last)
   i32x4 acc[MATS][MT] = {};
   struct Operands { i32x4 b[U][MATS], a[U][MT]; };
+  auto weights = [](const int8_t* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
+    else return *reinterpret_cast<const i32x4*>(p);
+  };
   // tiles k, k + nk, ... of this wave, U of them; past the end the last one again, which is then not used
   auto fetch = [&](int k, Operands& o) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const size_t at = (size_t)min(k + u * nk, k1 - 1);
-      o.b[u][0] = *reinterpret_cast<const i32x4*>(pb + at * TILE8_BYTES);
-      if constexpr (DUAL) o.b[u][1] = *reinterpret_cast<const i32x4*>(pb2 + at * TILE8_BYTES);
+      o.b[u][0] = weights(pb + at * TILE8_BYTES);
+      if constexpr (DUAL) o.b[u][1] = weights(pb2 + at * TILE8_BYTES);
 #pragma unroll
       for (int i = 0; i < MT; ++i) o.a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
     }
@@ -574,11 +584,15 @@ static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) 
   if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
 }
+template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED>
+static int few8_run(const Gemm8Args& g, int groups, hipStream_t s) {
+  const int strips = FEW_WAVES / g.few_nk;
+  few8_kernel<ST, ACT, MT, STREAM, GROUPED><<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, 0, s>>>(g);
+  return launch_status();
+}
 template <typename ST, int ACT, int MT, bool GROUPED>
 static int few8_launch(const Gemm8Args& g, int groups, hipStream_t s) {
-  const int strips = FEW_WAVES / g.few_nk;
-  few8_kernel<ST, ACT, MT, GROUPED><<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, 0, s>>>(g);
-  return launch_status();
+  return g.stream ? few8_run<ST, ACT, MT, true, GROUPED>(g, groups, s) : few8_run<ST, ACT, MT, false, GROUPED>(g, groups, s);
 }
 template <typename ST, int ACT, bool GROUPED>
 static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {

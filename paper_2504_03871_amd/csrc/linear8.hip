@@ -78,6 +78,7 @@ int launch_linear8(const moe_linear8* c, const void* x, const float* xs, const v
   g.M = c->T; g.N = c->d_out; g.K = c->d_in;
   g.chunked = row_tiles_chunked(c->T, c->d_in, c->d_out, 1, mats, 1);
   g.few_nk = few_nk(c->d_out / TILE8_N, c->d_in / TILE8_K);
+  g.stream = streams8((long long)mats * c->d_in * c->d_out);
   g.parts = (int32_t*)ws;
   g.n_parts = cut.parts;
   return gemm8(c->dtype, c->act, g, cut, 0, s);

@@ -488,6 +488,41 @@ def test_matrices_of_more_than_2_to_the_32_elements():
     assert torch.equal(y[-5:], linear8(5, 64, N, "bf16", "none", dx[-5:].contiguous(), sx[-5:].contiguous(), lw, [ws]))
 
 
+@pytest.mark.parametrize("T", [3, 20, 50, 900])
+def test_weights_of_more_than_the_caches_hold(T):
+    """Their first columns' results, and single experts', are those of the same weights by themselves."""
+    torch.manual_seed(T)
+    K, N, n = 8192, 45056, 2048                       # 369 MB, requested as streaming data, and 17 MB
+    any8 = lambda *s: torch.randint(-127, 128, s, dtype=torch.int8, device=DEV)  # noqa: E731
+    x, xs, w, ws = any8(T, K), torch.rand(T, device=DEV), any8(N * K), torch.rand(N, device=DEV) / 5000
+    y = linear8(T, K, N, "bf16", "none", x, xs, [w], [ws])
+    assert torch.equal(y[:, :n], linear8(T, K, n, "bf16", "none", x, xs, [w[:n * K].clone()], [ws[:n].clone()]))
+    for act in ("swiglu", "gelu"):
+        E, k, d, f = 64, 2, 2048, 1024
+        if act == "gelu":
+            f = 1536                                  # 403 MB either way
+        cfg = B.make_cfg(T, d, f, E, k, B.DTYPE_BF16, ACT[act])
+        idx = torch.rand(T, E, device=DEV).topk(k).indices.int().contiguous()
+        i32 = lambda m: torch.empty(m, dtype=torch.int32, device=DEV)  # noqa: E731
+        counts, kept, offsets, row_of, src_of = i32(E), i32(E), i32(E + 1), i32(T * k), i32(T * k)
+        room = torch.empty(max(B.moe_workspace_bytes(cfg), B.moe_expert_ffn8_workspace_bytes(cfg)), dtype=torch.uint8, device=DEV)
+        B.moe_dispatch(cfg, None, idx, None, None, counts, kept, offsets, row_of, src_of, None, room)
+        w1 = [any8(E, d * f) for _ in range(2 if act == "swiglu" else 1)]
+        s1, w2, s2 = [torch.rand(E, f, device=DEV) / 20000 for _ in w1], any8(E, f * d), torch.rand(E, d, device=DEV) / 20000
+        y = empty(T * k, d, dtype="bf16")
+        B.moe_expert_ffn_fwd8(cfg, x[:, :d].contiguous(), xs, w1[0], s1[0], w1[1] if len(w1) > 1 else None, s1[1] if len(w1) > 1 else None, w2, s2, src_of, offsets, kept, None, None, y, room)
+        off = offsets.tolist()
+        for e in range(E):
+            n_rows = off[e + 1] - off[e]
+            if n_rows == 0:
+                continue
+            tok = (src_of[off[e]:off[e + 1]] // k).long()
+            h = linear8(n_rows, d, f, "bf16", act, x[tok, :d].contiguous(), xs[tok].contiguous(), [v[e].clone() for v in w1], [v[e].clone() for v in s1])
+            hc, hs = torch.empty((n_rows, f), dtype=torch.int8, device=DEV), empty(n_rows)
+            B.moe_quant_rows(B.DTYPE_BF16, n_rows, f, f, h, hc, hs)
+            assert torch.equal(y[off[e]:off[e + 1]], linear8(n_rows, f, d, "bf16", "none", hc, hs, [w2[e].clone()], [s2[e].clone()])), e
+
+
 def test_calls_on_two_streams_at_once():
     """Calls with buffers of their own do not see each other."""
     r = np.random.default_rng(7)
