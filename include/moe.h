@@ -522,7 +522,7 @@ MOE_API int moe_quant_weight(int32_t dtype, int32_t n, int32_t d_in, int32_t d_o
 /*
  * moe_linear's forward with both operands in 8 bits, for inference: y = act(z) + residual, z = x_scales w_scales (x W) + bias.
  *   x codes [T][d_in] and x_scales [T] as moe_quant_rows writes them, W, Wb and w_scales, wb_scales [d_out] as moe_quant_weight does (codes of
- *   other origin may be -128); bias, bias_b, residual, y in the storage type `dtype`, as in moe_linear_fwd, act too.
+ *   other origin may be -128); bias, bias_b, residual, y in the storage type `dtype`, as in moe_linear_fwd, act too; residual may be y itself.
  * Sums are 32-bit integers, exact; z, the activation and the residual's addition are fp32 and rounded once.
  * Shapes: 0 <= T <= 2^24, d_in and d_out multiples of 64, d_in <= MOE_MAX_ROW, d_out <= 2^20, d_in * d_out < 2^31.
  * `ws` holds moe_linear8_workspace_bytes, which is enough for any smaller T too and 0 up to 32 (ws may be NULL then), and is free again when
