@@ -1217,8 +1217,13 @@ int moe_expert_ffn_fwd8(const moe_cfg* cfg, const void* x, const float* x_scales
     ProfScope ps(cfg, MOE_PROF_GEMM1_FWD, s);
     CHECK(launch_expert8(cfg->dtype, cfg->act, g1, tr, max_tiles, A, s));
   }
-  CHECK(launch_quant_rows(cfg->dtype, A, f, f, w + l.hidden, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, codes, scales, s));
-  g2.A = codes; g2.a_scale = scales;
+  if (few8_quantises(tr, f)) {
+    g2.A = reinterpret_cast<const int8_t*>(w + l.hidden);
+    g2.quantise = 1;
+  } else {
+    CHECK(launch_quant_rows(cfg->dtype, A, f, f, w + l.hidden, RowRange{offsets, kept, slice_lo, slice_hi, cfg->E}, codes, scales, s));
+    g2.A = codes; g2.a_scale = scales;
+  }
   g2.B = static_cast<const int8_t*>(W2); g2.b_scale = w2_scales;
   g2.N = d; g2.K = f; g2.C = y_perm;
   ProfScope ps(cfg, MOE_PROF_GEMM2_FWD, s);

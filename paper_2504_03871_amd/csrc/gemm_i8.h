@@ -23,6 +23,7 @@ struct Gemm8Args {
   int E;
   int chunked;              // order of the tiles (block_to_tile)
   int stream;               // weights read once are requested as streaming data (streams8)
+  int quantise;             // few rows, no activation: A is rows of the storage type, quantised in the product (few8_quantises)
   int few_nk;               // few rows: waves that share a strip's K range (1, 2, 4 or 8)
   int32_t* parts;           // dense tiles: sums of K parts, [part][matrix][row][N]
   int n_parts;
@@ -50,6 +51,12 @@ inline size_t linear8_ws_bytes(long long T, int N, int mats) {
 inline bool streams8(long long weights) { return weights >= MEMORY_SIDE_CACHE / 4 * 5; }
 // Row tiles of the experts' products: 0 for the few-row kernel
 int expert8_tile_rows(long long rows, int E);
+// Few rows per expert: whether the second product quantises its rows itself, in every block that reads them, instead of a launch in front of
+// it.  (Both products, us, launch -> this: 4 tokens x 8 of 256 experts, d 2048, f 1024, 40.2 -> 36.3; 64 x 4 of 64, d 1024, f 512, 25.2 -> 22.0;
+// 8 x 2 of 8, d 1024, f 2048, 17.6 -> 15.5; where the weights take long the same within 1 %: 32 x 8 of 128 93.3 -> 92.3, 16 x 8 76.8 -> 77.8,
+// 64 x 8 of 128, d 7168, f 2048, 667 -> 673.)
+constexpr int FEW_QUANT_MAX = 2048;   // values of a row: four groups of eight in a lane, two rows to a wave
+inline bool few8_quantises(int tile_rows, int K) { return tile_rows == 0 && K <= FEW_QUANT_MAX; }
 
 int launch_linear8(const moe_linear8* c, const void* x, const float* xs, const void* W, const float* ws8, const void* Wb, const float* wbs, const void* bias,
                    const void* bias_b, const void* residual, void* y, void* ws, hipStream_t s);

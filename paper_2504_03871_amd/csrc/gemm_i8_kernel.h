@@ -432,15 +432,20 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 // last are used.  (16 rows, 16 x 14336 x 4096, four | two in flight: 11.9 | 10.9 us, but 1 x 14336 x 4096 from memory 12.1 | 13.1 and 32 tokens
 // x 8 of 128 experts 93 | 95; eight: worse.)  Bound by the read of the weights: 16 x 4096 x 14336 of two matrices 19.2 us, 6.1 TB/s with a
 // part in the caches, 25.8 (4.6) from memory; 4 tokens x 2 of 8 experts, d 4096, f 14336, 160 us, 6.6 TB/s of 1.06 GB.
+// QUANT: A is rows of the storage type, which every block quantises into LDS for itself while its first weights are on their way (rows.h:
+// the codes and scales that moe_quant_rows gives).
 // Experts: blockIdx.y is the n-th group of 16 MT rows of some expert, which every block finds for itself from the experts' row counts.
 constexpr int FEW_WAVES = 8;
+static_assert(16 * (FEW_QUANT_MAX + 16) + FEW_WAVES * 1024 < 64 * 1024, "LDS of a launch without an attribute");
 
-template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED>
+template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED, bool QUANT>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
   constexpr int MATS = DUAL ? 2 : 1, ROWS = 16 * MT, U = MT == 1 ? 4 : 2;
   __shared__ __align__(16) i32x4 s_sum[FEW_WAVES][MATS * MT][64];
   __shared__ int s_tile[3], s_scan[FEW_WAVES];
+  extern __shared__ __attribute__((aligned(16))) char smem[];   // QUANT: the rows' codes
+  __shared__ float s_scale[ROWS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int e = 0, row0 = blockIdx.y * ROWS, rows = min(ROWS, g.M - row0);
   if constexpr (GROUPED) {
@@ -480,7 +485,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   for (int i = 0; i < MT; ++i)
     pa[i] = g.A + (size_t)row_of_a(g, row0 + min(i * 16 + (lane & 15), rows - 1)) * K + (lane >> 4) * 16;   // (rows past the group repeat its last)
   i32x4 acc[MATS][MT] = {};
-  struct Operands { i32x4 b[U][MATS], a[U][MT]; };
+  const char* la = smem + (QUANT ? min(lane & 15, rows - 1) * (K + 16) + (lane >> 4) * 16 : 0);
+  struct Operands { i32x4 b[U][MATS], a[U][QUANT ? 1 : MT]; };
   auto weights = [](const int8_t* p) {
     if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
     else return *reinterpret_cast<const i32x4*>(p);
@@ -492,8 +498,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
       const size_t at = (size_t)min(k + u * nk, k1 - 1);
       o.b[u][0] = weights(pb + at * TILE8_BYTES);
       if constexpr (DUAL) o.b[u][1] = weights(pb2 + at * TILE8_BYTES);
+      if constexpr (!QUANT) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) o.a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
+        for (int i = 0; i < MT; ++i) o.a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
+      }
     }
   };
   auto use = [&](int k, const Operands& o) {
@@ -501,15 +509,48 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     for (int u = 0; u < U; ++u) {
       if (k + u * nk >= k1) break;
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int i = 0; i < MT; ++i) {
+        i32x4 a;
+        if constexpr (QUANT) a = *reinterpret_cast<const i32x4*>(la + (k + u * nk) * TILE8_K);
+        else a = o.a[u][i];
 #pragma unroll
-        for (int q = 0; q < MATS; ++q) acc[q][i] = mfma8(o.b[u][q], o.a[u][i], acc[q][i]);
+        for (int q = 0; q < MATS; ++q) acc[q][i] = mfma8(o.b[u][q], a, acc[q][i]);
+      }
     }
   };
   int k = kw;
+  Operands x, y;
+  if constexpr (QUANT) {
+    // a wave takes two rows; they are requested before the first weights, whose latency their codes hide in
+    constexpr int RPW = ROWS / FEW_WAVES, NCH = FEW_QUANT_MAX / (8 * WAVE);
+    Raw8<ST> raw[RPW][NCH];
+#pragma unroll
+    for (int r = 0; r < RPW; ++r)
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        raw[r][i] = load_row8<ST, false, false>(reinterpret_cast<const ST*>(g.A) + (size_t)(row0 + min(wave + r * FEW_WAVES, rows - 1)) * K, (i * WAVE + lane) * 8, K);
+    if (k < k1) fetch(k, x);
+#pragma unroll
+    for (int r = 0; r < RPW; ++r) {
+      const int m = wave + r * FEW_WAVES;
+      float v[NCH][8];
+      unsigned top = 0;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        unpack8<ST>(raw[r][i], v[i]);
+        top = top_of(top, v[i]);
+      }
+      if (m >= rows) break;
+      const RowScale q = row_scale(wave_reduce(top, max_u));
+      if (lane == 0) s_scale[m] = q.scale;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i)
+        if ((i * WAVE + lane) * 8 < K) *reinterpret_cast<any_u32x2*>(smem + m * (K + 16) + (i * WAVE + lane) * 8) = codes8(v[i], q.up);
+    }
+    __syncthreads();
+  }
   if (k < k1) {
-    Operands x, y;
-    fetch(k, x);
+    if constexpr (!QUANT) fetch(k, x);
     for (;;) {
       const int k2 = k + U * nk;
       if (k2 < k1) fetch(k2, y);
@@ -539,7 +580,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     const size_t row = row0 + m;
     const size_t cs = (size_t)e * g.N + c;
     const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
-    f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
+    f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], QUANT ? s_scale[m] : g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
     y += load4<ST>(g.residual, row * g.N + c);
     ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
     if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
@@ -584,20 +625,23 @@ static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) 
   if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
 }
-template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED>
+template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED, bool QUANT>
 static int few8_run(const Gemm8Args& g, int groups, hipStream_t s) {
   const int strips = FEW_WAVES / g.few_nk;
-  few8_kernel<ST, ACT, MT, STREAM, GROUPED><<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, 0, s>>>(g);
+  few8_kernel<ST, ACT, MT, STREAM, GROUPED, QUANT>
+      <<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, QUANT ? 16 * MT * (g.K + 16) : 0, s>>>(g);
   return launch_status();
 }
-template <typename ST, int ACT, int MT, bool GROUPED>
+template <typename ST, int ACT, int MT, bool GROUPED, bool QUANT = false>
 static int few8_launch(const Gemm8Args& g, int groups, hipStream_t s) {
-  return g.stream ? few8_run<ST, ACT, MT, true, GROUPED>(g, groups, s) : few8_run<ST, ACT, MT, false, GROUPED>(g, groups, s);
+  return g.stream ? few8_run<ST, ACT, MT, true, GROUPED, QUANT>(g, groups, s) : few8_run<ST, ACT, MT, false, GROUPED, QUANT>(g, groups, s);
 }
 template <typename ST, int ACT, bool GROUPED>
 static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
   constexpr int D = ACT == MOE_ACT_SWIGLU ? 2 : 1;   // columns are of both matrices together
   if (c.few) {
+    if constexpr (GROUPED && ACT == MOE_ACT_NONE)
+      if (g.quantise) return few8_launch<ST, ACT, 1, true, true>(g, max_tiles, s);
     if constexpr (GROUPED) return few8_launch<ST, ACT, 1, true>(g, max_tiles, s);
     else return c.rows == 16 ? few8_launch<ST, ACT, 1, false>(g, 1, s) : few8_launch<ST, ACT, 2, false>(g, 1, s);
   }

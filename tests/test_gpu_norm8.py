@@ -413,11 +413,27 @@ def test_a_token_that_is_no_number_stays_one():
                                                          (300, 3, 2, 128, 320, 0, True), (600, 2, 1, 64, 64, 0, False), (1500, 5, 2, 192, 192, 600, True), (2000, 3, 2, 64, 128, 0, False)])
 def test_experts_are_the_dense_products_of_their_rows(T, E, k, d, f, cap, sliced, act, dtype):
     r = np.random.default_rng(T + E)
-    mats = 2 if act == "swiglu" else 1
-    cfg = B.make_cfg(T, d, f, E, k, DT[dtype], ACT[act], cap)
     idx = np.stack([r.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
     if T > 100:
         idx[r.random((T, k)) < 0.02] = -1                  # dropped assignments
+    check_experts(r, idx, T, E, k, d, f, cap, sliced, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("f", [64, 576, 2048, 2112])
+def test_one_expert_of_many_has_all_tokens(f, act, dtype):
+    """Groups of sixteen rows of it and one of nine, beside experts of one row and of none, in rows up to and beyond those that the second
+    product quantises by itself."""
+    T, E, k = 57, 20, 2
+    r = np.random.default_rng(f)
+    idx = np.stack([np.full(T, 3), np.where(np.arange(T) < 9, np.arange(T) + 7, -1)], axis=1).astype(np.int32)
+    check_experts(r, idx, T, E, k, 128, f, 0, False, act, dtype)
+
+
+def check_experts(r, idx, T, E, k, d, f, cap, sliced, act, dtype):
+    mats = 2 if act == "swiglu" else 1
+    cfg = B.make_cfg(T, d, f, E, k, DT[dtype], ACT[act], cap)
     i32 = lambda n: torch.full((n,), -7, dtype=torch.int32, device=DEV)  # noqa: E731
     counts, kept, offsets, row_of, src_of = i32(E), i32(E), i32(E + 1), i32(T * k), i32(T * k)
     lo = hi = None
