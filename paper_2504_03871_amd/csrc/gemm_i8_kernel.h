@@ -36,6 +36,8 @@ __device__ __forceinline__ f32x4 finish8(const i32x4& a, const i32x4& a2, float 
     if constexpr (ACT == MOE_ACT_SWIGLU) y[v] = silu8<ST>(z) * fmaf((float)a2[v], row * col2[v], bias2[v]);
     else if constexpr (ACT == MOE_ACT_GELU) y[v] = gelu8<ST>(z);
     else y[v] = z;
+    // A number in fp32, also for the compiler, which else rounds a product to fp16 without rounding it to fp32 first, in some kernels.
+    if constexpr (__is_same(ST, f16)) asm("" : "+v"(y[v]));
   }
   return y;
 }
@@ -581,7 +583,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     const size_t cs = (size_t)e * g.N + c;
     const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
     f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], QUANT ? s_scale[m] : g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
-    y += load4<ST>(g.residual, row * g.N + c);
+    if (g.residual != nullptr) y += load4<ST>(g.residual, row * g.N + c);   // (not zeros: -0 would lose its sign)
     ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
     if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
     else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
@@ -604,7 +606,7 @@ __global__ __launch_bounds__(256) void join8_kernel(Gemm8Args g) {
   const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + c), sw2 = MATS > 1 ? *reinterpret_cast<const f32x4*>(g.b2_scale + c) : sw;
   f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], g.a_scale[row], sw, sw2, load4<ST>(g.bias, c), load4<ST>(MATS > 1 ? g.bias2 : nullptr, c));
   const size_t at = (size_t)row * g.N + c;
-  y += load4<ST>(g.residual, at);
+  if (g.residual != nullptr) y += load4<ST>(g.residual, at);
   ST* out = reinterpret_cast<ST*>(g.C) + at;
   if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
   else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};

@@ -399,6 +399,25 @@ def test_a_row_has_the_same_bits_whatever_stands_beside_it(act):
         assert torch.equal(linear8(n, K, N, "bf16", act, dx[:n], xs[:n], dw, ws, res=res[:n].contiguous()), y[:n]), n
 
 
+@pytest.mark.parametrize("act", ["none", "gelu", "swiglu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_every_kernel_gives_a_row_the_same_bits(dtype, act):
+    """Two million results, by strips, by tiles of every size and by K parts: sums just beside a border of fp16, zeros of both signs."""
+    r = np.random.default_rng(6)
+    T, K, N = 512, 1088, 4096
+    x, w = torch.from_numpy(codes(r, T, K)).to(DEV), [torch.randint(-127, 128, (K * N,), dtype=torch.int8, device=DEV) for _ in range(2 if act == "swiglu" else 1)]
+    x[5] = 0
+    xs, ws = dev(r.random(T) + 0.5), [dev((r.random(N) + 0.5) * 10.0 ** r.uniform(-7, -4, N)) for _ in w]
+    bits = lambda y: y.view(torch.int32 if dtype == "f32" else torch.int16)  # noqa: E731
+    y = linear8(T, K, N, dtype, act, x, xs, w, ws)
+    for n in (16, 32, 64, 128, 256):
+        parts = torch.cat([linear8(n, K, N, dtype, act, x[i:i + n].contiguous(), xs[i:i + n].contiguous(), w, ws) for i in range(0, T, n)])
+        assert torch.equal(bits(parts), bits(y)), n
+    # many rows, in the widest tiles
+    many = linear8(8 * T, K, N, dtype, act, x.repeat(8, 1), xs.repeat(8), w, ws)
+    assert torch.equal(bits(many[-T:]), bits(y))
+
+
 def test_a_token_that_is_no_number_stays_one():
     x, xs = torch.ones((3, 64), dtype=torch.int8, device=DEV), dev([1.0, float("nan"), 2.0])
     y = linear8(3, 64, 64, "bf16", "none", x, xs, [laid(np.ones((64, 64), np.int8))], [dev(np.ones(64))])
