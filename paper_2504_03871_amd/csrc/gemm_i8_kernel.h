@@ -428,19 +428,25 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 }
 
 // ---- few rows ----
-// A block of eight waves takes strips of 16 columns and a group of 16 MT rows: 8 / nk strips, the K range of each shared out among nk
-// waves, 64 values at a time in turn, whose sums are added in LDS, in any order the same: they are integers.  An operand of B is one
-// contiguous 1 KB load of a wave, of A 16 rows x 64 bytes that all strips read from the caches; the next U of either are requested before the
-// last are used.  (16 rows, 16 x 14336 x 4096, four | two in flight: 11.9 | 10.9 us, but 1 x 14336 x 4096 from memory 12.1 | 13.1 and 32 tokens
-// x 8 of 128 experts 93 | 95; eight: worse.)  Bound by the read of the weights: 16 x 4096 x 14336 of two matrices 19.2 us, 6.1 TB/s with a
-// part in the caches, 25.8 (4.6) from memory; 4 tokens x 2 of 8 experts, d 4096, f 14336, 160 us, 6.6 TB/s of 1.06 GB.
+// A block of eight waves takes strips of 16 columns (NS = 2: pairs of them) and a group of 16 MT rows: 8 / nk strips, the K range of each shared
+// out among nk waves, 128 values at a time in turn, whose sums are added in LDS, in any order the same: they are integers.  An operand of B is
+// one contiguous 1 KB load of a wave, of A 16 rows x 64 bytes that all strips read from the caches, the other half of whose lines is the next one;
+// the next U of either are requested before the last are used.  (64 values at a time: 16 x 14336 x 4096 16.1 us from memory instead of 14.9,
+// 32 of them 22.1 instead of 19.7, 32 tokens x 2 of 8 experts, d 4096, f 14336, 224 instead of 218.  Two in flight instead of four: 1 x 14336 x
+// 4096 12.1 -> 13.1 and 32 tokens x 8 of 128 experts 93 -> 95; eight: worse.)
+// Bound by the read of the weights, with more than eight rows also by that of A, which takes a lookup for every row: 1 x 4096 x 14336 of two
+// matrices 18.4 us, 6.4 TB/s with a part in the caches, 22.8 (5.1) from memory, 16 rows 19.2 and 25.2; 4 tokens x 2 of 8 experts 160 us, 6.6 TB/s.
+// A pair of strips shares what is read of A, but leaves half as many blocks: worth it with two tiles of rows from 8192 columns on (from memory, one
+// strip | two: 17 x 8192 x 8192 18.8 | 15.3, 32 24.2 | 18.2, 32 x 4096 x 14336 of two matrices 33.1 | 27.5, 32 x 8192 x 28672 77.8 | 61.5,
+// 32 x 2048 x 8192 of two 10.8 | 10.7; 32 x 4096 x 4096 7.9 | 10.0; one tile of rows: 16 x 8192 x 8192 16.8 | 15.4, but 8 14.5 | 15.0).
 // QUANT: A is rows of the storage type, which every block quantises into LDS for itself while its first weights are on their way (rows.h:
 // the codes and scales that moe_quant_rows gives).
 // Experts: blockIdx.y is the n-th group of 16 MT rows of some expert, which every block finds for itself from the experts' row counts.
 constexpr int FEW_WAVES = 8;
+constexpr int FEW_PAIRS = 512;   // strips from which a wave takes two
 static_assert(16 * (FEW_QUANT_MAX + 16) + FEW_WAVES * 1024 < 64 * 1024, "LDS of a launch without an attribute");
 
-template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED, bool QUANT>
+template <typename ST, int ACT, int MT, int NS, bool STREAM, bool GROUPED, bool QUANT>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
   constexpr int MATS = DUAL ? 2 : 1, ROWS = 16 * MT, U = MT == 1 ? 4 : 2;
@@ -477,7 +483,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     rows = __builtin_amdgcn_readfirstlane(s_tile[2]);
   }
   const int nk = g.few_nk, strips = FEW_WAVES / nk, kw = wave % nk;   // this wave's part of K
-  const int K = g.K, KT = K / TILE8_K, n0 = (blockIdx.x * strips + wave / nk) * TILE8_N;
+  const int K = g.K, KT = K / TILE8_K, n0 = (blockIdx.x * strips + wave / nk) * NS * TILE8_N;
   const bool has = n0 < g.N;   // (the last block may have fewer strips)
   const int k1 = has ? KT : 0;
   const size_t strip = ((size_t)e * g.N + n0) * K + lane * 16;
@@ -486,9 +492,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
 #pragma unroll
   for (int i = 0; i < MT; ++i)
     pa[i] = g.A + (size_t)row_of_a(g, row0 + min(i * 16 + (lane & 15), rows - 1)) * K + (lane >> 4) * 16;   // (rows past the group repeat its last)
-  i32x4 acc[MATS][MT] = {};
+  i32x4 acc[NS][MATS][MT] = {};
   const char* la = smem + (QUANT ? min(lane & 15, rows - 1) * (K + 16) + (lane >> 4) * 16 : 0);
-  struct Operands { i32x4 b[U][MATS], a[U][QUANT ? 1 : MT]; };
+  struct Operands { i32x4 b[U][NS][MATS], a[U][QUANT ? 1 : MT]; };
   auto weights = [](const int8_t* p) {
     if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(p));
     else return *reinterpret_cast<const i32x4*>(p);
@@ -497,9 +503,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   auto fetch = [&](int k, Operands& o) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const size_t at = (size_t)min(k + u * nk, k1 - 1);
-      o.b[u][0] = weights(pb + at * TILE8_BYTES);
-      if constexpr (DUAL) o.b[u][1] = weights(pb2 + at * TILE8_BYTES);
+      const size_t at = (size_t)min(k + (u >> 1) * 2 * nk + (u & 1), k1 - 1);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        o.b[u][n][0] = weights(pb + ((size_t)n * KT + at) * TILE8_BYTES);
+        if constexpr (DUAL) o.b[u][n][1] = weights(pb2 + ((size_t)n * KT + at) * TILE8_BYTES);
+      }
       if constexpr (!QUANT) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) o.a[u][i] = *reinterpret_cast<const i32x4*>(pa[i] + at * TILE8_K);
@@ -509,18 +518,21 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
   auto use = [&](int k, const Operands& o) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (k + u * nk >= k1) break;
+      const int kt = k + (u >> 1) * 2 * nk + (u & 1);
+      if (kt >= k1) break;
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         i32x4 a;
-        if constexpr (QUANT) a = *reinterpret_cast<const i32x4*>(la + (k + u * nk) * TILE8_K);
+        if constexpr (QUANT) a = *reinterpret_cast<const i32x4*>(la + kt * TILE8_K);
         else a = o.a[u][i];
 #pragma unroll
-        for (int q = 0; q < MATS; ++q) acc[q][i] = mfma8(o.b[u][q], a, acc[q][i]);
+        for (int n = 0; n < NS; ++n)
+#pragma unroll
+          for (int q = 0; q < MATS; ++q) acc[n][q][i] = mfma8(o.b[u][n][q], a, acc[n][q][i]);
       }
     }
   };
-  int k = kw;
+  int k = 2 * kw;
   Operands x, y;
   if constexpr (QUANT) {
     // a wave takes two rows; they are requested before the first weights, whose latency their codes hide in
@@ -565,28 +577,33 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few8_kernel(Gemm8Args g) {
     }
   }
 #pragma unroll
-  for (int q = 0; q < MATS; ++q)
+  for (int n = 0; n < NS; ++n) {
+    if (n > 0) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MT; ++i) s_sum[wave][q * MT + i][lane] = acc[q][i];
-  __syncthreads();
-  // the strips' MT row tiles of 16 go round the waves
-  for (int j = wave; j < strips * MT; j += FEW_WAVES) {
-    const int st = j / MT, i = j % MT, m = i * 16 + (lane & 15), c = (blockIdx.x * strips + st) * TILE8_N + (lane >> 4) * 4;
-    if (m >= rows || c >= g.N) continue;
-    i32x4 sum[MATS];
+    for (int q = 0; q < MATS; ++q)
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) {
-      sum[q] = s_sum[st * nk][q * MT + i][lane];
-      for (int w = 1; w < nk; ++w) sum[q] += s_sum[st * nk + w][q * MT + i][lane];
+      for (int i = 0; i < MT; ++i) s_sum[wave][q * MT + i][lane] = acc[n][q][i];
+    __syncthreads();
+    // the strips' MT row tiles of 16 go round the waves
+    for (int j = wave; j < strips * MT; j += FEW_WAVES) {
+      const int st = j / MT, i = j % MT, m = i * 16 + (lane & 15), c = ((blockIdx.x * strips + st) * NS + n) * TILE8_N + (lane >> 4) * 4;
+      if (m >= rows || c >= g.N) continue;
+      i32x4 sum[MATS];
+#pragma unroll
+      for (int q = 0; q < MATS; ++q) {
+        sum[q] = s_sum[st * nk][q * MT + i][lane];
+        for (int w = 1; w < nk; ++w) sum[q] += s_sum[st * nk + w][q * MT + i][lane];
+      }
+      const size_t row = row0 + m;
+      const size_t cs = (size_t)e * g.N + c;
+      const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
+      const float sx = QUANT ? s_scale[m] : g.a_scale[row_of_a(g, (int)row)];
+      f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], sx, sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
+      if (g.residual != nullptr) y += load4<ST>(g.residual, row * g.N + c);   // (not zeros: -0 would lose its sign)
+      ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
+      if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
+      else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
     }
-    const size_t row = row0 + m;
-    const size_t cs = (size_t)e * g.N + c;
-    const f32x4 sw = *reinterpret_cast<const f32x4*>(g.b_scale + cs), sw2 = DUAL ? *reinterpret_cast<const f32x4*>(g.b2_scale + cs) : sw;
-    f32x4 y = finish8<ST, ACT>(sum[0], sum[MATS - 1], QUANT ? s_scale[m] : g.a_scale[row_of_a(g, (int)row)], sw, sw2, load4<ST>(g.bias, c), load4<ST>(DUAL ? g.bias2 : nullptr, c));
-    if (g.residual != nullptr) y += load4<ST>(g.residual, row * g.N + c);   // (not zeros: -0 would lose its sign)
-    ST* out = reinterpret_cast<ST*>(g.C) + row * g.N + c;
-    if constexpr (__is_same(ST, float)) *reinterpret_cast<f32x4*>(out) = y;
-    else *reinterpret_cast<u32x2*>(out) = u32x2{Half16<ST>::pack2(y[0], y[1]), Half16<ST>::pack2(y[2], y[3])};
   }
 }
 
@@ -627,25 +644,26 @@ static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) 
   if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
 }
-template <typename ST, int ACT, int MT, bool STREAM, bool GROUPED, bool QUANT>
+template <typename ST, int ACT, int MT, int NS, bool STREAM, bool GROUPED, bool QUANT>
 static int few8_run(const Gemm8Args& g, int groups, hipStream_t s) {
-  const int strips = FEW_WAVES / g.few_nk;
-  few8_kernel<ST, ACT, MT, STREAM, GROUPED, QUANT>
+  const int strips = FEW_WAVES / g.few_nk * NS;
+  few8_kernel<ST, ACT, MT, NS, STREAM, GROUPED, QUANT>
       <<<dim3((g.N / TILE8_N + strips - 1) / strips, groups), FEW_WAVES * 64, QUANT ? 16 * MT * (g.K + 16) : 0, s>>>(g);
   return launch_status();
 }
-template <typename ST, int ACT, int MT, bool GROUPED, bool QUANT = false>
+template <typename ST, int ACT, int MT, int NS, bool GROUPED, bool QUANT = false>
 static int few8_launch(const Gemm8Args& g, int groups, hipStream_t s) {
-  return g.stream ? few8_run<ST, ACT, MT, true, GROUPED, QUANT>(g, groups, s) : few8_run<ST, ACT, MT, false, GROUPED, QUANT>(g, groups, s);
+  return g.stream ? few8_run<ST, ACT, MT, NS, true, GROUPED, QUANT>(g, groups, s) : few8_run<ST, ACT, MT, NS, false, GROUPED, QUANT>(g, groups, s);
 }
 template <typename ST, int ACT, bool GROUPED>
 static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
   constexpr int D = ACT == MOE_ACT_SWIGLU ? 2 : 1;   // columns are of both matrices together
   if (c.few) {
     if constexpr (GROUPED && ACT == MOE_ACT_NONE)
-      if (g.quantise) return few8_launch<ST, ACT, 1, true, true>(g, max_tiles, s);
-    if constexpr (GROUPED) return few8_launch<ST, ACT, 1, true>(g, max_tiles, s);
-    else return c.rows == 16 ? few8_launch<ST, ACT, 1, false>(g, 1, s) : few8_launch<ST, ACT, 2, false>(g, 1, s);
+      if (g.quantise) return few8_launch<ST, ACT, 1, 1, true, true>(g, max_tiles, s);
+    if constexpr (GROUPED) return few8_launch<ST, ACT, 1, 1, true>(g, max_tiles, s);
+    else if (c.rows == 16) return few8_launch<ST, ACT, 1, 1, false>(g, 1, s);
+    else return g.N / TILE8_N >= FEW_PAIRS ? few8_launch<ST, ACT, 2, 2, false>(g, 1, s) : few8_launch<ST, ACT, 2, 1, false>(g, 1, s);
   }
   const long long rt = GROUPED ? max_tiles : (g.M + c.rows - 1) / c.rows;
   if (c.rows == 256) {   // two matrices: four waves down, so that a wave has 64 columns of either and writes whole lines (fp32 has them with 32)
