@@ -6,7 +6,9 @@
 // The norm is that of h as it is stored: the backward, which reads it, differentiates exactly what the forward computed, and a
 // forward from a kept h gives the same bits.  Sums are fp32; every result is rounded once.
 //
-// One pass over memory each: a row stays in the registers of one or several waves (rows.h) between its sums and its results.
+// One pass over memory each: a row stays in the registers of one or several waves (rows.h) between its sums and its results.  Bound by HBM:
+// 16384 rows of 4096, bf16 in an fp32 stream, dropout 0.1: forward 805 MB in 148 us, 5.4 TB/s, backward 1074 MB in 216 us, 5.0 TB/s, and 5 us
+// for adding gamma's partial sums (a copy of 2 GiB runs at 5.6 TB/s).  Small ones by latency: 300 rows of 516 fp32 4.5 and 5.3 us.
 #include "gemm.h"
 #include "norm.h"
 
@@ -246,7 +248,8 @@ __global__ __launch_bounds__(16 * DGAMMA_ROWS) void norm_dgamma_kernel(const flo
 }
 
 // A thread takes U groups of eight adjacent values, 256 apart, and requests them all before it uses the first.  Rows are found by a
-// division of a block's own 32-bit numbers.
+// division of a block's own 32-bit numbers.  32768 rows of 4096 bf16 with a residual 805 MB in 136 us, 5.9 TB/s, without 537 MB in 88, 6.1 TB/s:
+// HBM, with the vector ALUs at 0.77 of their cycles for the generator.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void dropout_kernel(DropArgs drop, const T* x, const T* residual, T* y, long long rows, int width, unsigned groups) {
   const uint64_t offset = drop_offset(drop);
