@@ -66,7 +66,7 @@ __device__ __forceinline__ int row_of_a(const Gemm8Args& g, int r) {
 template <int BM, int BN, bool DUAL, int DEPTH>
 constexpr int gemm8_lds_bytes() { return DEPTH == 2 ? 3 * BM * BK8 + 2 * BN * BK8 * (DUAL ? 2 : 1) : DEPTH * BK8 * (BM + BN * (DUAL ? 2 : 1)); }
 
-template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool GROUPED>
+template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool STREAM, bool GROUPED>
 __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_kernel(Gemm8Args g) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr bool DUAL = ACT == MOE_ACT_SWIGLU;
@@ -123,8 +123,6 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     b_vo[i] = ((unsigned)(n0 / TILE8_N + id / 2) * (unsigned)KT + (unsigned)(id & 1)) * TILE8_BYTES + (unsigned)lane * 16u;
   }
   const int half = wave & 1;
-  // weights that one row tile takes, of more than the caches hold: streaming data (Gemm8Args.stream)
-  const bool once = BM < 256 && g.stream && (GROUPED ? __builtin_amdgcn_readfirstlane(t.mates) == 0 : n_rt == 1);
   const unsigned smem_base = lds_addr(smem);
   const int wbase = wave * 1024;
   int a_fr[2];
@@ -133,12 +131,12 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
   const int b_fr = B_AT + wn * TNN * 2 * TILE8_BYTES + lane * 16;
 
   auto load_a = [&](int q, int stage, int buf) { load_to_lds16(ra, smem_base + buf + wbase + NT * 16 * q, a_vo[q] + (unsigned)stage * BK8); };
-  auto load_b = [&](int q, int stage, int buf) {
+  auto load_b = [&](auto once, int q, int stage, int buf) {
     const int c = DUAL ? q / 2 : q;
     const bool first = !DUAL || q % 2 == 0;
     const unsigned off = 2 * stage + half < KT ? b_vo[c] + (unsigned)stage * (2 * TILE8_BYTES) : OUT_OF_RANGE;
     const unsigned to = smem_base + B_AT + buf + (first ? 0 : B_BYTES) + wbase + NT * 16 * c;
-    if (BM < 256 && once) load_to_lds16_nt(first ? rb : rb2, to, off);
+    if constexpr (decltype(once)::value != 0) load_to_lds16_nt(first ? rb : rb2, to, off);
     else load_to_lds16(first ? rb : rb2, to, off);
   };
   i32x4 af[TM], bf[2][TNN], bf2[2][DUAL ? TNN : 1];
@@ -180,21 +178,21 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     }
   };
 
-  auto request = [&](int stage, int abuf, int bbuf) {
+  auto request = [&](auto once, int stage, int abuf, int bbuf) {
 #pragma unroll
-    for (int q = 0; q < LB; ++q) load_b(q, stage, bbuf);
+    for (int q = 0; q < LB; ++q) load_b(once, q, stage, bbuf);
 #pragma unroll
     for (int q = 0; q < LA; ++q) load_a(q, stage, abuf);
   };
   constexpr int L = LA + LB;
   // s_waitcnt vmcnt(n) lgkmcnt(0): the n newest loads may be in flight, every read of LDS is done
 #define MOE_WAIT8(n_) __builtin_amdgcn_s_waitcnt(((n_) & 15) | (((n_) >> 4) << 14) | 0x70)
-  auto mainloop = [&](int bands) {
+  auto mainloop = [&](auto once, int bands) {
     if constexpr (DEPTH == 2) {
       int a0 = 0, a1 = A_BYTES, a2 = 2 * A_BYTES, b0 = 0, b1 = B_STAGE;
-      request(S0, a0, b0);
+      request(once, S0, a0, b0);
       if (KS - S0 > 1) {
-        request(S0 + 1, a1, b1);
+        request(once, S0 + 1, a1, b1);
         MOE_WAIT8(L);
       } else {
         MOE_WAIT8(0);
@@ -226,7 +224,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
           if constexpr (LOAD) {
 #pragma unroll
             for (int q = 0; q < LB; ++q)
-              if (q * TM / LB == r) load_b(q, S + 2, b0);   // (in the first half of the regions: 0.6 % slower)
+              if (q * TM / LB == r) load_b(once, q, S + 2, b0);   // (in the first half of the regions: 0.6 % slower)
           }
         }, bands);
         const int a = a0; a0 = a1; a1 = a2; a2 = a;
@@ -246,7 +244,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
       static_assert(DEPTH == 3 && 2 * L < 64, "the wait counter");
 #pragma unroll
       for (int q = 0; q < DEPTH; ++q)
-        if (S0 + q < KS) request(S0 + q, q * A_BYTES, q * B_STAGE);
+        if (S0 + q < KS) request(once, S0 + q, q * A_BYTES, q * B_STAGE);
       auto wait_for = [&](int left) {   // all but `left` stages
         if (left >= 2) MOE_WAIT8(2 * L);
         else if (left == 1) MOE_WAIT8(L);
@@ -274,7 +272,7 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
 #pragma unroll
             for (int q = 0; q < L; ++q)
               if (q * TM / L == r) {
-                if (q < LB) load_b(q, S + DEPTH, at * B_STAGE);
+                if (q < LB) load_b(once, q, S + DEPTH, at * B_STAGE);
                 else load_a(q - LB, S + DEPTH, at * A_BYTES);
               }
           }
@@ -289,8 +287,15 @@ __global__ __launch_bounds__(WGM* WGN * 64, PER_CU* WGM* WGN / 4) void gemm8_ker
     }
   };
 #undef MOE_WAIT8
-  if (ni == WTM) mainloop(WTM);
-  else mainloop(ni);
+  if constexpr (STREAM) {
+    // weights that one row tile takes, of more than the caches hold (Gemm8Args.stream).  (Chosen at each load, the wave's branches cost the K
+    // loop a quarter: 128 x 4096 x 4096 11.9 -> 15.6 us.)
+    if (GROUPED ? __builtin_amdgcn_readfirstlane(t.mates) == 0 : n_rt == 1) mainloop(Const<1>{}, ni);
+    else mainloop(Const<0>{}, ni);
+  } else {
+    if (ni == WTM) mainloop(Const<0>{}, WTM);
+    else mainloop(Const<0>{}, ni);
+  }
 
   if (!GROUPED && n_parts > 1) {   // 32-bit sums of this K part, whole lines
     constexpr int CW = TNN * 16;
@@ -633,19 +638,25 @@ __global__ __launch_bounds__(256) void join8_kernel(Gemm8Args g) {
 }
 
 // ---- launches ----
-template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool GROUPED>
-static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) {
+template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool STREAM, bool GROUPED>
+static int gemm8_run(const Gemm8Args& g, long long row_tiles, hipStream_t s) {
   constexpr int LDS = gemm8_lds_bytes<BM, BN, ACT == MOE_ACT_SWIGLU, DEPTH>();
   static_assert(LDS * PER_CU <= LDS_BYTES, "blocks that a compute unit holds");
-  const void* fn = reinterpret_cast<const void*>(gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, GROUPED>);
+  const void* fn = reinterpret_cast<const void*>(gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, STREAM, GROUPED>);
   if (LDS > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
     if (e != hipSuccess) return set_hip_error(e);
   }
   const long long grid = row_tiles * ((g.N + BN - 1) / BN) * (GROUPED ? 1 : g.n_parts);
-  gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, GROUPED><<<(unsigned)grid, WGM * WGN * 64, LDS, s>>>(g);
+  gemm8_kernel<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, STREAM, GROUPED><<<(unsigned)grid, WGM * WGN * 64, LDS, s>>>(g);
   if (!GROUPED && g.n_parts > 1) join8_kernel<ST, ACT><<<(unsigned)(((size_t)g.M * (g.N / 4) + 255) / 256), 256, 0, s>>>(g);
   return launch_status();
+}
+template <typename ST, int ACT, int BM, int BN, int WGM, int WGN, int PER_CU, int DEPTH, bool GROUPED>
+static int gemm8_launch(const Gemm8Args& g, long long row_tiles, hipStream_t s) {
+  if constexpr (BM < 256)
+    if (g.stream) return gemm8_run<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, true, GROUPED>(g, row_tiles, s);
+  return gemm8_run<ST, ACT, BM, BN, WGM, WGN, PER_CU, DEPTH, false, GROUPED>(g, row_tiles, s);
 }
 template <typename ST, int ACT, int MT, int NS, bool STREAM, bool GROUPED, bool QUANT>
 static int few8_run(const Gemm8Args& g, int groups, hipStream_t s) {
