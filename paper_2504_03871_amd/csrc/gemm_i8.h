@@ -34,9 +34,10 @@ struct Gemm8Args {
 inline uint64_t quotient_factor(int k) { return (1ull << 33) / k + 1; }
 static_assert(MOE_MAX_K <= 8, "quotient_factor");
 
-// How a product is cut: up to 32 rows (rows = 16 or 32) in strips of 16 columns, else tiles of rows x cols, their K range in `parts`.
+// How a product is cut: up to 32 rows (rows = 16 or 32) in strips of 16 columns, else tiles of rows x cols, `per_cu` of them to a compute unit, their
+// K range in `parts`.
 constexpr int FEW_ROWS8 = 32, MAX_PARTS8 = 8;
-struct Cut8 { bool few; int rows, cols, parts; };
+struct Cut8 { bool few; int rows, cols, per_cu, parts; };
 Cut8 cut_linear8(long long T, int N, int K, int mats);
 // Room for the parts' sums: enough for any smaller T too.  Tiles that are cut make one round of blocks, 512 of 128 x 128 sums at most.
 inline size_t linear8_ws_bytes(long long T, int N, int mats) {

@@ -4,25 +4,37 @@
 
 namespace moe {
 
-// A tile shape, rows and columns (two matrices: of both together), how many run at a time, and what a round of them takes, us: `fixed` in
-// front of and behind the K loop, and per 128 K values `alone` where few tiles run and `full` where all do.  Fitted to T x d x n, us in the
-// order below: 1024 x 1024 x 1024 15.2 | 7.4 | 6.1; 128 x 4096 x 4096 27.2 | 15.9 | 11.8; 300 x 4096 x 4096 39 | 19 | 13.1; 8192 x 4096 x 1024
-// 43 | 34 | 43; 8192 x 1024 x 4096 42 | 46 | 58; 8192 x 2048 x 8192 122 | 138 | 179; 8192 x 8192 x 8192 432 | 492 | -; two matrices 512 x 2048
-// x 2048 24 | 10.5 | 8.1, 4096 x 2048 x 4096 63 | 72 | 87.  Tiles of 64 in one | two | four | eight parts: 64 x 14336 x 4096 32.5 | 22.4 | 16.7 |
-// 17.2 (strips: 29), 100 x 8192 x 1024 19.1 | 14.0 | 11.2 | 10.9, 128 x 4096 x 4096 11.8 | 12.5 | 13.4 | 19.0.  Strips against the best tiles: 16 x
-// 14336 x 4096 12.1 | 14.9, 32 x 4096 x 4096 7.0 | 9.2, 32 x 14336 x 4096 17.2 | 15.3, 64 x 4096 x 4096 10.7 | 10.8, 24 x 4096 x 14336 of two
-// matrices 20.7 | 22.2, 64 of them - | 20.7 (5.8 TB/s).
+// A tile shape, rows and columns (two matrices: of both together), how many a compute unit holds, and what a round of them takes, us: `fixed`
+// in front of and behind the K loop, and per 128 K values `alone` where up to half of the 256 compute units have a tile, `one` where all have
+// one, `two` where all have two; with a second tile on some, these take nine tenths of that; `second`: what a second matrix adds to `fixed`.
+// Fitted to (us, bf16, in the order of the shapes)
+//   T x K x N             256 x 256   256 x 128   128 x 128: 1 | 2 to a unit   64 x 128
+//   1024 x 1024 x 2048       16.2        10.6             8.4 | 8.0               6.7
+//   300 x 4096 x 4096        39.5        23.4            17.3 | 19.5             13.5
+//   1500 x 2880 x 2048       32.6        21.2            15.2 | 16.2             17.9
+//   3001 x 2880 x 1152       31.3        20.7            16.1 | 17.0             18.1
+//   4096 x 4096 x 1024       40.1        23.9            20.6 | 20.6             23.5
+//   4096 x 4096 x 2048       42.0        33.2            40.4 | 34.3             44.7
+//   3000 x 8192 x 4096       85.2       102             104   | 95.6            116
+//   8192 x 8192 x 2048      100         114             140   | 121             155
+// and alike for two matrices (1500 x 1024 x 1024: 17.0, 10.8, 7.9 | 8.7, 7.8).  What bounds the smaller ones is the caches' traffic: 64 x 128 tiles take 24 KB a stage, 18 TB/s together.
+// Tiles of 64 in one | two | four | eight K parts: 64 x 14336 x 4096 32.5 | 22.4 | 16.7 | 17.2 (strips: 29), 100 x 8192 x 1024 19.1 | 14.0 | 11.2 | 10.9,
+// 128 x 4096 x 4096 11.8 | 12.5 | 13.4 | 19.0.  Strips against the best tiles: 16 x 14336 x 4096 12.1 | 14.9, 32 x 4096 x 4096 7.0 | 9.2, 32 x 14336 x
+// 4096 17.2 | 15.3, 64 x 4096 x 4096 10.7 | 10.8, 24 x 4096 x 14336 of two matrices 20.7 | 22.2, 64 of them - | 20.7 (5.8 TB/s).
 struct Shape8 {
-  int rows, cols, slots;
-  double fixed, alone, full;
-  double us(long long tiles, int stages) const {
-    const long long r = tiles % slots, rounds = tiles / slots;
-    double t = rounds * (fixed + stages * full);
-    if (r > 0) t += fixed + stages * (alone + (full - alone) * r / slots);
+  int rows, cols, per_cu;
+  double fixed, second, alone, one, two;
+  double us(long long tiles, int stages, int mats) const {
+    const long long slots = 256 * per_cu, r = tiles % slots, rounds = tiles / slots;
+    const double around = fixed + (mats - 1) * second;
+    double t = rounds * (around + stages * (per_cu > 1 ? two : one));
+    if (r > 256) t += around + stages * two * (0.9 + 0.1 * (r - 256) / 256);
+    else if (r > 0) t += around + stages * (alone + (one - alone) * std::max(0ll, r - 128) / 128);
     return t;
   }
 };
-constexpr Shape8 SHAPES8[] = {{256, 256, 256, 7.0, 1.0, 1.55}, {128, 128, 512, 3.8, 0.37, 0.9}, {64, 128, 512, 2.5, 0.26, 0.55}};
+constexpr Shape8 SHAPES8[] = {{256, 256, 1, 8.3, 0, 0.98, 1.43, 0}, {256, 128, 1, 6.0, 0, 0.54, 0.81, 0}, {128, 128, 1, 5.3, -0.5, 0.35, 0.485, 0},
+                              {128, 128, 2, 4.4, 0.8, 0.42, 0.52, 0.89}, {64, 128, 2, 4.2, -0.2, 0.27, 0.285, 0.59}};
 constexpr double JOIN8_US = 2.5, JOIN8_US_PER_MB = 0.6;   // the adding launch; sums written and read again
 constexpr int PART8_STAGES = 4;    // stages that a part has at least
 
@@ -36,8 +48,7 @@ static int few_nk(long long strips, int tiles) {
 }
 
 Cut8 cut_linear8(long long T, int N, int K, int mats) {
-
-  if (T <= FEW_ROWS8) return Cut8{true, T <= 16 ? 16 : 32, TILE8_N, 1};
+  if (T <= FEW_ROWS8) return Cut8{true, T <= 16 ? 16 : 32, TILE8_N, 0, 1};
   Cut8 best = {};
   double least = 1e30;
   const int stages = (K + 127) / 128;
@@ -45,10 +56,10 @@ Cut8 cut_linear8(long long T, int N, int K, int mats) {
     const int cols = s.cols / mats;
     const long long tiles = (T + s.rows - 1) / s.rows * ((N + cols - 1) / cols);
     for (int p = 1; p <= MAX_PARTS8; ++p) {
-      if (p > 1 && (s.rows == 256 || p * tiles > s.slots || stages < p * PART8_STAGES)) break;
-      double us = s.us(tiles * p, (stages + p - 1) / p);
+      if (p > 1 && (s.rows == 256 || p * tiles > 256 * s.per_cu || stages < p * PART8_STAGES)) break;
+      double us = s.us(tiles * p, (stages + p - 1) / p, mats);
       if (p > 1) us += JOIN8_US + JOIN8_US_PER_MB * (double)p * T * N * mats * 4 / 1e6;
-      if (us < least) { least = us; best = Cut8{false, s.rows, cols, p}; }
+      if (us < least) { least = us; best = Cut8{false, s.rows, cols, s.per_cu, p}; }
     }
   }
   return best;
@@ -89,7 +100,7 @@ int launch_expert8(int dtype, int act, const Gemm8Args& args, int tile_rows, int
   const int mats = act == MOE_ACT_SWIGLU ? 2 : 1;
   g.chunked = row_tiles_chunked(rows, g.K, g.N, g.E, mats, 1);
   g.n_parts = 1;
-  const Cut8 cut = {tile_rows == 0, tile_rows, 0, 1};
+  const Cut8 cut = {tile_rows == 0, tile_rows, 0, tile_rows == 256 ? 1 : 2, 1};
   if (cut.few) {
     max_tiles = std::min(g.E, rows) + rows / 16;   // every expert's last group may be a part of one
     g.few_nk = few_nk((long long)(g.N / TILE8_N) * std::min(g.E, rows), g.K / TILE8_K);
