@@ -366,7 +366,7 @@ def test_products(T, K, N, dtype, act):
 
 def test_a_tile_of_every_shape():
     """Sizes at which each of the tile shapes is chosen, whole and partly filled."""
-    for T, K, N in ((2048, 256, 4096), (2047, 192, 4032), (8192, 128, 1024), (1500, 1024, 576)):
+    for T, K, N in ((2048, 256, 4096), (2047, 192, 4032), (8192, 128, 1024), (1500, 1024, 576), (1500, 2880, 2048), (1413, 2752, 1984), (4000, 2112, 2048)):
         r = np.random.default_rng(T)
         x, w = codes(r, T, K), codes(r, K, N)
         xs, ws = np.float32(r.random(T) + 0.5), np.float32(r.random(N) + 0.5) / K
@@ -374,6 +374,10 @@ def test_a_tile_of_every_shape():
             y = linear8(T, K, N, dtype, "none", torch.from_numpy(x).to(DEV), dev(xs), [laid(w)], [dev(ws)])
             want = (torch.from_numpy(x).to(DEV).double() @ torch.from_numpy(w).to(DEV).double()).cpu().numpy() * xs.astype(np.float64)[:, None] * ws.astype(np.float64)
             near("y", y, want, 4 * U * np.abs(want) + half_step(dtype) * np.abs(want))
+            res = dev(r.normal(size=(T, N)), dtype)
+            y = linear8(T, K, N, dtype, "none", torch.from_numpy(x).to(DEV), dev(xs), [laid(w)], [dev(ws)], res=res)
+            want_r = want + f64(res)
+            near("y", y, want_r, 5 * U * (np.abs(want) + np.abs(f64(res))) + half_step(dtype) * np.abs(want_r))
 
 
 def test_the_longest_sums_are_exact():
@@ -413,9 +417,10 @@ def test_every_kernel_gives_a_row_the_same_bits(dtype, act):
     for n in (16, 32, 64, 128, 256):
         parts = torch.cat([linear8(n, K, N, dtype, act, x[i:i + n].contiguous(), xs[i:i + n].contiguous(), w, ws) for i in range(0, T, n)])
         assert torch.equal(bits(parts), bits(y)), n
-    # many rows, in the widest tiles
-    many = linear8(8 * T, K, N, dtype, act, x.repeat(8, 1), xs.repeat(8), w, ws)
-    assert torch.equal(bits(many[-T:]), bits(y))
+    # many rows, in the other tiles, the widest last
+    for n in (380, 700, 1000, 1500, 2000, 8 * T):
+        rows = torch.arange(n, device=DEV) % T
+        assert torch.equal(bits(linear8(n, K, N, dtype, act, x[rows], xs[rows], w, ws)), bits(y)[rows]), n
 
 
 def test_a_token_that_is_no_number_stays_one():
