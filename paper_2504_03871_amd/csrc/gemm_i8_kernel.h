@@ -3,7 +3,7 @@
 //
 // Tiles.  v_mfma_i32_16x16x64_i8 has the operand registers of the 16-bit 16 x 16 x 32 instruction and twice its products, so a stage of
 // 128 K values is as many bytes as one of 64 there, and the pipeline is the one of gemm_bf16_kernel.h: LDS stages filled by loads that
-// write LDS directly, three of A and two of B (the smallest tiles: three of both), two K steps to an iteration with one block barrier, in regions of one row tile's
+// write LDS directly, three of A and two of B (64 rows, or 128 that have a compute unit alone: three of both), two K steps to an iteration with one block barrier, in regions of one row tile's
 // instructions each, behind which the reads of the next step's fragments and this step's share of the loads are issued.  A comes in rows and
 // is swizzled in LDS (kc_off); B comes in the order of the instruction (quant8.h) and is read lane by lane.  Sums of 64 K values past
 // the end (an odd number of them) are those of a B of zeros, which the descriptor's byte count gives.
