@@ -686,12 +686,12 @@ static int gemm8_act(const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream
   }
   const long long rt = GROUPED ? max_tiles : (g.M + c.rows - 1) / c.rows;
   // two matrices: four waves down, so that a wave has 64 columns of either and writes whole lines (fp32 has them with 32)
-  if (c.rows == 256 && (GROUPED || c.cols * D == 256)) {
+  if (c.rows == 256 && c.cols * D == 256) {
     constexpr int DOWN = __is_same(ST, float) ? 2 : 2 * D;
     return gemm8_launch<ST, ACT, 256, 256 / D, DOWN, 8 / DOWN, 1, 2, GROUPED>(g, rt, s);
   }
+  if (c.rows == 256) return gemm8_launch<ST, ACT, 256, 128 / D, 4, 2, 1, 2, GROUPED>(g, rt, s);
   if constexpr (!GROUPED) {
-    if (c.rows == 256) return gemm8_launch<ST, ACT, 256, 128 / D, 4, 2, 1, 2, GROUPED>(g, rt, s);
     if (c.rows == 128 && c.per_cu == 1) return gemm8_launch<ST, ACT, 128, 128 / D, 2 * D, 4 / D, 1, 3, GROUPED>(g, rt, s);
   }
   if (c.rows == 128) return gemm8_launch<ST, ACT, 128, 128 / D, 2, 2, 2, 2, GROUPED>(g, rt, s);

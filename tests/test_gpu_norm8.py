@@ -434,7 +434,8 @@ def test_a_token_that_is_no_number_stays_one():
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("act", ["gelu", "swiglu"])
 @pytest.mark.parametrize("T, E, k, d, f, cap, sliced", [(1, 1, 1, 64, 64, 0, False), (4, 16, 2, 128, 192, 0, False), (9, 256, 8, 64, 128, 0, True), (100, 4, 2, 192, 128, 40, False),
-                                                         (300, 3, 2, 128, 320, 0, True), (600, 2, 1, 64, 64, 0, False), (1500, 5, 2, 192, 192, 600, True), (2000, 3, 2, 64, 128, 0, False)])
+                                                         (300, 3, 2, 128, 320, 0, True), (600, 2, 1, 64, 64, 0, False), (1500, 5, 2, 192, 192, 600, True), (2000, 3, 2, 64, 128, 0, False),
+                                                         (2100, 2, 2, 2048, 2048, 0, True)])
 def test_experts_are_the_dense_products_of_their_rows(T, E, k, d, f, cap, sliced, act, dtype):
     r = np.random.default_rng(T + E)
     idx = np.stack([r.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
