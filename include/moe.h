@@ -68,7 +68,7 @@ enum {
   MOE_ERR_ALIGN = -5,     /* a device pointer is not 16-byte aligned */
   MOE_ERR_HIP = -6,       /* a launch failed; see moe_last_hip_error() */
   MOE_ERR_WORKSPACE = -7, /* ws_bytes is smaller than moe_workspace_bytes(cfg) */
-  MOE_ERR_OVERLAP = -8    /* two results of one call at the same address */
+  MOE_ERR_OVERLAP = -8    /* two results of one call at the same address, or a result at that of an operand of another type */
 };
 
 /*
@@ -482,14 +482,16 @@ MOE_API int moe_dropout(int32_t dtype, int64_t rows, int32_t width, const moe_dr
  * x, gamma, y, dy, dx: storage type `dtype` [T][d] ([d]: gamma; NULL: ones).  residual, h, dh_add, dh: type `stream`, dtype or
  * MOE_DTYPE_F32.  rstd [T] fp32.  residual, drop NULL: none.  h NULL: not kept (h may be residual; and x, where the types are one).  rstd
  * NULL: not kept (inference).  y or codes and scales may be NULL, not all of them: codes [T][d] and scales [T] are y in 8 bits, quantised
- * as by moe_quant_rows below before y is rounded to its type.  y may be x (h and y must differ: MOE_ERR_OVERLAP).
+ * as by moe_quant_rows below before y is rounded to its type.  y may be x; h and y must differ, codes from both and from what is read, and where
+ * the types are two h from x and y from residual: MOE_ERR_OVERLAP.
  * The norm is that of h as it is stored, kept or not.  Sums are fp32 (of squares: up to 3.4e38).
  * Any T >= 0 up to 2^24, 1 <= d <= MOE_MAX_NORM; rows that start at multiples of 16 bytes are fastest.
  *
  * Backward: a = gamma dy, u = h rstd; dh = rstd (a - u mean(a u)) + dh_add (NULL: nothing; the gradient that reaches h by other ways), which
  * is the gradient of residual too; dx = dropout's gradient of dh; dgamma = sum over the rows of dy u.  dh, dx, dgamma may be NULL: skipped;
- * dh may be dh_add, and dx or dh may be dy or h (dx not dh: MOE_ERR_OVERLAP).  dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or
- * dtype (accumulate must be 0).  ws holds moe_norm_bwd_workspace_bytes (enough for any smaller T too) and is needed for dgamma only.  No atomics: the same bits every time.
+ * dh may be dh_add or h, dx may be dy, and where the types are one dh may be dy, dx may be h (else, and for dx at dh: MOE_ERR_OVERLAP).
+ * dgamma is of type moe_norm.grad, MOE_DTYPE_F32 (accumulate != 0 adds to it) or dtype (accumulate must be 0).  ws holds
+ * moe_norm_bwd_workspace_bytes (enough for any smaller T too) and is needed for dgamma only.  No atomics: the same bits every time.
  */
 #define MOE_MAX_NORM 16384
 typedef struct moe_norm {
@@ -510,7 +512,7 @@ MOE_API int moe_norm_bwd(const moe_norm* norm, const moe_drop* drop, const void*
  * round(v * (127 / m)) in fp32, ties to even, from -127 to 127, scale m * (1 / 127).  A row or column with an infinity or NaN has codes of
  * zero and the scale NaN: its products are NaN.
  * moe_quant_rows: a matrix of `rows` rows and `width` <= MOE_MAX_ROW columns, `pitch` (>= width) elements from row to row; codes
- * [rows][width] without gaps, scales [rows].  rows * pitch <= 2^40.
+ * [rows][width] without gaps (not at src: MOE_ERR_OVERLAP), scales [rows].  rows * pitch <= 2^40.
  * moe_quant_weight: n matrices [d_in][d_out], d_in and d_out multiples of 64, each below 2^31 values; scales [n][d_out]; codes [n], the
  * d_in * d_out bytes of a matrix in the order in which the products read them: column c and row r lie at byte
  *   ((c / 16) * (d_in / 64) + r / 64) * 1024 + (r % 64 / 16) * 256 + (c % 16) * 16 + r % 16.

@@ -220,7 +220,7 @@ const char* moe_error_string(int code) {
     case MOE_ERR_ALIGN: return "device pointer not 16-byte aligned";
     case MOE_ERR_HIP: return "HIP launch failed (see moe_last_hip_error)";
     case MOE_ERR_WORKSPACE: return "workspace smaller than moe_workspace_bytes(cfg), or problem too large for the static scratch";
-    case MOE_ERR_OVERLAP: return "two results at the same address";
+    case MOE_ERR_OVERLAP: return "two results at the same address, or a result over an operand of another type";
     default: return "unknown error code";
   }
 }
@@ -1057,6 +1057,10 @@ static int check_norm(const moe_norm* n) {
   return MOE_OK;
 }
 
+// Whether a result takes an operand's place, or another result's.  A row is read whole before any of it is written, so one type's rows may be
+// replaced by themselves; rows of another length lie over rows that other blocks may still have to read.
+static bool same_place(const void* a, const void* b) { return a != nullptr && a == b; }
+
 int moe_norm_fwd(const moe_norm* norm, const moe_drop* drop, const void* x, const void* residual, const void* gamma, void* h, float* rstd, void* y,
                  void* codes, float* scales, void* stream) {
   CHECK(check_norm(norm));
@@ -1065,7 +1069,8 @@ int moe_norm_fwd(const moe_norm* norm, const moe_drop* drop, const void* x, cons
   REQUIRE(x);
   if (y == nullptr) REQUIRE(codes);
   if ((codes == nullptr) != (scales == nullptr)) return MOE_ERR_NULL;
-  if (h != nullptr && h == y) return MOE_ERR_OVERLAP;
+  if (same_place(h, y) || same_place(codes, x) || same_place(codes, residual) || same_place(codes, h) || same_place(codes, y)) return MOE_ERR_OVERLAP;
+  if (norm->stream != norm->dtype && (same_place(h, x) || same_place(y, residual))) return MOE_ERR_OVERLAP;
   ALIGNED(x); ALIGNED(residual); ALIGNED(gamma); ALIGNED(h); ALIGNED(rstd); ALIGNED(y); ALIGNED(codes); ALIGNED(scales);
   NormFwdArgs a = {x, residual, gamma, h, rstd, y, (int8_t*)codes, scales, drop_args(drop), norm->T, norm->d, norm->eps};
   return launch_norm_fwd(norm, a, (hipStream_t)stream);
@@ -1083,7 +1088,8 @@ int moe_norm_bwd(const moe_norm* norm, const moe_drop* drop, const void* dy, con
   CHECK(check_norm(norm));
   CHECK(check_drop(drop));
   if (accumulate && norm->grad != MOE_DTYPE_F32) return MOE_ERR_BAD_DTYPE;
-  if (dh != nullptr && dh == dx) return MOE_ERR_OVERLAP;
+  if (same_place(dh, dx)) return MOE_ERR_OVERLAP;
+  if (norm->stream != norm->dtype && (same_place(dx, h) || same_place(dx, dh_add) || same_place(dh, dy))) return MOE_ERR_OVERLAP;
   ALIGNED(dy); ALIGNED(h); ALIGNED(gamma); ALIGNED(rstd); ALIGNED(dh_add); ALIGNED(dh); ALIGNED(dx); ALIGNED(dgamma); ALIGNED(ws);
   if (norm->T > 0) {
     REQUIRE(dy); REQUIRE(h); REQUIRE(rstd);
@@ -1104,6 +1110,7 @@ int moe_quant_rows(int32_t dtype, int64_t rows, int32_t width, int64_t pitch, co
   if (rows == 0) return MOE_OK;
   REQUIRE(src); REQUIRE(codes); REQUIRE(scales);
   ALIGNED(src); ALIGNED(codes); ALIGNED(scales);
+  if (same_place(codes, src)) return MOE_ERR_OVERLAP;
   return launch_quant_rows(dtype, rows, width, pitch, src, RowRange{}, (int8_t*)codes, scales, (hipStream_t)stream);
 }
 
