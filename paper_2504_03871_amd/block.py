@@ -127,9 +127,10 @@ class NormedBlock:
 
 class ServedBlock:
     """The same block as it answers requests, T tokens at a time: every product with weights and activations in 8 bits, a scale for each
-    column and each token.  `source`: a SharedExpertMoE whose weights are quantised here, once; its router is used as it is."""
+    column and each token.  `source`: a SharedExpertMoE whose weights are quantised here, once; its router is used as it is.  `capacity`: rows
+    kept per expert of these T tokens, 0: all of them; the source's counts rows of a training batch, and does not hold here."""
 
-    def __init__(self, source, gamma, T, eps=1e-6):
+    def __init__(self, source, gamma, T, eps=1e-6, capacity=0):
         m, self.T, self.score = source.moe, T, source.score
         dtype, d, f, fs, td = m.cfg.dtype, m.d, m.f, source.Wg.shape[1], m.tdtype
         if dtype == B.DTYPE_F32:
@@ -148,7 +149,7 @@ class ServedBlock:
         self.W1, self.W1b, self.W2 = quantised(m.W1), (None, None) if m.W1b is None else quantised(m.W1b), quantised(m.W2)
         self.Wg, self.Wu, self.Wd = (quantised(w) for w in (source.Wg, source.Wu, source.Wd))
         self.Wr, self.bias, self.balance, self.gamma = m.Wr, m.bias, source.balance, gamma
-        self.cfg = B.make_cfg(T, d, f, m.E, m.k, dtype, m.act, m.cfg.capacity)
+        self.cfg = B.make_cfg(T, d, f, m.E, m.k, dtype, m.act, capacity)
         self.norm = B.make_norm(T, d, dtype, eps=eps)
         self.up, self.down = B.make_linear8(T, d, fs, dtype, B.ACT_SWIGLU), B.make_linear8(T, fs, d, dtype)
         A = T * m.k

@@ -1,0 +1,35 @@
+"""The block that answers requests, beyond the batch that its source was trained with."""
+import numpy as np
+import pytest
+
+from paper_2504_03871_amd import binding as B
+from tests.test_gpu_normed_block import D, EPS, T, normed
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def rows(n, td, seed):
+    return torch.as_tensor(np.random.default_rng(seed).normal(size=(n, D))).to(td).cuda()
+
+
+def test_more_tokens_than_a_training_batch_that_had_a_capacity():
+    """A token's answer is the one it gets by itself: no expert turns a request away because of others in the call."""
+    from paper_2504_03871_amd.block import ServedBlock
+    n = normed(B.DTYPE_BF16)
+    n.block.moe.cfg.capacity = 5
+    n_tokens = 2 * T + 3
+    s = ServedBlock(n.block, n.gamma, n_tokens, eps=EPS)
+    x, res = rows(n_tokens, torch.bfloat16, 1), rows(n_tokens, torch.bfloat16, 2)
+    out = s.forward(x, res)[0].clone()
+    assert torch.equal(s.kept, s.counts) and int(s.counts.max()) > 5
+    one = ServedBlock(n.block, n.gamma, 1, eps=EPS)
+    for i in (0, 7, n_tokens - 1):
+        got = one.forward(x[i:i + 1], res[i:i + 1])[0]
+        assert torch.equal(one.topk_idx[0], s.topk_idx[i])
+        # the gate's product for few tokens may add up in another order, which moves a weight's last bits and so one rounding of the routed sum and one
+        # of out, each by at most a whole step: half of this where neither is above twice the row's largest result
+        assert bool(((got[0].double() - out[i].double()).abs() <= 4 * 2.0 ** -8 * out[i].double().abs().max()).all())
+    limited = ServedBlock(n.block, n.gamma, n_tokens, eps=EPS, capacity=5)
+    limited.forward(x, res)
+    assert int(limited.kept.max()) == 5
