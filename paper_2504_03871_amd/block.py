@@ -87,6 +87,10 @@ class SharedExpertMoE:
         self.balance += rate * torch.sign(load.mean() - load)
 
 
+def _torch_type(dtype):
+    return {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(dtype, torch.float32)
+
+
 class NormedBlock:
     """A SharedExpertMoE with what a network has in front of it, in training: the residual stream takes in the last block's output, with
     dropout, and the block sees its norm.
@@ -101,7 +105,7 @@ class NormedBlock:
         self.block, m = block, block.moe
         T, d, dtype = m.T, m.d, m.cfg.dtype
         self.norm = B.make_norm(T, d, dtype, stream, eps=eps)
-        st = {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(self.norm.stream, torch.float32)
+        st = _torch_type(self.norm.stream)
         e = lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device=m.device)  # noqa: E731
         self.step = torch.zeros(1, dtype=torch.int64, device=m.device)
         self.drop = B.make_drop(p, seed, layer << 32, self.step) if p > 0 else None
@@ -128,9 +132,10 @@ class NormedBlock:
 class ServedBlock:
     """The same block as it answers requests, T tokens at a time: every product with weights and activations in 8 bits, a scale for each
     column and each token.  `source`: a SharedExpertMoE whose weights are quantised here, once; its router is used as it is.  `capacity`: rows
-    kept per expert of these T tokens, 0: all of them; the source's counts rows of a training batch, and does not hold here."""
+    kept per expert of these T tokens, 0: all of them; the source's counts rows of a training batch, and does not hold here.
+    `stream`: type of the residual stream, as in NormedBlock."""
 
-    def __init__(self, source, gamma, T, eps=1e-6, capacity=0):
+    def __init__(self, source, gamma, T, eps=1e-6, capacity=0, stream=None):
         m, self.T, self.score = source.moe, T, source.score
         dtype, d, f, fs, td = m.cfg.dtype, m.d, m.f, source.Wg.shape[1], m.tdtype
         if dtype == B.DTYPE_F32:
@@ -150,10 +155,10 @@ class ServedBlock:
         self.Wg, self.Wu, self.Wd = (quantised(w) for w in (source.Wg, source.Wu, source.Wd))
         self.Wr, self.bias, self.balance, self.gamma = m.Wr, m.bias, source.balance, gamma
         self.cfg = B.make_cfg(T, d, f, m.E, m.k, dtype, m.act, capacity)
-        self.norm = B.make_norm(T, d, dtype, eps=eps)
+        self.norm = B.make_norm(T, d, dtype, stream, eps=eps)
         self.up, self.down = B.make_linear8(T, d, fs, dtype, B.ACT_SWIGLU), B.make_linear8(T, fs, d, dtype)
         A = T * m.k
-        self.h, self.y, self.codes, self.scales, self.out = e(T, d), e(T, d), i8(T, d), f32(T), e(T, d)
+        self.h, self.y, self.codes, self.scales, self.out = e(T, d, dtype=_torch_type(self.norm.stream)), e(T, d), i8(T, d), f32(T), e(T, d)
         self.logits, self.topk_idx, self.topk_w = f32(T, m.E), i32(T, m.k), f32(T, m.k)
         self.counts, self.kept, self.offsets, self.row_of, self.src_of, self.y_perm = i32(m.E), i32(m.E), i32(m.E + 1), i32(A), i32(A), e(A, d)
         self.hidden, self.hidden_codes, self.hidden_scales = e(T, fs), i8(T, fs), f32(T)

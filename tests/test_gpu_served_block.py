@@ -33,3 +33,20 @@ def test_more_tokens_than_a_training_batch_that_had_a_capacity():
     limited = ServedBlock(n.block, n.gamma, n_tokens, eps=EPS, capacity=5)
     limited.forward(x, res)
     assert int(limited.kept.max()) == 5
+
+
+@pytest.mark.parametrize("stream", [None, B.DTYPE_F32])
+def test_two_blocks_have_the_stream_of_those_they_serve(stream):
+    """h is the training block's, bit for bit where both take the same rows; out within what 8 bits cost."""
+    from paper_2504_03871_amd.block import ServedBlock
+    train = [normed(B.DTYPE_BF16, stream, 0.0, i, i) for i in range(2)]
+    serve = [ServedBlock(n.block, n.gamma, T, eps=EPS, stream=stream) for n in train]
+    x, res = rows(T, torch.bfloat16, 3), rows(T, torch.bfloat16, 4).to(train[0].h.dtype) / 3
+    want, wh = train[0].forward(x, res)
+    got, h = serve[0].forward(x, res)
+    assert h.dtype == wh.dtype and torch.equal(h, wh)
+    got, h2 = serve[1].forward(want, h)
+    want, wh2 = train[1].forward(want, wh)
+    assert torch.equal(h2, wh2)
+    # as tests/test_gpu_normed_block.py: 0.7 % of a product's terms, for two operands, in three products, at four times that
+    assert float((got.double() - want.double()).norm() / want.double().norm()) <= 0.06

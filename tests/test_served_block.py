@@ -26,3 +26,9 @@ def test_the_training_batch_s_capacity_is_no_limit_on_requests(monkeypatch, T):
     src = source(capacity=3)
     assert served(monkeypatch, src, T).cfg.capacity <= 0          # unlimited
     assert served(monkeypatch, src, T, capacity=9).cfg.capacity == 9
+
+
+def test_the_residual_stream_may_be_of_full_precision(monkeypatch):
+    assert served(monkeypatch).h.dtype == torch.bfloat16
+    s = served(monkeypatch, stream=B.DTYPE_F32)
+    assert s.h.dtype == torch.float32 and s.norm.stream == B.DTYPE_F32 and s.norm.dtype == B.DTYPE_BF16 and s.out.dtype == torch.bfloat16
