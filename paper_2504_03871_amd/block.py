@@ -91,6 +91,12 @@ def _torch_type(dtype):
     return {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(dtype, torch.float32)
 
 
+def _check_rows(name, t, like, *shape):
+    """A caller's tensor: kernels take its address alone, and would read past the end of a smaller one."""
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be {list(shape)} of {like.dtype} on {like.device}, contiguous")
+
+
 class NormedBlock:
     """A SharedExpertMoE with what a network has in front of it, in training: the residual stream takes in the last block's output, with
     dropout, and the block sees its norm.
@@ -116,13 +122,18 @@ class NormedBlock:
         self.ws = e(max(256, B.moe_norm_bwd_workspace_bytes(self.norm)), dtype=torch.uint8)
 
     def forward(self, branch, residual=None):
-        """(out, h)."""
+        """(out, h).  branch: [T, d] of the block's type, residual: of the stream's."""
+        _check_rows("branch", branch, self.block.moe.x, *self.h.shape)
+        if residual is not None:
+            _check_rows("residual", residual, self.h, *self.h.shape)
         B.moe_norm_fwd(self.norm, self.drop, branch, residual, self.gamma, self.h, self.rstd, self.block.moe.x, None, None)
         self.block.forward()
         return self.block.moe.out, self.h
 
     def backward(self, d_h=None, accumulate=0):
         """(gradient of branch, gradient of residual) from block.moe.d_out and `d_h`, what reaches h past this block."""
+        if d_h is not None:
+            _check_rows("d_h", d_h, self.h, *self.h.shape)
         self.block.backward(accumulate)
         B.moe_norm_bwd(self.norm, self.drop, self.block.moe.dx, self.h, self.gamma, self.rstd, d_h, self.dh,
                        None if self.d_branch is self.dh else self.d_branch, self.dgamma, accumulate, self.ws)
@@ -140,6 +151,7 @@ class ServedBlock:
         dtype, d, f, fs, td = m.cfg.dtype, m.d, m.f, source.Wg.shape[1], m.tdtype
         if dtype == B.DTYPE_F32:
             raise ValueError("8-bit products of experts have results of 16 bits")
+        _check_rows("gamma", gamma, m.x, d)
         e = lambda *s, dtype=td: torch.empty(*s, dtype=dtype, device=m.device)  # noqa: E731
         i32 = lambda *s: e(*s, dtype=torch.int32)  # noqa: E731
         f32 = lambda *s: e(*s, dtype=torch.float32)  # noqa: E731
@@ -167,6 +179,9 @@ class ServedBlock:
 
     def forward(self, branch, residual=None):
         """(out, h) as NormedBlock's, without dropout."""
+        _check_rows("branch", branch, self.y, *self.h.shape)
+        if residual is not None:
+            _check_rows("residual", residual, self.h, *self.h.shape)
         B.moe_norm_fwd(self.norm, None, branch, residual, self.gamma, self.h, None, self.y, self.codes, self.scales)
         B.moe_route_scored(self.cfg, self.score, self.y, self.Wr, self.bias, self.balance, None, self.logits, self.topk_idx, self.topk_w, self.ws)
         B.moe_dispatch(self.cfg, None, self.topk_idx, None, None, self.counts, self.kept, self.offsets, self.row_of, self.src_of, None, self.ws)

@@ -32,3 +32,56 @@ def test_the_residual_stream_may_be_of_full_precision(monkeypatch):
     assert served(monkeypatch).h.dtype == torch.bfloat16
     s = served(monkeypatch, stream=B.DTYPE_F32)
     assert s.h.dtype == torch.float32 and s.norm.stream == B.DTYPE_F32 and s.norm.dtype == B.DTYPE_BF16 and s.out.dtype == torch.bfloat16
+
+
+def norm_calls(monkeypatch):
+    """Nothing may be launched: what the norm is called with."""
+    calls = []
+    for name in ("moe_norm_fwd", "moe_norm_bwd"):
+        monkeypatch.setattr(B, name, lambda *a, **k: calls.append(a))
+    from paper_2504_03871_amd.block import SharedExpertMoE
+    monkeypatch.setattr(SharedExpertMoE, "forward", lambda self: None)
+    monkeypatch.setattr(SharedExpertMoE, "backward", lambda self, accumulate=0: None)
+    return calls
+
+
+def wrong(T, d, dtype, other):
+    """Tensors that are not [T, d] of dtype, without gaps, on this device."""
+    return [torch.empty(T, d, dtype=other), torch.empty(T - 1, d, dtype=dtype), torch.empty(T, d + 8, dtype=dtype), torch.empty(T * d, dtype=dtype),
+            torch.empty(T, 2 * d, dtype=dtype)[:, ::2], torch.empty(d, T, dtype=dtype).T, torch.empty(T, d, dtype=dtype, device="meta")]
+
+
+@pytest.mark.parametrize("stream", [None, B.DTYPE_F32])
+def test_operands_that_are_not_the_block_s_rows_are_refused(monkeypatch, stream):
+    from paper_2504_03871_amd.block import NormedBlock
+    T, d, half = SIZES["T"], SIZES["d_model"], torch.bfloat16
+    st, not_st = (half, torch.float32) if stream is None else (torch.float32, half)
+    calls = norm_calls(monkeypatch)
+    n, s = NormedBlock(source(), stream=stream), served(monkeypatch, T=T, stream=stream)
+    branch, res = torch.empty(T, d, dtype=half), torch.empty(T, d, dtype=st)
+    for b in (n, s):
+        for t in wrong(T, d, half, torch.float16) + [None]:
+            with pytest.raises(ValueError, match="branch"):
+                b.forward(t, res)
+        for t in wrong(T, d, st, not_st):
+            with pytest.raises(ValueError, match="residual"):
+                b.forward(branch, t)
+    for t in wrong(T, d, st, not_st):
+        with pytest.raises(ValueError, match="d_h"):
+            n.backward(t)
+    assert not calls
+    n.forward(branch)
+    n.forward(branch, res)
+    n.backward()
+    n.backward(res)
+    assert len(calls) == 4
+
+
+def test_gamma_is_a_row_of_the_block_s_type(monkeypatch):
+    from paper_2504_03871_amd.block import ServedBlock
+    src = source()
+    served(monkeypatch, src)
+    for g in (torch.ones(SIZES["d_model"]), torch.ones(SIZES["d_model"] + 1, dtype=torch.bfloat16), torch.ones(1, SIZES["d_model"], dtype=torch.bfloat16),
+              torch.ones(2 * SIZES["d_model"], dtype=torch.bfloat16)[::2], None):
+        with pytest.raises(ValueError, match="gamma"):
+            ServedBlock(src, g, 4)
