@@ -108,6 +108,8 @@ class NormedBlock:
     their own."""
 
     def __init__(self, block, stream=None, p=0.0, seed=0, layer=0, eps=1e-6):
+        if not 0 <= p < 1:
+            raise ValueError("dropout's probability must be 0 <= p < 1")
         self.block, m = block, block.moe
         T, d, dtype = m.T, m.d, m.cfg.dtype
         self.norm = B.make_norm(T, d, dtype, stream, eps=eps)

@@ -85,3 +85,10 @@ def test_gamma_is_a_row_of_the_block_s_type(monkeypatch):
               torch.ones(2 * SIZES["d_model"], dtype=torch.bfloat16)[::2], None):
         with pytest.raises(ValueError, match="gamma"):
             ServedBlock(src, g, 4)
+
+
+@pytest.mark.parametrize("p", [-0.1, 1.0, float("nan"), 2.0])
+def test_a_probability_that_is_none_is_refused(p):
+    from paper_2504_03871_amd.block import NormedBlock
+    with pytest.raises(ValueError, match="0 <= p < 1"):
+        NormedBlock(source(), p=p)
