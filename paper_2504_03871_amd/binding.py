@@ -460,7 +460,7 @@ def make_drop(p, seed, offset=0, step=None) -> MoeDrop:
     """Dropout of probability p; `seed` and `offset` name the mask.  `step`: a tensor of one int64 on the GPU, added to offset when the
     kernel runs; the caller keeps it alive."""
     if step is not None and not isinstance(step, int):
-        if step.element_size() != 8 or step.numel() < 1 or not step.is_cuda:
+        if step.element_size() != 8 or step.is_floating_point() or step.is_complex() or step.numel() < 1 or not step.is_cuda:
             raise ValueError("step must be a 64-bit integer on the GPU")
         step = step.data_ptr()
     return MoeDrop(int(seed) % (1 << 64), int(offset) % (1 << 64), step, float(p))

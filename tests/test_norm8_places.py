@@ -50,3 +50,16 @@ def test_codes_have_a_place_of_their_own():
     for at in (X, R, H, Y):
         overlaps(B.moe_norm_fwd, norm, None, X, R, G, H, RS, Y, at, RS, stream=S)
     overlaps(B.moe_quant_rows, B.DTYPE_BF16, 5, 64, 64, X, X, RS, stream=S)
+
+
+def test_drop_s_step_is_a_whole_number():
+    """64 bits of another kind would name a mask by their pattern."""
+    import torch
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+    made = lambda dtype: torch.zeros(2, dtype=dtype).as_subclass(OnGpu)  # noqa: E731
+    assert B.make_drop(0.1, 1, 0, made(torch.int64)).step
+    for dtype in (torch.float64, torch.complex64, torch.int32, torch.float32):
+        with pytest.raises(ValueError):
+            B.make_drop(0.1, 1, 0, made(dtype))
