@@ -21,6 +21,8 @@ namespace moe {
 // Tiles of 64 in one | two | four | eight K parts: 64 x 14336 x 4096 32.5 | 22.4 | 16.7 | 17.2 (strips: 29), 100 x 8192 x 1024 19.1 | 14.0 | 11.2 | 10.9,
 // 128 x 4096 x 4096 11.8 | 12.5 | 13.4 | 19.0.  Strips against the best tiles: 16 x 14336 x 4096 12.1 | 14.9, 32 x 4096 x 4096 7.0 | 9.2, 32 x 14336 x
 // 4096 17.2 | 15.3, 64 x 4096 x 4096 10.7 | 10.8, 24 x 4096 x 14336 of two matrices 20.7 | 22.2, 64 of them - | 20.7 (5.8 TB/s).
+// Up to 32 rows always strips, also where tiles in K parts are faster (17 to 32 rows of long K): those calls need no workspace, which the
+// interface promises and a program that generates relies on.
 struct Shape8 {
   int rows, cols, per_cu;
   double fixed, second, alone, one, two;
@@ -71,6 +73,9 @@ Cut8 cut_linear8(long long T, int N, int K, int mats) {
 //   128: 398 | 157 | 136 | 159     1024: - | 744 | 575 | 525;     128 experts, 512: - | 828 | 653 | 565
 // d 4096, f 14336, 8 experts
 //   2: 213 | 223 | 258 | 321     4: 239 | 251 | 271 | 335     16: 337 | 253 | 275 | 340     64: 930 | 384 | 299 | 350     256: - | 784 | 633 | 498
+// Fitted to eight experts or more.  With fewer the line comes early: from eight rows per expert to nine, d 4096, f 14336, 1 expert 36 -> 57,
+// 2 66 -> 99, 4 115 -> 144, 8 221 -> 238; d 2048, f 1024, 10.4 -> 17.5, 10.6 -> 17.6, 12.2 -> 19.0, 15.7 -> 20.4: tiles of 64 rows without K parts
+// leave compute units idle.  And it goes by the mean: where one expert has nearly all rows, strips read its weights once for every sixteen.
 int expert8_tile_rows(long long rows, int E) { return rows <= 8ll * E ? 0 : rows <= 40ll * E ? 64 : rows <= 200ll * E ? 128 : 256; }
 
 static int gemm8(int dtype, int act, const Gemm8Args& g, const Cut8& c, int max_tiles, hipStream_t s) {
