@@ -91,10 +91,11 @@ def _torch_type(dtype):
     return {B.DTYPE_BF16: torch.bfloat16, B.DTYPE_F16: torch.float16}.get(dtype, torch.float32)
 
 
-def _check_rows(name, t, like, *shape):
-    """A caller's tensor: kernels take its address alone, and would read past the end of a smaller one."""
-    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{name} must be {list(shape)} of {like.dtype} on {like.device}, contiguous")
+def _check_rows(name, t, like, rows, d):
+    """A caller's tensor, [rows, d] or split further in front of d: kernels take its address alone, and would read past the end of a smaller one."""
+    if (not isinstance(t, torch.Tensor) or t.shape[-1:] != (d,) or t.numel() != rows * d or t.dtype != like.dtype or t.device != like.device
+            or not t.is_contiguous()):
+        raise ValueError(f"{name} must be [{rows}, {d}] of {like.dtype} on {like.device}, contiguous")
 
 
 class NormedBlock:
@@ -153,7 +154,7 @@ class ServedBlock:
         dtype, d, f, fs, td = m.cfg.dtype, m.d, m.f, source.Wg.shape[1], m.tdtype
         if dtype == B.DTYPE_F32:
             raise ValueError("8-bit products of experts have results of 16 bits")
-        _check_rows("gamma", gamma, m.x, d)
+        _check_rows("gamma", gamma, m.x, 1, d)
         e = lambda *s, dtype=td: torch.empty(*s, dtype=dtype, device=m.device)  # noqa: E731
         i32 = lambda *s: e(*s, dtype=torch.int32)  # noqa: E731
         f32 = lambda *s: e(*s, dtype=torch.float32)  # noqa: E731

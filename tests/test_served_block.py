@@ -74,14 +74,15 @@ def test_operands_that_are_not_the_block_s_rows_are_refused(monkeypatch, stream)
     n.forward(branch, res)
     n.backward()
     n.backward(res)
-    assert len(calls) == 4
+    n.forward(branch.view(2, T // 2, d), res.view(4, 2, T // 8, d))      # sequences of a batch
+    assert len(calls) == 5
 
 
 def test_gamma_is_a_row_of_the_block_s_type(monkeypatch):
     from paper_2504_03871_amd.block import ServedBlock
     src = source()
     served(monkeypatch, src)
-    for g in (torch.ones(SIZES["d_model"]), torch.ones(SIZES["d_model"] + 1, dtype=torch.bfloat16), torch.ones(1, SIZES["d_model"], dtype=torch.bfloat16),
+    for g in (torch.ones(SIZES["d_model"]), torch.ones(SIZES["d_model"] + 1, dtype=torch.bfloat16), torch.ones(2, SIZES["d_model"], dtype=torch.bfloat16),
               torch.ones(2 * SIZES["d_model"], dtype=torch.bfloat16)[::2], None):
         with pytest.raises(ValueError, match="gamma"):
             ServedBlock(src, g, 4)
